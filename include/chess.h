@@ -7,7 +7,7 @@
  *
  * C ABI.  Every data pointer is a DEVICE pointer owned by the caller unless it says "host".
  * The library never allocates or frees device memory; only chess_append_kv and chess_reuse_step write the K/V
- * pools (the appended token's rows, nothing else).  Every call is
+ * pools (the appended token's rows, nothing else), and only chess_quant_store 8-bit pools.  Every call is
  * asynchronous on `stream` (a hipStream_t passed as void*, NULL = the default stream), does no
  * host synchronisation, and can be captured in a HIP graph.  A context caches launch shapes: calls on one
  * context must not run concurrently from several host threads (use one context per thread).
@@ -338,6 +338,83 @@ int chess_workspace_error(chess_ctx* ctx, const void* workspace, int32_t* flag, 
 int chess_sparse_decode_static(chess_ctx* ctx, const void* q, const void* k_pool, const void* v_pool,
                                const int32_t* block_table, const int32_t* seq_lens, const int32_t* page_ids,
                                const int32_t* n_selected, int32_t batch, float* out, void* stream);
+
+/*
+ * ---- Pages handed out on the device ----------------------------------------------------------------------------
+ * Block tables and slot maps from request lengths, without the host: a list of free physical pages and its length live in device
+ * memory, chess_release_pages puts the pages of ended sequences back, chess_map_tokens deals pages to the tokens of the next step and says
+ * where each token goes.  A page belongs to one sequence at a time.  lens_after may be seq_lens and n_left may be n_free (in place).
+ * Both use the workspace (an arrival counter).  CHESS_EINVAL on null or misaligned pointers, sizes outside the configuration, or when the
+ * context's device is not the current one; CHESS_ENOTSUP for batch above 4096.
+ */
+#define CHESS_MAX_TOKENS (1 << 29)   /* most new tokens of one chess_map_tokens call */
+
+/* Entries that the `writes` array of chess_map_tokens must have room for: min(max_tokens, max_tokens / B + 2 batch). */
+int chess_write_rows(const chess_ctx* ctx, int32_t max_tokens, int32_t batch, size_t* rows);
+
+/*
+ * done: device int32 [batch].  For every sequence with done[b] != 0, in order: its ceil(seq_lens[b] / B) pages, in logical order, are appended
+ * to free_pages [capacity] behind the *n_free entries it holds, and lens_after[b] = 0; the other lengths are copied.  The block table
+ * is not changed.  Should the list be too short for a sequence's pages, that sequence and those behind it keep theirs.
+ * *n_left = the list's new length.
+ */
+int chess_release_pages(chess_ctx* ctx, const int32_t* seq_lens, const int32_t* done, int32_t batch, const int32_t* block_table,
+                        int32_t* free_pages, int32_t capacity, const int32_t* n_free, int32_t* lens_after, int32_t* n_left, void* workspace,
+                        void* stream);
+
+/*
+ * new_lens: device int32 [batch], the tokens each sequence wants behind the seq_lens[b] it holds (<= 0: none).  A sequence whose row has no room
+ * (length + tokens above max_pages_per_seq * page_size, or a negative length) gets nothing; otherwise sequences are served in order
+ * as long as their tokens add up to at most max_tokens and the new pages to at most *n_free: the first that does not fit and all behind it get
+ * nothing.  Pages are taken from the end of free_pages.  Written:
+ *   block_table  the entries of the new pages (nothing else of it)
+ *   lens_after   int32 [batch]       seq_lens plus the tokens that a sequence got
+ *   n_left       int32               *n_free minus the pages taken (free_pages itself is not changed)
+ *   token_start  int32 [batch + 1]   where each sequence's tokens start among all of them; the last entry is their number
+ *   slots        int64 [max_tokens]  page * B + offset of every token; entries behind the last token are left as they are.  May be NULL
+ *   writes       int32 [rows][4], rows from chess_write_rows, 16-byte aligned: one entry a touched page, in token order: {physical page, row of its
+ *                first new token, offset of that token in the page, new tokens in the page}; entries behind the last are left as they are
+ *   counts       int32 [4]           {tokens, entries of `writes`, pages taken, sequences that wanted tokens and got none}
+ */
+int chess_map_tokens(chess_ctx* ctx, const int32_t* seq_lens, const int32_t* new_lens, int32_t batch, int32_t max_tokens, int32_t* block_table,
+                     const int32_t* free_pages, const int32_t* n_free, int32_t* lens_after, int32_t* n_left, int32_t* token_start, int64_t* slots,
+                     int32_t* writes, int32_t* counts, void* workspace, void* stream);
+
+/*
+ * ---- The cache in 8 bits ---------------------------------------------------------------------------------------
+ * Half the bytes of the bf16 pools, the same pages, block tables, lists and summaries:
+ *   K pool   e4m3 (OCP; no infinities, NaN = 0x7f) [physical page][H][B][d]
+ *   V pool   e4m3 [physical page][H][d][B]              (token-minor inside a page)
+ *   scales   fp32 [physical page][H][2]                 of the page's keys, of its values: powers of two between 2^-64 and 2^119; a
+ *                                                       byte stands for its e4m3 value times that
+ * Pools 16-byte aligned, scales 8-byte.  CHESS_EINVAL also when the context's device is not the current one.
+ */
+
+/*
+ * New tokens into the pages that chess_map_tokens dealt them (writes, counts: as it leaves them; only counts[1] is read; max_writes: the
+ * entries `writes` has room for, which the launch is sized by).  k_new, v_new: bf16 [token][H][128], k_stride / v_stride elements from a token to
+ * the next (>= H * 128, a multiple of 8: the keys and values may be slices of a wider projection), 16-byte aligned.
+ * Per page and head, keys and values each: scale = 2^e, the smallest with max |x| <= 448 * 2^e over the page's new values (-64 <= e <= 119), or
+ * the page's own scale if it held tokens before (an offset above 0) and its scale is larger.  A byte is x / 2^e rounded to nearest even,
+ * saturated at 448; a value that is not finite is stored as NaN and left out of the maximum.  When a page's scale grows, the tokens it held are
+ * moved to it (exact but where they become subnormal: below 2^-6 of the scale).  Bytes behind the new tokens are left as they are.
+ * No two entries may name the same page.
+ */
+int chess_quant_store(chess_ctx* ctx, const void* k_new, int64_t k_stride, const void* v_new, int64_t v_stride, const int32_t* writes,
+                      const int32_t* counts, int32_t max_writes, void* k_pool, void* v_pool, float* scales, void* stream);
+
+/* chess_summarize (recent_pages = 0; from_page as there, or NULL) or chess_summarize_recent (recent_pages >= 1, from_page NULL; 1 is the refresh of
+ * a decode step) on the values that 8-bit pages stand for; the summaries are what chess_select and chess_select_shared read. */
+int chess_quant_summarize(chess_ctx* ctx, const void* k_pool, const float* scales, const int32_t* block_table, const int32_t* seq_lens,
+                          int32_t batch, const int32_t* from_page, int32_t recent_pages, void* summaries, void* stream);
+
+/* chess_sparse_decode and chess_dense_decode on the values that 8-bit pages stand for: bf16 queries, fp32 accumulation, fp32 out; no other
+ * rounding to fewer bits.  Arguments otherwise as for those. */
+int chess_quant_sparse_decode(chess_ctx* ctx, const void* q, const void* k_pool, const void* v_pool, const float* scales,
+                              const int32_t* block_table, const int32_t* seq_lens, const int32_t* page_ids, const int32_t* n_selected,
+                              int32_t batch, float* out, void* workspace, void* stream);
+int chess_quant_dense_decode(chess_ctx* ctx, const void* q, const void* k_pool, const void* v_pool, const float* scales,
+                             const int32_t* block_table, const int32_t* seq_lens, int32_t batch, float* out, void* workspace, void* stream);
 
 const char* chess_strerror(int code);
 int chess_version(void);

@@ -22,6 +22,8 @@ _lib = None
 
 EXPORTS = ["chess_create", "chess_destroy", "chess_summary_bytes", "chess_summary_layout", "chess_workspace_bytes", "chess_workspace_init",
            "chess_summarize", "chess_summarize_tail", "chess_summarize_recent", "chess_append_kv", "chess_select", "chess_anchor", "chess_select_shared", "chess_entropy", "chess_trigger_update", "chess_monitor_step", "chess_extend_window", "chess_reuse_step", "chess_sparse_decode", "chess_sparse_decode_static", "chess_dense_decode", "chess_decode_step",
+           "chess_write_rows", "chess_release_pages", "chess_map_tokens", "chess_quant_store", "chess_quant_summarize",
+           "chess_quant_sparse_decode", "chess_quant_dense_decode",
            "chess_debug_force_splits", "chess_debug_force_cluster", "chess_debug_force_schedule", "chess_debug_force_general_cut", "chess_debug_set_poll_limit", "chess_workspace_error", "chess_strerror", "chess_version"]
 
 
@@ -119,6 +121,13 @@ def load_library() -> ctypes.CDLL:
         lib.chess_sparse_decode_static.argtypes = [vp, vp, vp, vp, i32p, i32p, i32p, i32p, ctypes.c_int32, vp, vp]
         lib.chess_dense_decode.argtypes = [vp, vp, vp, vp, i32p, i32p, ctypes.c_int32, vp, vp, vp]
         lib.chess_decode_step.argtypes = [vp, vp, vp, vp, i32p, i32p, vp, ctypes.c_int32, ctypes.c_int32, vp, i32p, i32p, vp, vp, vp]
+        lib.chess_write_rows.argtypes = [vp, ctypes.c_int32, ctypes.c_int32, ctypes.POINTER(ctypes.c_size_t)]
+        lib.chess_release_pages.argtypes = [vp, i32p, i32p, ctypes.c_int32, i32p, i32p, ctypes.c_int32, i32p, i32p, i32p, vp, vp]
+        lib.chess_map_tokens.argtypes = [vp, i32p, i32p, ctypes.c_int32, ctypes.c_int32] + [vp] * 11
+        lib.chess_quant_store.argtypes = [vp, vp, ctypes.c_int64, vp, ctypes.c_int64, i32p, i32p, ctypes.c_int32, vp, vp, vp, vp]
+        lib.chess_quant_summarize.argtypes = [vp, vp, vp, i32p, i32p, ctypes.c_int32, i32p, ctypes.c_int32, vp, vp]
+        lib.chess_quant_sparse_decode.argtypes = [vp, vp, vp, vp, vp, i32p, i32p, i32p, i32p, ctypes.c_int32, vp, vp, vp]
+        lib.chess_quant_dense_decode.argtypes = [vp, vp, vp, vp, vp, i32p, i32p, ctypes.c_int32, vp, vp, vp]
         lib.chess_debug_force_splits.argtypes = [vp, ctypes.c_int32, ctypes.c_int32]
         lib.chess_debug_force_cluster.argtypes = [vp, ctypes.c_int32]
         lib.chess_debug_force_general_cut.argtypes = [vp, ctypes.c_int32]
@@ -141,6 +150,18 @@ def _ptr(t):
 
 def _stream():
     return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+
+
+_BYTES = (torch.uint8, torch.float8_e4m3fn)
+_INT, _LONG, _FLOAT, _BF16 = (torch.int32,), (torch.int64,), (torch.float32,), (torch.bfloat16,)
+
+
+def _need(t, name, dtypes, numel):
+    """A contiguous tensor on the current device, of one of the types, with that many elements at least.  (The library sees a pointer only;
+    about 0.3 us a tensor.)"""
+    if t.dtype not in dtypes or t.numel() < numel or not t.is_contiguous() or t.get_device() != torch.cuda.current_device():
+        raise ChessError(f"{name}: a contiguous {' or '.join(str(d) for d in dtypes)} tensor of at least {numel} elements on the current device is wanted, "
+                         f"got {t.dtype} {tuple(t.shape)} on {t.device}")
 
 
 class Chess:
@@ -290,6 +311,103 @@ class Chess:
                                                _ptr(seq_lens), _ptr(summaries), int(bool(refresh_tail)),
                                                seq_lens.shape[0], ctypes.byref(p),
                                                _ptr(page_ids), _ptr(n_selected), _ptr(out), _ptr(workspace), _stream()))
+
+    # ---- pages handed out on the device
+    def write_rows(self, max_tokens: int, batch: int) -> int:
+        """Entries `writes` must have room for."""
+        n = ctypes.c_size_t()
+        self._check(self.lib.chess_write_rows(self._h, max_tokens, batch, ctypes.byref(n)))
+        return n.value
+
+    def release_pages(self, seq_lens, done, block_table, free_pages, n_free, lens_after, n_left, workspace):
+        batch = seq_lens.shape[0]
+        for t, name, numel in ((seq_lens, "seq_lens", batch), (done, "done", batch), (block_table, "block_table", batch * self.cfg.max_pages_per_seq),
+                               (free_pages, "free_pages", 1), (n_free, "n_free", 1), (lens_after, "lens_after", batch), (n_left, "n_left", 1)):
+            _need(t, name, _INT, numel)
+        self._check(self.lib.chess_release_pages(self._h, _ptr(seq_lens), _ptr(done), batch, _ptr(block_table), _ptr(free_pages),
+                                                 free_pages.shape[0], _ptr(n_free), _ptr(lens_after), _ptr(n_left), _ptr(workspace), _stream()))
+
+    def map_tokens(self, seq_lens, new_lens, block_table, free_pages, n_free, lens_after, n_left, token_start, slots, writes, counts, workspace,
+                   max_tokens=None):
+        """max_tokens: by default what `slots` has room for; slots may be None if it is given."""
+        batch = seq_lens.shape[0]
+        if max_tokens is None:
+            if slots is None:
+                raise ChessError("map_tokens: slots or max_tokens is wanted")
+            max_tokens = slots.shape[0]
+        for t, name, numel in ((seq_lens, "seq_lens", batch), (new_lens, "new_lens", batch),
+                               (block_table, "block_table", batch * self.cfg.max_pages_per_seq), (free_pages, "free_pages", 1), (n_free, "n_free", 1),
+                               (lens_after, "lens_after", batch), (n_left, "n_left", 1), (token_start, "token_start", batch + 1),
+                               (writes, "writes", 4 * min(max_tokens, max_tokens // self.cfg.page_size + 2 * batch)), (counts, "counts", 4)):
+            _need(t, name, _INT, numel)
+        if slots is not None:
+            _need(slots, "slots", _LONG, max_tokens)
+        self._check(self.lib.chess_map_tokens(self._h, _ptr(seq_lens), _ptr(new_lens), batch, max_tokens, _ptr(block_table), _ptr(free_pages),
+                                              _ptr(n_free), _ptr(lens_after), _ptr(n_left), _ptr(token_start), _ptr(slots), _ptr(writes),
+                                              _ptr(counts), _ptr(workspace), _stream()))
+
+    # ---- the cache in 8 bits: pools uint8 or float8_e4m3fn, scales fp32 [physical page, H_kv, 2]
+    def _need_pool(self, pool, scales, name):
+        block = self.cfg.page_size * self.cfg.head_dim
+        _need(pool, name, _BYTES, block)
+        if pool.numel() * 2 != scales.numel() * block:
+            raise ChessError(f"{name}: {pool.numel()} bytes and {scales.numel()} scales are not of the same pages")
+
+    def quant_store(self, k_new, v_new, writes, counts, k_pool, v_pool, scales):
+        """k_new / v_new: bf16 [tokens, H_kv, 128], the rows of a token contiguous (slices of a wider projection will do); no tokens, nothing
+        stored."""
+        H, d = self.cfg.n_kv_heads, self.cfg.head_dim
+        for t, name in ((k_new, "k_new"), (v_new, "v_new")):
+            if t.dtype != torch.bfloat16 or tuple(t.shape[1:]) != (H, d) or t.stride(2) != 1 or (t.stride(1) != d and H > 1) or t.get_device() != torch.cuda.current_device():
+                raise ChessError(f"{name}: a bf16 tensor [tokens, {H}, {d}] on the current device with contiguous token rows is wanted, "
+                                 f"got {t.dtype} {tuple(t.shape)} of strides {t.stride()} on {t.device}")
+        _need(writes, "writes", _INT, 4)
+        _need(counts, "counts", _INT, 4)
+        _need(scales, "scales", _FLOAT, 2 * H)
+        self._need_pool(k_pool, scales, "k_pool")
+        self._need_pool(v_pool, scales, "v_pool")
+        if k_new.shape[0] != v_new.shape[0]:
+            raise ChessError(f"k_new and v_new have {k_new.shape[0]} and {v_new.shape[0]} tokens")
+        if k_new.shape[0] == 0:
+            return
+        self._check(self.lib.chess_quant_store(self._h, _ptr(k_new), k_new.stride(0), _ptr(v_new), v_new.stride(0), _ptr(writes), _ptr(counts),
+                                               writes.numel() // 4, _ptr(k_pool), _ptr(v_pool), _ptr(scales), _stream()))
+
+    def quant_summarize(self, k_pool, scales, block_table, seq_lens, summaries, from_page=None, recent_pages: int = 0):
+        batch = seq_lens.shape[0]
+        _need(scales, "scales", _FLOAT, 2 * self.cfg.n_kv_heads)
+        self._need_pool(k_pool, scales, "k_pool")
+        _need(block_table, "block_table", _INT, batch * self.cfg.max_pages_per_seq)
+        _need(seq_lens, "seq_lens", _INT, batch)
+        if from_page is not None:
+            _need(from_page, "from_page", _INT, batch)
+        _need(summaries, "summaries", (torch.uint8,), self.summary_bytes)
+        self._check(self.lib.chess_quant_summarize(self._h, _ptr(k_pool), _ptr(scales), _ptr(block_table), _ptr(seq_lens), batch, _ptr(from_page),
+                                                   recent_pages, _ptr(summaries), _stream()))
+
+    def _need_attention(self, q, k_pool, v_pool, scales, block_table, seq_lens, out, batch):
+        c = self.cfg
+        _need(q, "q", _BF16, batch * c.n_q_heads * c.head_dim)
+        _need(scales, "scales", _FLOAT, 2 * c.n_kv_heads)
+        self._need_pool(k_pool, scales, "k_pool")
+        self._need_pool(v_pool, scales, "v_pool")
+        _need(block_table, "block_table", _INT, batch * c.max_pages_per_seq)
+        _need(seq_lens, "seq_lens", _INT, batch)
+        _need(out, "out", _FLOAT, batch * c.n_q_heads * c.head_dim)
+
+    def quant_sparse_decode(self, q, k_pool, v_pool, scales, block_table, seq_lens, page_ids, n_selected, out, workspace):
+        batch = seq_lens.shape[0]
+        self._need_attention(q, k_pool, v_pool, scales, block_table, seq_lens, out, batch)
+        _need(page_ids, "page_ids", _INT, batch * self.cfg.n_kv_heads * self.cfg.max_selected_pages)
+        _need(n_selected, "n_selected", _INT, batch * self.cfg.n_kv_heads)
+        self._check(self.lib.chess_quant_sparse_decode(self._h, _ptr(q), _ptr(k_pool), _ptr(v_pool), _ptr(scales), _ptr(block_table), _ptr(seq_lens),
+                                                       _ptr(page_ids), _ptr(n_selected), batch, _ptr(out), _ptr(workspace), _stream()))
+
+    def quant_dense_decode(self, q, k_pool, v_pool, scales, block_table, seq_lens, out, workspace):
+        batch = seq_lens.shape[0]
+        self._need_attention(q, k_pool, v_pool, scales, block_table, seq_lens, out, batch)
+        self._check(self.lib.chess_quant_dense_decode(self._h, _ptr(q), _ptr(k_pool), _ptr(v_pool), _ptr(scales), _ptr(block_table), _ptr(seq_lens),
+                                                      batch, _ptr(out), _ptr(workspace), _stream()))
 
     def workspace_error(self, workspace) -> int:
         flag = ctypes.c_int32()

@@ -118,6 +118,29 @@ SplitShape choose_splits(const chess_ctx* ctx, int batch, int64_t max_list_pages
     return chess::choose_splits(c, batch, max_list_pages, listed);
 }
 
+// The same for 8-bit pages, whose tiles hold twice the tokens.
+SplitShape choose_quant_splits(const chess_ctx* ctx, int batch, int64_t max_list_pages, bool listed)
+{
+    const chess::Geom& g = ctx->geom;
+    const chess::SplitLimits c{ctx->n_cu, ctx->quant_blocks * ctx->n_cu, ctx->max_splits, g.n_kv_heads, g.group,
+                               2 * chess::kTileTokens / g.page_size, ctx->force_splits, ctx->force_waves};
+    return chess::choose_splits(c, batch, max_list_pages, listed);
+}
+
+// Whether the context's device is the current one: a launch goes there.
+bool on_device(const chess_ctx* ctx)
+{
+    int dev = -1;
+    return hipGetDevice(&dev) == hipSuccess && dev == ctx->device;
+}
+
+bool misaligned(std::initializer_list<const void*> pointers, uintptr_t mask)
+{
+    uintptr_t all = 0;
+    for (const void* p : pointers) all |= reinterpret_cast<uintptr_t>(p);
+    return (all & mask) != 0;
+}
+
 int decode_common(chess_ctx* ctx, const void* q, const void* k_pool, const void* v_pool, const int32_t* block_table,
                   const int32_t* seq_lens, const int32_t* page_ids, const int32_t* n_selected, int32_t batch,
                   float* out, void* workspace, void* stream)
@@ -199,6 +222,8 @@ int chess_create(const chess_config* cfg, chess_ctx** out)
     c->workspace_bytes = align_up(c->ws_entcnt_off + (size_t)cfg->max_batch * chess::kArrivalStride * sizeof(int32_t), 256);
     c->dense_blocks = 2;
     if (chess::dense_occupancy(g.page_size, g.group, &v) == hipSuccess && v > 0) c->dense_blocks = v;
+    c->quant_blocks = 2;
+    if (chess::quant_occupancy(g.page_size, g.group, &v) == hipSuccess && v > 0) c->quant_blocks = v;
     c->force_cluster = 0;
     c->force_schedule = 0;
     c->force_general_cut = 0;
@@ -715,6 +740,98 @@ int chess_dense_decode(chess_ctx* ctx, const void* q, const void* k_pool, const 
                        void* workspace, void* stream)
 {
     return decode_common(ctx, q, k_pool, v_pool, block_table, seq_lens, nullptr, nullptr, batch, out, workspace, stream);
+}
+
+int chess_write_rows(const chess_ctx* ctx, int32_t max_tokens, int32_t batch, size_t* rows)
+{
+    if (!ctx || !rows || max_tokens < 1 || max_tokens > CHESS_MAX_TOKENS || batch < 1) return CHESS_EINVAL;
+    *rows = (size_t)chess::most_writes(max_tokens, batch, ctx->geom.page_size);
+    return CHESS_OK;
+}
+
+int chess_release_pages(chess_ctx* ctx, const int32_t* seq_lens, const int32_t* done, int32_t batch, const int32_t* block_table,
+                        int32_t* free_pages, int32_t capacity, const int32_t* n_free, int32_t* lens_after, int32_t* n_left, void* workspace,
+                        void* stream)
+{
+    if (!ctx || !seq_lens || !done || !block_table || !free_pages || !n_free || !lens_after || !n_left || !workspace) return CHESS_EINVAL;
+    if (batch < 1 || batch > ctx->cfg.max_batch || capacity < 1 || misaligned({workspace}, 15) || !on_device(ctx)) return CHESS_EINVAL;
+    if (batch > chess::kPageMost) return CHESS_ENOTSUP;
+    const chess::ReleaseArgs a{seq_lens, done, block_table, free_pages, n_free, lens_after, n_left,
+                               reinterpret_cast<int32_t*>(static_cast<char*>(workspace) + ctx->ws_cnt_off), batch, capacity, ctx->geom.max_pages};
+    return chess::launch_release(ctx, a, static_cast<hipStream_t>(stream)) == hipSuccess ? CHESS_OK : CHESS_EHIP;
+}
+
+int chess_map_tokens(chess_ctx* ctx, const int32_t* seq_lens, const int32_t* new_lens, int32_t batch, int32_t max_tokens, int32_t* block_table,
+                     const int32_t* free_pages, const int32_t* n_free, int32_t* lens_after, int32_t* n_left, int32_t* token_start, int64_t* slots,
+                     int32_t* writes, int32_t* counts, void* workspace, void* stream)
+{
+    if (!ctx || !seq_lens || !new_lens || !block_table || !free_pages || !n_free || !lens_after || !n_left || !token_start || !writes || !counts ||
+        !workspace)
+        return CHESS_EINVAL;
+    if (batch < 1 || batch > ctx->cfg.max_batch || max_tokens < 1 || max_tokens > CHESS_MAX_TOKENS) return CHESS_EINVAL;
+    if (misaligned({writes, workspace}, 15) || misaligned({slots}, 7) || !on_device(ctx)) return CHESS_EINVAL;
+    if (batch > chess::kPageMost) return CHESS_ENOTSUP;
+    const chess::MapArgs a{seq_lens, new_lens, block_table, free_pages, n_free, lens_after, n_left, token_start, slots,
+                           reinterpret_cast<int4*>(writes), counts,
+                           reinterpret_cast<int32_t*>(static_cast<char*>(workspace) + ctx->ws_cnt_off), batch, max_tokens, ctx->geom.max_pages};
+    return chess::launch_map(ctx, a, static_cast<hipStream_t>(stream)) == hipSuccess ? CHESS_OK : CHESS_EHIP;
+}
+
+int chess_quant_store(chess_ctx* ctx, const void* k_new, int64_t k_stride, const void* v_new, int64_t v_stride, const int32_t* writes,
+                      const int32_t* counts, int32_t max_writes, void* k_pool, void* v_pool, float* scales, void* stream)
+{
+    if (!ctx || !k_new || !v_new || !writes || !counts || !k_pool || !v_pool || !scales || max_writes < 1) return CHESS_EINVAL;
+    const int64_t row = (int64_t)ctx->geom.n_kv_heads * kHeadDim;
+    if (k_stride < row || v_stride < row || ((k_stride | v_stride) & 7)) return CHESS_EINVAL;
+    if (misaligned({k_new, v_new, writes, k_pool, v_pool}, 15) || misaligned({scales}, 7) || !on_device(ctx)) return CHESS_EINVAL;
+    if ((int64_t)max_writes * ctx->geom.n_kv_heads > (int64_t)1 << 29) return CHESS_ENOTSUP;      // waves, in 32 bits
+    const chess::StoreArgs a{static_cast<const uint16_t*>(k_new), static_cast<const uint16_t*>(v_new), k_stride, v_stride,
+                             reinterpret_cast<const int4*>(writes), counts, static_cast<uint8_t*>(k_pool), static_cast<uint8_t*>(v_pool), scales,
+                             ctx->geom.n_kv_heads, max_writes};
+    return chess::launch_quant_store(ctx, a, static_cast<hipStream_t>(stream)) == hipSuccess ? CHESS_OK : CHESS_EHIP;
+}
+
+int chess_quant_summarize(chess_ctx* ctx, const void* k_pool, const float* scales, const int32_t* block_table, const int32_t* seq_lens,
+                          int32_t batch, const int32_t* from_page, int32_t recent_pages, void* summaries, void* stream)
+{
+    if (!ctx || !k_pool || !scales || !block_table || !seq_lens || !summaries) return CHESS_EINVAL;
+    if (batch < 1 || batch > ctx->cfg.max_batch || recent_pages < 0 || (from_page && recent_pages > 0)) return CHESS_EINVAL;
+    if (misaligned({k_pool, summaries}, 15) || misaligned({scales}, 7) || !on_device(ctx)) return CHESS_EINVAL;
+    char* sb = static_cast<char*>(summaries);
+    const hipError_t e = chess::launch_quant_summarize(ctx, static_cast<const uint8_t*>(k_pool), scales, block_table, seq_lens, batch, from_page,
+                                                       recent_pages, sb + ctx->page_off, sb + ctx->chunk_off, sb + ctx->grid_off,
+                                                       static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? CHESS_OK : CHESS_EHIP;
+}
+
+static int quant_decode_common(chess_ctx* ctx, const void* q, const void* k_pool, const void* v_pool, const float* scales,
+                               const int32_t* block_table, const int32_t* seq_lens, const int32_t* page_ids, const int32_t* n_selected,
+                               int32_t batch, float* out, void* workspace, void* stream)
+{
+    if (!ctx || !q || !k_pool || !v_pool || !scales || !block_table || !seq_lens || !out || !workspace) return CHESS_EINVAL;
+    if (batch < 1 || batch > ctx->cfg.max_batch) return CHESS_EINVAL;
+    if (misaligned({q, k_pool, v_pool, out, workspace}, 15) || misaligned({scales}, 7) || !on_device(ctx)) return CHESS_EINVAL;
+    const SplitShape sh = choose_quant_splits(ctx, batch, page_ids ? ctx->geom.max_sel : ctx->geom.max_pages, page_ids != nullptr);
+    char* wb = static_cast<char*>(workspace);
+    const hipError_t e = chess::launch_quant_decode(
+        ctx, static_cast<const uint16_t*>(q), static_cast<const uint8_t*>(k_pool), static_cast<const uint8_t*>(v_pool), scales, block_table,
+        seq_lens, page_ids, n_selected, batch, sh.n_splits, sh.waves, sh.n_slots, out, reinterpret_cast<float*>(wb + ctx->ws_acc_off),
+        reinterpret_cast<float*>(wb + ctx->ws_ml_off), reinterpret_cast<int32_t*>(wb + ctx->ws_cnt_off), static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? CHESS_OK : CHESS_EHIP;
+}
+
+int chess_quant_sparse_decode(chess_ctx* ctx, const void* q, const void* k_pool, const void* v_pool, const float* scales,
+                              const int32_t* block_table, const int32_t* seq_lens, const int32_t* page_ids, const int32_t* n_selected,
+                              int32_t batch, float* out, void* workspace, void* stream)
+{
+    if (!page_ids || !n_selected) return CHESS_EINVAL;
+    return quant_decode_common(ctx, q, k_pool, v_pool, scales, block_table, seq_lens, page_ids, n_selected, batch, out, workspace, stream);
+}
+
+int chess_quant_dense_decode(chess_ctx* ctx, const void* q, const void* k_pool, const void* v_pool, const float* scales,
+                             const int32_t* block_table, const int32_t* seq_lens, int32_t batch, float* out, void* workspace, void* stream)
+{
+    return quant_decode_common(ctx, q, k_pool, v_pool, scales, block_table, seq_lens, nullptr, nullptr, batch, out, workspace, stream);
 }
 
 int chess_debug_force_splits(chess_ctx* ctx, int32_t n_splits, int32_t waves)

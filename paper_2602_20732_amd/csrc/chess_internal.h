@@ -162,6 +162,9 @@ __device__ __forceinline__ int load_by_lane(const int32_t* p)
     return p[zero];
 }
 
+// What stands before is requested before what stands behind (the compiler moves a load that only a branch uses into the branch).
+__device__ __forceinline__ void requested_by_here() { asm volatile("" : : : "memory"); }
+
 // Values that cross workgroups inside one launch travel as agent-scope atomics: on gfx950 these are loads and
 // stores with the sc1 bit, which do not live in the per-XCD L2s as cached copies (a store is written through to
 // the memory side that all eight XCDs share before it is acknowledged, a load is served from there), so they are
@@ -250,6 +253,7 @@ struct chess_ctx {
     int force_general_cut;                                 // 0 = automatic
     int poll_limit;                                        // 0 = the default
     int dense_blocks;                                      // workgroups of attention over every page per CU
+    int quant_blocks;                                      // ... of 8-bit pages
     int occ_lds, occ_blocks;                               // cached occupancy query of the select kernel
     int step_occ_lds, step_occ_blocks;                     // ... and of the fused step kernel
     int shared_occ_lds, shared_occ_blocks;                 // ... and of the model-wide select kernel
@@ -349,5 +353,64 @@ hipError_t launch_decode(chess_ctx* ctx, const uint16_t* q, const uint16_t* k_po
                          const int32_t* block_table, const int32_t* seq_lens, const int32_t* page_ids,
                          const int32_t* n_selected, int batch, int n_splits, int waves, int n_slots, float* out,
                          float* ws_acc, float* ws_ml, int32_t* arrivals, hipStream_t stream);
+
+// Pages handed out and taken back (pages.hip).  lens_after / n_left may be seq_lens / n_free.
+constexpr int kPageMost = 4096;      // most sequences: their three sums are in LDS
+struct MapArgs {
+    const int32_t* seq_lens;
+    const int32_t* new_lens;
+    int32_t* block_table;
+    const int32_t* free_pages;
+    const int32_t* n_free;
+    int32_t* lens_after;
+    int32_t* n_left;
+    int32_t* token_start;
+    int64_t* slots;          // or null
+    int4* writes;
+    int32_t* counts;
+    int32_t* arrivals;       // one counter, zero between launches
+    int batch, max_tokens, max_pages;
+};
+struct ReleaseArgs {
+    const int32_t* seq_lens;
+    const int32_t* done;
+    const int32_t* block_table;
+    int32_t* free_pages;
+    const int32_t* n_free;
+    int32_t* lens_after;
+    int32_t* n_left;
+    int32_t* arrivals;
+    int batch, capacity, max_pages;
+};
+// Pages that so many new tokens of `batch` sequences can lie in.
+inline int64_t most_writes(int64_t tokens, int64_t batch, int page_size)
+{
+    const int64_t n = tokens / page_size + 2 * batch;
+    return tokens < n ? tokens : n;
+}
+hipError_t launch_map(chess_ctx* ctx, const MapArgs& a, hipStream_t stream);
+hipError_t launch_release(chess_ctx* ctx, const ReleaseArgs& a, hipStream_t stream);
+
+// 8-bit pages (quant_store.hip, quant_summarize.hip, quant_decode.hip).  scales: fp32 [physical page][H_kv][2] (keys, values).
+struct StoreArgs {
+    const uint16_t* k_new;
+    const uint16_t* v_new;
+    int64_t k_stride, v_stride;      // elements from a token to the next
+    const int4* writes;
+    const int32_t* counts;
+    uint8_t* k_pool;
+    uint8_t* v_pool;
+    float* scales;
+    int heads, max_writes;
+};
+hipError_t launch_quant_store(chess_ctx* ctx, const StoreArgs& a, hipStream_t stream);
+hipError_t launch_quant_summarize(chess_ctx* ctx, const uint8_t* k_pool, const float* scales, const int32_t* block_table,
+                                  const int32_t* seq_lens, int batch, const int32_t* from_page, int recent, void* pages, void* chunks,
+                                  void* grids, hipStream_t stream);
+// As launch_decode.
+hipError_t launch_quant_decode(chess_ctx* ctx, const uint16_t* q, const uint8_t* k_pool, const uint8_t* v_pool, const float* scales,
+                               const int32_t* block_table, const int32_t* seq_lens, const int32_t* page_ids, const int32_t* n_selected, int batch,
+                               int n_splits, int waves, int n_slots, float* out, float* ws_acc, float* ws_ml, int32_t* arrivals, hipStream_t stream);
+hipError_t quant_occupancy(int page_size, int group, int* blocks_per_cu);
 
 }  // namespace chess

@@ -1,0 +1,316 @@
+// Paged decode attention over 8-bit pages, a list of them or every page: split-K with an online-softmax merge, as decode.hip does it for bf16.
+//
+// Work unit: one wave, one tile of 64 tokens (16 KB of keys and values, what 32 tokens are in bf16), all G <= 16 query heads of a KV head.
+// Both products run on 16 x 16 x 32 bf16 MFMA tiles with fp32 accumulation: e4m3 bytes times a power of two are bf16 values exactly, so
+// the queries stay bf16 and nothing is rounded that the cache has not rounded already.  A lane of group g = lane / 16:
+//   S^T[token][head] = K[token][d] . Q^T[d][head]   four products of 16 tokens; its two 16-byte loads of a key row are d = 16 g .. + 15 and
+//                                                   64 + 16 g .. + 15, and the contraction runs over d in that order for both operands
+//   O^T[d][head]    += V^T[d][token] . P[token][head]   a 16-byte load is tokens 16 g .. + 15 of one d: two contraction steps of 32 tokens
+// Row i of product c is token 16 (i / 4) + 4 c + i % 4, so the 16 weights a lane ends up with are those of its own 16 tokens, which lie in
+// one page: no weight moves between lanes, and the page's two scales are one number each a lane (the keys' times the softmax scale, the
+// values' inside the conversion).  The weights are split into three bf16 parts (24 bits; two parts were the largest error there was).
+// Bound: HBM.
+#include "deal.h"
+#include "quant_device.h"
+
+namespace chess {
+
+constexpr int kQuantTokens = 64;     // of a tile
+typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
+
+// Eight stored bytes, times a power of two, as a MFMA operand.
+__device__ __forceinline__ bf16x8 operand_of(uint32_t lo, uint32_t hi, float scale)
+{
+    const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, false), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, true);
+    const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, false), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, true);
+    return bf16x8{a.x, a.y, b.x, b.y, c.x, c.y, d.x, d.y};
+}
+
+// Where a lane finds its parts of a tile: the page its key rows lie in (tokens 16 (m16 / 4) ..), the page of its own 16 tokens (16 grp ..) and
+// how many of these exist.
+struct QuantRef {
+    int pk, pv, nt;
+};
+
+template <int B>
+struct QuantTile {
+    uint4 k[4][2];      // [product][half row]
+    uint4 v[8];         // [16-row block of d]
+    float2 scale;       // of the lane's own page: keys, values
+    int nt;
+};
+
+// Listed pages of tile t at the lane's two places, as stored in the list (an index beyond the list's last entry is that entry; before the list's
+// length is known, its row's last).
+template <int B, bool kList>
+__device__ __forceinline__ void quant_ids(int2& raw, int t, const int32_t* ids, int last, int m16, int grp)
+{
+    constexpr int PPT = kQuantTokens / B;
+    const int at_k = t * PPT + (m16 >> 2) * 16 / B, at_v = t * PPT + grp * 16 / B;
+    raw = kList ? make_int2(ids[min(at_k, last)], ids[min(at_v, last)]) : make_int2(at_k, at_v);
+}
+
+template <int B>
+__device__ __forceinline__ QuantRef quant_pages(int t, int n_pages, const int2& raw, const int32_t* bt_row, int L, int P, int m16, int grp)
+{
+    constexpr int PPT = kQuantTokens / B;
+    // (a page beyond the last, or a bad id, must not become a bad address)
+    const int lk = min(max(raw.x, 0), P - 1), lv = min(max(raw.y, 0), P - 1);
+    const int held = lv == P - 1 ? L - lv * B : B;
+    QuantRef r;
+    r.pk = bt_row[lk];
+    r.pv = bt_row[lv];
+    r.nt = t * PPT + grp * 16 / B < n_pages ? held - 16 * grp % B : 0;
+    return r;
+}
+
+template <int B>
+__device__ __forceinline__ void quant_rows(QuantTile<B>& tl, const QuantRef& r, const uint8_t* k_pool, const uint8_t* v_pool, const float* scales,
+                                           int H, int h, int m16, int grp)
+{
+    const int64_t at_k = ((int64_t)r.pk * H + h) * (B * kHeadDim), at_v = (int64_t)r.pv * H + h;
+    const uint8_t* k_row = k_pool + at_k + ((16 * (m16 >> 2)) % B + (m16 & 3)) * kHeadDim + 16 * grp;
+#pragma unroll
+    for (int c = 0; c < 4; ++c)
+#pragma unroll
+        for (int half = 0; half < 2; ++half) tl.k[c][half] = *reinterpret_cast<const uint4*>(k_row + 4 * c * kHeadDim + 64 * half);
+    tl.scale = *reinterpret_cast<const float2*>(scales + 2 * at_v);
+    const uint8_t* v_row = v_pool + at_v * (B * kHeadDim) + m16 * B + 16 * grp % B;
+#pragma unroll
+    for (int blk = 0; blk < 8; ++blk) tl.v[blk] = *reinterpret_cast<const uint4*>(v_row + blk * 16 * B);
+    tl.nt = r.nt;
+}
+
+// Online-softmax state of one wave: all G heads of one KV head.
+struct QuantAcc {
+    bf16x8 qop[4];      // head m16: d = 64 j + 16 grp + 8 i .. + 7 is step 2 j + i; heads >= G are zero columns
+    float m_run, l_run;
+    f32x4 o[8];
+
+    __device__ __forceinline__ void request(const uint16_t* __restrict__ q_rows, int G, int m16, int grp)
+    {
+        const uint4* src = reinterpret_cast<const uint4*>(q_rows + (size_t)(m16 < G ? m16 : 0) * kHeadDim) + 2 * grp;
+#pragma unroll
+        for (int st = 0; st < 4; ++st) qop[st] = as_bf16x8(src[8 * (st >> 1) + (st & 1)]);
+    }
+    __device__ __forceinline__ void start(int G, int m16)
+    {
+        const uint32_t keep = m16 < G ? 0xffffffffu : 0u;
+#pragma unroll
+        for (int st = 0; st < 4; ++st) {
+            uint4 v = __builtin_bit_cast(uint4, qop[st]);
+            v.x &= keep; v.y &= keep; v.z &= keep; v.w &= keep;
+            qop[st] = as_bf16x8(v);
+        }
+        m_run = kNegBig;
+        l_run = 0.f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+
+    template <int B>
+    __device__ __forceinline__ void process(QuantTile<B>& tl, float scale_log2)
+    {
+        f32x4 s[4];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            s[c] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                const uint4 w = tl.k[c][half];
+                s[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(operand_of(w.x, w.y, 1.f), qop[2 * half], s[c], 0, 0, 0);
+                s[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(operand_of(w.z, w.w, 1.f), qop[2 * half + 1], s[c], 0, 0, 0);
+            }
+        }
+        const float by = tl.scale.x * scale_log2;
+        float x[16];
+#pragma unroll
+        for (int e = 0; e < 16; ++e) x[e] = e < tl.nt ? s[e >> 2][e & 3] * by : -INFINITY;
+        float tmax = x[0];
+#pragma unroll
+        for (int e = 1; e < 16; ++e) tmax = fmaxf(tmax, x[e]);
+        tmax = fmaxf(tmax, __shfl_xor(tmax, 16));
+        tmax = fmaxf(tmax, __shfl_xor(tmax, 32));
+        const float m_new = fmaxf(m_run, tmax);
+        const float alpha = __builtin_amdgcn_exp2f(m_run - m_new);
+        m_run = m_new;
+        float psum = 0.f;
+        bf16x8 p[2][3];
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            const float w = __builtin_amdgcn_exp2f(x[e] - m_new);
+            psum += w;
+            const __bf16 hi = (__bf16)w;
+            const float rest = w - (float)hi;
+            const __bf16 mid = (__bf16)rest;
+            p[e >> 3][0][e & 7] = hi;
+            p[e >> 3][1][e & 7] = mid;
+            p[e >> 3][2][e & 7] = (__bf16)(rest - (float)mid);
+        }
+        l_run = l_run * alpha + psum;
+        if (tl.nt < 16) {                             // bytes behind the last token may be anything (NaN among them)
+            uint32_t keep[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int n = tl.nt - 4 * i;
+                keep[i] = n >= 4 ? 0xffffffffu : n <= 0 ? 0u : (1u << (8 * n)) - 1u;
+            }
+#pragma unroll
+            for (int blk = 0; blk < 8; ++blk) {
+                tl.v[blk].x &= keep[0]; tl.v[blk].y &= keep[1]; tl.v[blk].z &= keep[2]; tl.v[blk].w &= keep[3];
+            }
+        }
+#pragma unroll
+        for (int blk = 0; blk < 8; ++blk) {
+            f32x4 acc = o[blk] * alpha;
+            const uint4 w = tl.v[blk];
+            const bf16x8 v0 = operand_of(w.x, w.y, tl.scale.y), v1 = operand_of(w.z, w.w, tl.scale.y);
+#pragma unroll
+            for (int part = 0; part < 3; ++part) {
+                acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v0, p[0][part], acc, 0, 0, 0);
+                acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v1, p[1][part], acc, 0, 0, 0);
+            }
+            o[blk] = acc;
+        }
+    }
+};
+
+struct QuantArgs {
+    const uint8_t* k_pool;
+    const uint8_t* v_pool;
+    const float* scales;
+    float* out;
+    float* ws_acc;
+    float* ws_ml;
+    int32_t* arrivals;
+    float scale_log2;
+    int batch;
+};
+using QuantKernel = void (*)(uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, int, int, int, int, QuantArgs);
+using QuantLines = ArgLinesOf<QuantKernel, QuantArgs>;
+
+// grid: (n_splits, H_kv, batch), or dealt by length (H_kv, n_slots).  heads: KV heads << 8 | group.
+template <int B, int NW, bool kList, bool kDealt = false>
+__global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2))) void quant_decode_kernel(
+    uint64_t seq_lens_at, uint64_t block_table_at, uint64_t q_at, uint64_t page_ids_at, uint64_t n_selected_at, int heads, int max_sel, int max_pages,
+    int n_splits, QuantArgs a)
+{
+    constexpr int PPT = kQuantTokens / B;
+    extern __shared__ float lds_f[];                  // DecodeLds<NW>::floats(G)
+    __shared__ int lds_last;
+    const int G = heads & 255, H = heads >> 8, h = kDealt ? blockIdx.x : blockIdx.y;
+    QuantLines lines;
+    lines.ask();
+    DecodeLds<NW> lds(lds_f, G);
+    const int32_t* seq_lens = device_pointer<const int32_t>(seq_lens_at);
+
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int m16 = lane & 15, grp = lane >> 4;
+    int split = blockIdx.x, b = blockIdx.z, ns = n_splits, L_raw;
+    size_t part0 = ((size_t)b * H + h) * n_splits;
+    if constexpr (kDealt) {
+        __shared__ DealLds<NW> deal_lds;
+        const SlotShare sh = share_slots<B, NW, kQuantTokens>(blockIdx.y, gridDim.y, a.batch, n_splits, G, seq_lens, max_pages, lane, wave, deal_lds);
+        if (sh.b < 0) return;                         // (uniform: nobody waits for a slot without work)
+        split = sh.split;
+        b = sh.b;
+        ns = sh.n_splits;
+        L_raw = sh.len;
+        part0 = (size_t)h * gridDim.y + sh.first;
+    }
+    const size_t row = (size_t)b * H + h;
+    const int32_t* ids = kList ? device_pointer<const int32_t>(page_ids_at) + row * max_sel : nullptr;
+    const int32_t* bt_row = device_pointer<const int32_t>(block_table_at) + (size_t)b * max_pages;
+    // tiles are dealt round-robin over splits and waves: the first of a wave is known before the list's length is
+    const int stride = ns * NW;
+    int t = split + ns * wave;
+    int2 raw_cur, raw_nxt, raw_nn;
+    if constexpr (!kDealt) L_raw = load_by_lane(seq_lens + b);
+    int n_raw = kList ? load_by_lane(device_pointer<const int32_t>(n_selected_at) + row) : 0;
+    quant_ids<B, kList>(raw_cur, t, ids, max_sel - 1, m16, grp);
+    quant_ids<B, kList>(raw_nxt, t + stride, ids, max_sel - 1, m16, grp);
+    QuantAcc acc;
+    acc.request(device_pointer<const uint16_t>(q_at) + ((size_t)b * H * G + (size_t)h * G) * kHeadDim, G, m16, grp);
+    requested_by_here();
+    if constexpr (!kDealt) L_raw = __builtin_amdgcn_readfirstlane(L_raw);
+    if (kList) n_raw = __builtin_amdgcn_readfirstlane(n_raw);
+    const int L = min(max(L_raw, 0), max_pages * B);
+    const int P = (L + B - 1) / B;
+    const int n_pages = P == 0 ? 0 : (kList ? min(max(n_raw, 0), max_sel) : P);
+    const int n_tiles = (n_pages + PPT - 1) / PPT;
+
+    lines.hold();
+    acc.start(G, m16);
+    if (t < n_tiles) {
+        // block-table entries run one tile ahead of the rows, page numbers one tile ahead of those
+        const int last = kList ? max_sel - 1 : 0;
+        QuantRef rc = quant_pages<B>(t, n_pages, raw_cur, bt_row, L, P, m16, grp);
+        QuantRef rn = quant_pages<B>(t + stride, n_pages, raw_nxt, bt_row, L, P, m16, grp);
+        quant_ids<B, kList>(raw_nn, t + 2 * stride, ids, last, m16, grp);
+        QuantTile<B> tl;
+        for (; t < n_tiles; t += stride) {
+            quant_rows<B>(tl, rc, a.k_pool, a.v_pool, a.scales, H, h, m16, grp);
+            const QuantRef rnn = quant_pages<B>(t + 2 * stride, n_pages, raw_nn, bt_row, L, P, m16, grp);
+            quant_ids<B, kList>(raw_nn, t + 3 * stride, ids, last, m16, grp);
+            acc.process(tl, a.scale_log2);
+            rc = rn;
+            rn = rnn;
+        }
+    }
+    acc.l_run += __shfl_xor(acc.l_run, 16);
+    acc.l_run += __shfl_xor(acc.l_run, 32);
+
+    float* out_rows = a.out + ((size_t)b * H * G + (size_t)h * G) * kHeadDim;
+    if (!combine_waves<NW>(acc.o, acc.m_run, acc.l_run, lds, G, ns, split, part0, out_rows, a.ws_acc, a.ws_ml)) return;
+    if (!arrive_last(a.arrivals + row * kArrivalStride, ns, &lds_last)) return;
+    if constexpr (kDealt) {                           // (the same in every lane, which the compiler cannot tell)
+        ns = own_reg(__builtin_amdgcn_readfirstlane(ns));
+        part0 = own_reg((unsigned)__builtin_amdgcn_readfirstlane((int)part0));
+    }
+    merge_splits<NW, kDealt ? kMergeDealt : kMergePlain>(G, ns, part0, out_rows, a.ws_acc, a.ws_ml);
+}
+
+static size_t quant_lds_bytes(int waves, int group) { return (size_t)(waves * group * kHeadDim + 2 * waves * group) * sizeof(float); }
+
+hipError_t launch_quant_decode(chess_ctx* ctx, const uint16_t* q, const uint8_t* k_pool, const uint8_t* v_pool, const float* scales,
+                               const int32_t* block_table, const int32_t* seq_lens, const int32_t* page_ids, const int32_t* n_selected, int batch,
+                               int n_splits, int waves, int n_slots, float* out, float* ws_acc, float* ws_ml, int32_t* arrivals, hipStream_t stream)
+{
+    const Geom& g = ctx->geom;
+    const bool dealt = n_slots > 0;                   // (every page, four waves: see choose_splits)
+    const dim3 grid = dealt ? dim3(g.n_kv_heads, n_slots) : dim3(n_splits, g.n_kv_heads, batch), block(64 * waves);
+    const size_t lds = quant_lds_bytes(waves, g.group);
+    // [page size 16 / 32][waves 4 / 1][list / every page], eight waves for a list, every page dealt by length
+    static const QuantKernel table[2][2][2] = {
+        {{quant_decode_kernel<16, 4, true>, quant_decode_kernel<16, 4, false>}, {quant_decode_kernel<16, 1, true>, quant_decode_kernel<16, 1, false>}},
+        {{quant_decode_kernel<32, 4, true>, quant_decode_kernel<32, 4, false>}, {quant_decode_kernel<32, 1, true>, quant_decode_kernel<32, 1, false>}}};
+    static const QuantKernel wide[2] = {quant_decode_kernel<16, 8, true>, quant_decode_kernel<32, 8, true>};
+    static const QuantKernel by_length[2] = {quant_decode_kernel<16, 4, false, true>, quant_decode_kernel<32, 4, false, true>};
+    const int by_page = g.page_size == 16 ? 0 : 1;
+    const QuantKernel kern = dealt ? by_length[by_page] : waves == 8 ? wide[by_page] : table[by_page][waves == 4 ? 0 : 1][page_ids ? 0 : 1];
+    if (lds > 64 * 1024) {
+        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+        if (e != hipSuccess) return e;
+    }
+    return launch(kern, grid, block, lds, stream, (uint64_t)seq_lens, (uint64_t)block_table, (uint64_t)q, (uint64_t)page_ids, (uint64_t)n_selected,
+                  g.n_kv_heads << 8 | g.group, g.max_sel, g.max_pages, n_splits,
+                  QuantArgs{k_pool, v_pool, scales, out, ws_acc, ws_ml, arrivals, ctx->sm_scale * 1.4426950408889634f, batch});
+}
+
+// Four-wave workgroups of attention over every page that fit on a compute unit, dealt or not, whichever are fewer.
+hipError_t quant_occupancy(int page_size, int group, int* blocks_per_cu)
+{
+    const size_t lds = quant_lds_bytes(4, group);
+    const QuantKernel fixed = page_size == 16 ? quant_decode_kernel<16, 4, false> : quant_decode_kernel<32, 4, false>;
+    const QuantKernel dealt = page_size == 16 ? quant_decode_kernel<16, 4, false, true> : quant_decode_kernel<32, 4, false, true>;
+    int n = 0;
+    *blocks_per_cu = 1 << 30;
+    for (const QuantKernel kern : {fixed, dealt}) {
+        const hipError_t e = hipOccupancyMaxActiveBlocksPerMultiprocessor(&n, kern, 256, lds);
+        if (e != hipSuccess) return e;
+        *blocks_per_cu = n < *blocks_per_cu ? n : *blocks_per_cu;
+    }
+    return hipSuccess;
+}
+
+}  // namespace chess

@@ -1,0 +1,185 @@
+"""Summaries of 8-bit pages bit for bit against fp64 means rounded once, and the calls of the 8-bit cache together as a server makes them: pages dealt,
+tokens stored, summaries refreshed, pages selected, attention over the lists."""
+from __future__ import annotations
+
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import helpers
+import oracle
+import paper_2602_20732_amd as pk
+import quant_reference as ref
+from gpu_common import host_views
+
+pytestmark = pytest.mark.gpu
+D = 128
+
+
+def ints(v):
+    return torch.tensor(np.asarray(v), dtype=torch.int32, device="cuda")
+
+
+def stored(mean):
+    """A mean as the summaries store it (the fp64 mean rounded once to fp32, that once more to bf16), as fp32."""
+    m = torch.from_numpy(np.asarray(mean).astype(np.float32))
+    return (m.to(torch.bfloat16).float() if helpers.SUMMARY_DTYPE else m).numpy()
+
+
+def means(children, fan):
+    return stored(np.stack([children[i:i + fan].astype(np.float64).mean(0) for i in range(0, len(children), fan)]))
+
+
+def units_of(rows, B, n_c, n_g):
+    """(page, chunk, grid vectors) of a sequence's fp64 rows [n, d]."""
+    page = stored(np.stack([rows[i:i + B].sum(0) / len(rows[i:i + B]) for i in range(0, len(rows), B)]))
+    chunk = means(page, n_c)
+    return page, chunk, means(chunk, n_g)
+
+
+def cache_of(rng, lens, pages, H, B):
+    held = [-(-n // B) for n in lens]
+    order, table, at = rng.permutation(sum(held) + 1), np.full((len(lens), pages), -1, np.int32), 0
+    for b, n in enumerate(held):
+        table[b, :n] = order[at:at + n]
+        at += n
+    k = rng.integers(0, 256, (sum(held) + 1, H, B, D), dtype=np.uint8)           # (NaN behind the last token)
+    for b, n in enumerate(lens):
+        for p in range(held[b]):
+            page = k[table[b, p]][:, : n - p * B]
+            page[page & 127 == 127] = 0x35
+    scales = 2.0 ** rng.integers(-12, 4, (sum(held) + 1, H, 2)).astype(np.float64)
+    return table, k, scales
+
+
+@pytest.mark.parametrize("B", [16, 32])
+@pytest.mark.parametrize("n_c,n_g", [(8, 8), (4, 4), (3, 5), (1, 1), (16, 16), (64, 4)])
+def test_summaries_of_whole_sequences_and_of_the_last_pages(B, n_c, n_g):
+    rng = np.random.default_rng(B + n_c)
+    H, lens = 2, [0, 1, B - 1, B, B + 1, 5 * B + 3, 40 * B, 70 * B - 1, 71 * B + 9]
+    pages = 75
+    table, k, scales = cache_of(rng, lens, pages, H, B)
+    lib = pk.Chess(pk.Config(4, H, B, len(lens), pages, pages, n_c, n_g, summary_dtype=helpers.SUMMARY_DTYPE))
+    kd, sd, bt, sl = torch.from_numpy(k).cuda(), torch.from_numpy(scales.astype(np.float32)).cuda(), torch.from_numpy(table).cuda(), ints(lens)
+    want = {(b, h): units_of(ref.rows_of(k, scales, 0, table[b], h, n), B, n_c, n_g) for b, n in enumerate(lens) for h in range(H) if n}
+
+    def check(summ, from_of):
+        """Units from the given pages on are new, those below are as they were (7)."""
+        got = host_views(lib, summ)
+        for (b, h), units in want.items():
+            start = from_of(b)
+            for level, (g, u) in enumerate(zip(got, units)):
+                start = start if level == 0 else start // (n_c if level == 1 else n_g)
+                assert np.array_equal(g[b, h, start:len(u)], u[start:]), (b, h, level)
+                assert (g[b, h, len(u):] == 7).all(), (b, h, level)
+        assert all((g[0] == 7).all() for g in got)                               # the empty sequence
+
+    def fresh(below=None):
+        summ = lib.new_summaries()
+        for g in lib.summary_views(summ):
+            g.fill_(7)
+        if below is not None:                                                    # valid below, as an earlier call left them
+            for level, g in enumerate(lib.summary_views(summ)):
+                for (b, h), units in want.items():
+                    n = below(b) if level == 0 else below(b) // n_c if level == 1 else below(b) // n_c // n_g
+                    g[b, h, :n] = torch.from_numpy(units[level][:n]).cuda().to(g.dtype)
+        return summ
+
+    summ = fresh()
+    lib.quant_summarize(kd, sd, bt, sl, summ)
+    torch.cuda.synchronize()
+    check(summ, lambda b: 0)
+    P = [-(-n // B) for n in lens]
+    for recent in (1, 2, 10, 16, 17, 40, 1000):
+        summ = fresh(lambda b: max(0, P[b] - recent))
+        lib.quant_summarize(kd, sd, bt, sl, summ, recent_pages=recent)
+        torch.cuda.synchronize()
+        check(summ, lambda b: 0)
+    start = [int(rng.integers(0, p + 1)) for p in P]
+    summ = fresh(lambda b: start[b])
+    lib.quant_summarize(kd, sd, bt, sl, summ, from_page=ints(start))
+    torch.cuda.synchronize()
+    check(summ, lambda b: 0)
+
+
+@pytest.mark.parametrize("B", [16, 32])
+def test_a_full_page_of_the_largest_and_smallest_values(B):
+    """The sum of a page is exact in fp32 at either end of what a scale can be."""
+    k = np.empty((2, 1, B, D), np.uint8)
+    k[:, :, ::2], k[:, :, 1::2] = 0x7e, 0x01                                     # 448 and 2^-9
+    for scale in (2.0 ** 119, 2.0 ** -64):
+        lib = pk.Chess(pk.Config(1, 1, B, 1, 2, 2, summary_dtype=helpers.SUMMARY_DTYPE))
+        summ = lib.new_summaries()
+        scales = np.full((2, 1, 2), scale)
+        lib.quant_summarize(torch.from_numpy(k).cuda(), torch.from_numpy(scales.astype(np.float32)).cuda(), ints([[1, 0]]), ints([2 * B - 1]), summ)
+        torch.cuda.synchronize()
+        page, chunk, grid = units_of(ref.rows_of(k, scales, 0, [1, 0], 0, 2 * B - 1), B, 8, 8)
+        for got, want in zip(host_views(lib, summ), (page, chunk, grid)):
+            assert np.array_equal(got[0, 0, : len(want)], want)
+
+
+@pytest.mark.parametrize("B", [16, 32])
+def test_a_server_over_an_8_bit_cache(B):
+    """Prompts arrive, tokens follow one by one, requests end and their rows take others; every few steps the whole chain is compared with the
+    definitions: pools, summaries, lists (the oracle's selection on those summaries) and attention."""
+    rng = np.random.default_rng(B)
+    H, Hq, batch, pages, n_phys, room = 2, 8, 4, 24, 80, 12
+    lib = pk.Chess(pk.Config(Hq, H, B, batch, pages, room, 4, 4, summary_dtype=helpers.SUMMARY_DTYPE))
+    geom = oracle.Geometry(Hq, H, D, B, 4, 4, pages, helpers.SUMMARY_DTYPE)
+    plan, oplan = pk.SelectPlan(budget_pages=4, window_pages=2), oracle.Plan(sink_pages=1, window_pages=2, budget_pages=4)
+    most = 9 * B
+    ws, summ = lib.new_workspace(), lib.new_summaries()
+    k = torch.randint(0, 256, (n_phys, H, B, D), dtype=torch.uint8, device="cuda")
+    v = torch.randint(0, 256, (n_phys, H, D, B), dtype=torch.uint8, device="cuda")
+    scales = torch.full((n_phys, H, 2), 2.0 ** 40, device="cuda")
+    hk, hv, hs = k.cpu().numpy(), v.cpu().numpy(), scales.cpu().double().numpy()
+    table = torch.full((batch, pages), -1, dtype=torch.int32, device="cuda")
+    free, n_free = ints(rng.permutation(n_phys)), ints([n_phys])
+    lens, done = ints([0] * batch), ints([0] * batch)
+    starts, counts, slots = ints([0] * (batch + 1)), ints([0] * 4), torch.zeros(most, dtype=torch.int64, device="cuda")
+    writes = torch.zeros((lib.write_rows(most, batch), 4), dtype=torch.int32, device="cuda")
+    ids, nsel = ints(np.zeros((batch, H, room))), ints(np.zeros((batch, H)))
+    out = torch.empty((batch, Hq, D), device="cuda")
+    h_lens, h_table, h_free, h_n = [0] * batch, table.cpu().numpy(), free.cpu().numpy(), n_phys
+    for step in range(26):
+        ended = [int(n > 6 * B and rng.random() < 0.2) for n in h_lens]
+        new = [int(rng.integers(B, 5 * B)) if e or n == 0 else 1 for e, n in zip(ended, h_lens)]
+        done.copy_(ints(ended))
+        lib.release_pages(lens, done, table, free, n_free, lens, n_free, ws)
+        lib.map_tokens(lens, ints(new), table, free, n_free, lens, n_free, starts, slots, writes, counts, ws)
+        x = torch.from_numpy(rng.normal(0, 1, (2, most, H, D)).astype(np.float32) * 2.0 ** rng.integers(-3, 3)).to(torch.bfloat16)
+        lib.quant_store(x[0].cuda(), x[1].cuda(), writes, counts, k, v, scales)
+        lib.quant_summarize(k, scales, table, lens, summ, recent_pages=max(-(-n // B) + 1 for n in new))
+        q = torch.from_numpy(rng.normal(0, 0.5, (batch, Hq, D)).astype(np.float32)).to(torch.bfloat16)
+        lib.select(q.cuda(), summ, lens, plan, ids, nsel, ws)
+        lib.quant_sparse_decode(q.cuda(), k, v, scales, table, lens, ids, nsel, out, ws)
+        # the same from the definitions
+        h_lens, h_free, h_n = ref.release(h_lens, ended, h_table, h_free, h_n, n_phys, B)
+        want = ref.map_tokens(h_lens, new, h_table, h_free, h_n, most, pages, B)
+        h_lens, h_table, h_n = want["lens_after"], np.array(want["table"], np.int32), want["n_left"]
+        ref.store(hk, hv, hs, x[0].double().numpy(), x[1].double().numpy(), want["writes"])
+        if step % 5 != 4:
+            continue
+        torch.cuda.synchronize()
+        assert counts.tolist() == want["counts"] and lens.tolist() == h_lens and np.array_equal(table.cpu().numpy(), h_table)
+        assert ref.same_bytes(k.cpu().numpy(), hk) and ref.same_bytes(v.cpu().numpy(), hv) and np.array_equal(scales.cpu().double().numpy(), hs)
+        arrays = [np.zeros((batch, H, n, D), np.float32) for n in (pages, -(-pages // 4), -(-(-(-pages // 4)) // 4))]
+        got = host_views(lib, summ)
+        for b, n in enumerate(h_lens):
+            for h in range(H):
+                for a, g, u in zip(arrays, got, units_of(ref.rows_of(hk, hs, 0, h_table[b], h, n), B, 4, 4) if n else ()):
+                    a[b, h, : len(u)] = u
+                    assert np.array_equal(g[b, h, : len(u)], u), (step, b, h)
+        qb = q.view(torch.int16).numpy().view(np.uint16)
+        want_ids, want_n = oracle.select(qb, *arrays, np.array(h_lens, np.int32), geom, oplan, room)
+        assert np.array_equal(ids.cpu().numpy(), want_ids) and np.array_equal(nsel.cpu().numpy(), want_n), step
+        got_out, qn = out.cpu().double().numpy(), q.double().numpy()
+        for b, n in enumerate(h_lens):
+            for h in range(H):
+                at = [t for p in want_ids[b, h, : want_n[b, h]] for t in range(p * B, min(n, p * B + B))]
+                kl, vl = (ref.rows_of(p, hs, w, h_table[b], h, n)[at] for w, p in ((0, hk), (1, hv)))
+                o, off = ref.attention(qn[b, 4 * h:4 * h + 4], kl, vl, 1 / math.sqrt(D))
+                assert (np.abs(got_out[b, 4 * h:4 * h + 4] - o) <= off).all(), (step, b, h)
+    assert lib.workspace_error(ws) == 0
