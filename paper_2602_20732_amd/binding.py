@@ -153,20 +153,22 @@ def _stream():
 
 
 _BYTES = (torch.uint8, torch.float8_e4m3fn)
-_INT, _LONG, _FLOAT, _BF16 = (torch.int32,), (torch.int64,), (torch.float32,), (torch.bfloat16,)
+_INT, _LONG, _FLOAT, _BF16, _BYTE = (torch.int32,), (torch.int64,), (torch.float32,), (torch.bfloat16,), (torch.uint8,)
 
 
-def _need(t, name, dtypes, numel):
-    """A contiguous tensor on the current device, of one of the types, with that many elements at least.  (The library sees a pointer only;
-    about 0.3 us a tensor.)"""
-    if t.dtype not in dtypes or t.numel() < numel or not t.is_contiguous() or t.get_device() != torch.cuda.current_device():
-        raise ChessError(f"{name}: a contiguous {' or '.join(str(d) for d in dtypes)} tensor of at least {numel} elements on the current device is wanted, "
-                         f"got {t.dtype} {tuple(t.shape)} on {t.device}")
+def _need(t, name, dtypes, numel, dev):
+    """A contiguous tensor on device `dev`, the context's, of one of the types, with that many elements at least.  (The library sees a pointer
+    only.  About 0.3 us a tensor: what these calls cost the host matters as much as what the smaller kernels take.)"""
+    if t.dtype not in dtypes or t.numel() < numel or not t.is_contiguous() or t.get_device() != dev:
+        raise ChessError(f"{name}: a contiguous {' or '.join(str(d) for d in dtypes)} tensor of at least {numel} elements on the context's device is wanted, "
+                         f"got {t.dtype} {tuple(t.shape)} of strides {t.stride()} on {t.device}")
 
 
 class Chess:
     """One configured instance of the library (one layer's shapes).  Methods launch asynchronously on the
     current torch stream and return nothing; outputs are the tensors passed in."""
+
+    device = None     # index of the device the context was created on
 
     def __init__(self, cfg: Config):
         self.lib = load_library()
@@ -177,6 +179,7 @@ class Chess:
         h = ctypes.c_void_p()
         self._check(self.lib.chess_create(ctypes.byref(c), ctypes.byref(h)))
         self._h = h
+        self.device = torch.cuda.current_device()
         n = ctypes.c_size_t()
         self._check(self.lib.chess_summary_bytes(h, ctypes.byref(n)))
         self.summary_bytes = n.value
@@ -320,94 +323,107 @@ class Chess:
         return n.value
 
     def release_pages(self, seq_lens, done, block_table, free_pages, n_free, lens_after, n_left, workspace):
-        batch = seq_lens.shape[0]
-        for t, name, numel in ((seq_lens, "seq_lens", batch), (done, "done", batch), (block_table, "block_table", batch * self.cfg.max_pages_per_seq),
-                               (free_pages, "free_pages", 1), (n_free, "n_free", 1), (lens_after, "lens_after", batch), (n_left, "n_left", 1)):
-            _need(t, name, _INT, numel)
-        self._check(self.lib.chess_release_pages(self._h, _ptr(seq_lens), _ptr(done), batch, _ptr(block_table), _ptr(free_pages),
-                                                 free_pages.shape[0], _ptr(n_free), _ptr(lens_after), _ptr(n_left), _ptr(workspace), _stream()))
+        batch, dev = seq_lens.shape[0], self.device
+        _need(seq_lens, "seq_lens", _INT, batch, dev)
+        _need(done, "done", _INT, batch, dev)
+        _need(block_table, "block_table", _INT, batch * self.cfg.max_pages_per_seq, dev)
+        _need(free_pages, "free_pages", _INT, 1, dev)
+        _need(n_free, "n_free", _INT, 1, dev)
+        _need(lens_after, "lens_after", _INT, batch, dev)
+        _need(n_left, "n_left", _INT, 1, dev)
+        self._check(self.lib.chess_release_pages(self._h, seq_lens.data_ptr(), done.data_ptr(), batch, block_table.data_ptr(), free_pages.data_ptr(),
+                                                 free_pages.numel(), n_free.data_ptr(), lens_after.data_ptr(), n_left.data_ptr(),
+                                                 workspace.data_ptr(), torch._C._cuda_getCurrentRawStream(dev)))
 
     def map_tokens(self, seq_lens, new_lens, block_table, free_pages, n_free, lens_after, n_left, token_start, slots, writes, counts, workspace,
                    max_tokens=None):
         """max_tokens: by default what `slots` has room for; slots may be None if it is given."""
-        batch = seq_lens.shape[0]
         if max_tokens is None:
             if slots is None:
                 raise ChessError("map_tokens: slots or max_tokens is wanted")
-            max_tokens = slots.shape[0]
-        for t, name, numel in ((seq_lens, "seq_lens", batch), (new_lens, "new_lens", batch),
-                               (block_table, "block_table", batch * self.cfg.max_pages_per_seq), (free_pages, "free_pages", 1), (n_free, "n_free", 1),
-                               (lens_after, "lens_after", batch), (n_left, "n_left", 1), (token_start, "token_start", batch + 1),
-                               (writes, "writes", 4 * min(max_tokens, max_tokens // self.cfg.page_size + 2 * batch)), (counts, "counts", 4)):
-            _need(t, name, _INT, numel)
+            max_tokens = slots.numel()
+        batch, dev = seq_lens.shape[0], self.device
+        _need(seq_lens, "seq_lens", _INT, batch, dev)
+        _need(new_lens, "new_lens", _INT, batch, dev)
+        _need(block_table, "block_table", _INT, batch * self.cfg.max_pages_per_seq, dev)
+        _need(free_pages, "free_pages", _INT, 1, dev)
+        _need(n_free, "n_free", _INT, 1, dev)
+        _need(lens_after, "lens_after", _INT, batch, dev)
+        _need(n_left, "n_left", _INT, 1, dev)
+        _need(token_start, "token_start", _INT, batch + 1, dev)
         if slots is not None:
-            _need(slots, "slots", _LONG, max_tokens)
-        self._check(self.lib.chess_map_tokens(self._h, _ptr(seq_lens), _ptr(new_lens), batch, max_tokens, _ptr(block_table), _ptr(free_pages),
-                                              _ptr(n_free), _ptr(lens_after), _ptr(n_left), _ptr(token_start), _ptr(slots), _ptr(writes),
-                                              _ptr(counts), _ptr(workspace), _stream()))
+            _need(slots, "slots", _LONG, max_tokens, dev)
+        _need(writes, "writes", _INT, 4 * min(max_tokens, max_tokens // self.cfg.page_size + 2 * batch), dev)
+        _need(counts, "counts", _INT, 4, dev)
+        self._check(self.lib.chess_map_tokens(self._h, seq_lens.data_ptr(), new_lens.data_ptr(), batch, max_tokens, block_table.data_ptr(),
+                                              free_pages.data_ptr(), n_free.data_ptr(), lens_after.data_ptr(), n_left.data_ptr(),
+                                              token_start.data_ptr(), _ptr(slots), writes.data_ptr(), counts.data_ptr(), workspace.data_ptr(),
+                                              torch._C._cuda_getCurrentRawStream(dev)))
 
     # ---- the cache in 8 bits: pools uint8 or float8_e4m3fn, scales fp32 [physical page, H_kv, 2]
-    def _need_pool(self, pool, scales, name):
+    def _need_pool(self, pool, scales, name, dev):
         block = self.cfg.page_size * self.cfg.head_dim
-        _need(pool, name, _BYTES, block)
+        _need(pool, name, _BYTES, block, dev)
         if pool.numel() * 2 != scales.numel() * block:
             raise ChessError(f"{name}: {pool.numel()} bytes and {scales.numel()} scales are not of the same pages")
 
     def quant_store(self, k_new, v_new, writes, counts, k_pool, v_pool, scales):
         """k_new / v_new: bf16 [tokens, H_kv, 128], the rows of a token contiguous (slices of a wider projection will do); no tokens, nothing
         stored."""
-        H, d = self.cfg.n_kv_heads, self.cfg.head_dim
+        n, H, d, dev = k_new.shape[0], self.cfg.n_kv_heads, self.cfg.head_dim, self.device
         for t, name in ((k_new, "k_new"), (v_new, "v_new")):
-            if t.dtype != torch.bfloat16 or tuple(t.shape[1:]) != (H, d) or t.stride(2) != 1 or (t.stride(1) != d and H > 1) or t.get_device() != torch.cuda.current_device():
-                raise ChessError(f"{name}: a bf16 tensor [tokens, {H}, {d}] on the current device with contiguous token rows is wanted, "
+            if t.dtype is not torch.bfloat16 or t.shape != (n, H, d) or t.stride(2) != 1 or (t.stride(1) != d and H > 1) or t.get_device() != dev:
+                raise ChessError(f"{name}: a bf16 tensor [{n}, {H}, {d}] on the context's device with contiguous token rows is wanted, "
                                  f"got {t.dtype} {tuple(t.shape)} of strides {t.stride()} on {t.device}")
-        _need(writes, "writes", _INT, 4)
-        _need(counts, "counts", _INT, 4)
-        _need(scales, "scales", _FLOAT, 2 * H)
-        self._need_pool(k_pool, scales, "k_pool")
-        self._need_pool(v_pool, scales, "v_pool")
-        if k_new.shape[0] != v_new.shape[0]:
-            raise ChessError(f"k_new and v_new have {k_new.shape[0]} and {v_new.shape[0]} tokens")
-        if k_new.shape[0] == 0:
+        _need(writes, "writes", _INT, 4, dev)
+        _need(counts, "counts", _INT, 4, dev)
+        _need(scales, "scales", _FLOAT, 2 * H, dev)
+        self._need_pool(k_pool, scales, "k_pool", dev)
+        self._need_pool(v_pool, scales, "v_pool", dev)
+        if n == 0:
             return
-        self._check(self.lib.chess_quant_store(self._h, _ptr(k_new), k_new.stride(0), _ptr(v_new), v_new.stride(0), _ptr(writes), _ptr(counts),
-                                               writes.numel() // 4, _ptr(k_pool), _ptr(v_pool), _ptr(scales), _stream()))
+        self._check(self.lib.chess_quant_store(self._h, k_new.data_ptr(), k_new.stride(0), v_new.data_ptr(), v_new.stride(0), writes.data_ptr(),
+                                               counts.data_ptr(), writes.numel() // 4, k_pool.data_ptr(), v_pool.data_ptr(), scales.data_ptr(),
+                                               torch._C._cuda_getCurrentRawStream(dev)))
 
     def quant_summarize(self, k_pool, scales, block_table, seq_lens, summaries, from_page=None, recent_pages: int = 0):
-        batch = seq_lens.shape[0]
-        _need(scales, "scales", _FLOAT, 2 * self.cfg.n_kv_heads)
-        self._need_pool(k_pool, scales, "k_pool")
-        _need(block_table, "block_table", _INT, batch * self.cfg.max_pages_per_seq)
-        _need(seq_lens, "seq_lens", _INT, batch)
+        batch, dev = seq_lens.shape[0], self.device
+        _need(scales, "scales", _FLOAT, 2 * self.cfg.n_kv_heads, dev)
+        self._need_pool(k_pool, scales, "k_pool", dev)
+        _need(block_table, "block_table", _INT, batch * self.cfg.max_pages_per_seq, dev)
+        _need(seq_lens, "seq_lens", _INT, batch, dev)
         if from_page is not None:
-            _need(from_page, "from_page", _INT, batch)
-        _need(summaries, "summaries", (torch.uint8,), self.summary_bytes)
-        self._check(self.lib.chess_quant_summarize(self._h, _ptr(k_pool), _ptr(scales), _ptr(block_table), _ptr(seq_lens), batch, _ptr(from_page),
-                                                   recent_pages, _ptr(summaries), _stream()))
+            _need(from_page, "from_page", _INT, batch, dev)
+        _need(summaries, "summaries", _BYTE, self.summary_bytes, dev)
+        self._check(self.lib.chess_quant_summarize(self._h, k_pool.data_ptr(), scales.data_ptr(), block_table.data_ptr(), seq_lens.data_ptr(), batch,
+                                                   _ptr(from_page), recent_pages, summaries.data_ptr(), torch._C._cuda_getCurrentRawStream(dev)))
 
-    def _need_attention(self, q, k_pool, v_pool, scales, block_table, seq_lens, out, batch):
+    def _need_attention(self, q, k_pool, v_pool, scales, block_table, seq_lens, out, batch, dev):
         c = self.cfg
-        _need(q, "q", _BF16, batch * c.n_q_heads * c.head_dim)
-        _need(scales, "scales", _FLOAT, 2 * c.n_kv_heads)
-        self._need_pool(k_pool, scales, "k_pool")
-        self._need_pool(v_pool, scales, "v_pool")
-        _need(block_table, "block_table", _INT, batch * c.max_pages_per_seq)
-        _need(seq_lens, "seq_lens", _INT, batch)
-        _need(out, "out", _FLOAT, batch * c.n_q_heads * c.head_dim)
+        values = batch * c.n_q_heads * c.head_dim
+        _need(q, "q", _BF16, values, dev)
+        _need(scales, "scales", _FLOAT, 2 * c.n_kv_heads, dev)
+        self._need_pool(k_pool, scales, "k_pool", dev)
+        self._need_pool(v_pool, scales, "v_pool", dev)
+        _need(block_table, "block_table", _INT, batch * c.max_pages_per_seq, dev)
+        _need(seq_lens, "seq_lens", _INT, batch, dev)
+        _need(out, "out", _FLOAT, values, dev)
 
     def quant_sparse_decode(self, q, k_pool, v_pool, scales, block_table, seq_lens, page_ids, n_selected, out, workspace):
-        batch = seq_lens.shape[0]
-        self._need_attention(q, k_pool, v_pool, scales, block_table, seq_lens, out, batch)
-        _need(page_ids, "page_ids", _INT, batch * self.cfg.n_kv_heads * self.cfg.max_selected_pages)
-        _need(n_selected, "n_selected", _INT, batch * self.cfg.n_kv_heads)
-        self._check(self.lib.chess_quant_sparse_decode(self._h, _ptr(q), _ptr(k_pool), _ptr(v_pool), _ptr(scales), _ptr(block_table), _ptr(seq_lens),
-                                                       _ptr(page_ids), _ptr(n_selected), batch, _ptr(out), _ptr(workspace), _stream()))
+        batch, dev = seq_lens.shape[0], self.device
+        self._need_attention(q, k_pool, v_pool, scales, block_table, seq_lens, out, batch, dev)
+        _need(page_ids, "page_ids", _INT, batch * self.cfg.n_kv_heads * self.cfg.max_selected_pages, dev)
+        _need(n_selected, "n_selected", _INT, batch * self.cfg.n_kv_heads, dev)
+        self._check(self.lib.chess_quant_sparse_decode(self._h, q.data_ptr(), k_pool.data_ptr(), v_pool.data_ptr(), scales.data_ptr(),
+                                                       block_table.data_ptr(), seq_lens.data_ptr(), page_ids.data_ptr(), n_selected.data_ptr(),
+                                                       batch, out.data_ptr(), workspace.data_ptr(), torch._C._cuda_getCurrentRawStream(dev)))
 
     def quant_dense_decode(self, q, k_pool, v_pool, scales, block_table, seq_lens, out, workspace):
-        batch = seq_lens.shape[0]
-        self._need_attention(q, k_pool, v_pool, scales, block_table, seq_lens, out, batch)
-        self._check(self.lib.chess_quant_dense_decode(self._h, _ptr(q), _ptr(k_pool), _ptr(v_pool), _ptr(scales), _ptr(block_table), _ptr(seq_lens),
-                                                      batch, _ptr(out), _ptr(workspace), _stream()))
+        batch, dev = seq_lens.shape[0], self.device
+        self._need_attention(q, k_pool, v_pool, scales, block_table, seq_lens, out, batch, dev)
+        self._check(self.lib.chess_quant_dense_decode(self._h, q.data_ptr(), k_pool.data_ptr(), v_pool.data_ptr(), scales.data_ptr(),
+                                                      block_table.data_ptr(), seq_lens.data_ptr(), batch, out.data_ptr(), workspace.data_ptr(),
+                                                      torch._C._cuda_getCurrentRawStream(dev)))
 
     def workspace_error(self, workspace) -> int:
         flag = ctypes.c_int32()

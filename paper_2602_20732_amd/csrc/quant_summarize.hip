@@ -3,7 +3,7 @@
 // e4m3 values are multiples of 2^-9 up to 448, so the sum of up to 32 of them has 23 bits: it is exact in fp32, in whatever order it is
 // formed, and times a power of two still is.  A full page's mean is that number times scale / B; a partial one's is divided in fp64 and
 // rounded once, as the summaries of bf16 pages are.
-// One workgroup owns one (sequence, KV head, grid); 8 lanes stream a page, 16 dims a lane (a row is 128 bytes).  Chunk and grid vectors as there.
+// quant_summarize_kernel: one workgroup owns one (sequence, KV head, grid); 8 lanes stream a page, 16 dims a lane (a row is 128 bytes).  Chunk and grid vectors as there.
 // Bound: HBM (one byte an element).
 #include <algorithm>
 
@@ -12,31 +12,25 @@
 
 namespace chess {
 
-// 16 dims of a row added to their sums.
-__device__ __forceinline__ void add_bytes(float (&acc)[16], const uint4& r)
+// Eight dims of a row added to their sums.
+__device__ __forceinline__ void add_bytes(float (&acc)[8], uint32_t a, uint32_t b)
 {
-    const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+    const f32x2 v[4] = {__builtin_amdgcn_cvt_pk_f32_fp8((int)a, false), __builtin_amdgcn_cvt_pk_f32_fp8((int)a, true),
+                        __builtin_amdgcn_cvt_pk_f32_fp8((int)b, false), __builtin_amdgcn_cvt_pk_f32_fp8((int)b, true)};
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[i], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)w[i], true);
-        acc[4 * i] += lo.x; acc[4 * i + 1] += lo.y; acc[4 * i + 2] += hi.x; acc[4 * i + 3] += hi.y;
-    }
+    for (int i = 0; i < 4; ++i) { acc[2 * i] += v[i].x; acc[2 * i + 1] += v[i].y; }
 }
 
-// The mean of n of a page's rows from their sum, as a vector stores it: 16 dims.
+// The mean of n of a page's rows from their sum, as a vector stores it: eight dims.
 template <int B, class T>
-__device__ __forceinline__ void put_means(Row8<T> (&to)[2], const float (&sum)[16], float scale, int n)
+__device__ __forceinline__ Row8<T> mean_of_rows(const float (&sum)[8], float scale, int n)
 {
+    double mean[8];
 #pragma unroll
-    for (int half = 0; half < 2; ++half) {
-        double mean[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float s = sum[8 * half + i];
-            mean[i] = n == B ? (double)(s * (scale * (1.f / B))) : (double)s * (double)scale / (double)n;
-        }
-        to[half].set(mean);
-    }
+    for (int i = 0; i < 8; ++i) mean[i] = n == B ? (double)(sum[i] * (scale * (1.f / B))) : (double)sum[i] * (double)scale / (double)n;
+    Row8<T> r;
+    r.set(mean);
+    return r;
 }
 
 template <int B, class T>
@@ -77,7 +71,7 @@ __global__ __launch_bounds__(256) void quant_summarize_kernel(const uint8_t* __r
             const int n = j == P - 1 ? L - j * B : B;
             const uint4* src = reinterpret_cast<const uint4*>(k_pool + ph * (B * kHeadDim)) + ln;
             const float scale = scales[2 * ph];
-            float acc[16] = {};
+            float lo[8] = {}, hi[8] = {};
 #pragma unroll
             for (int t0 = 0; t0 < B; t0 += 16) {
                 uint4 r[16];
@@ -85,9 +79,13 @@ __global__ __launch_bounds__(256) void quant_summarize_kernel(const uint8_t* __r
                 for (int t = 0; t < 16; ++t) r[t] = src[min(t0 + t, n - 1) * 8];     // (rows past the last token repeat it and are not added)
 #pragma unroll
                 for (int t = 0; t < 16; ++t)
-                    if (t0 + t < n) add_bytes(acc, r[t]);
+                    if (t0 + t < n) {
+                        add_bytes(lo, r[t].x, r[t].y);
+                        add_bytes(hi, r[t].z, r[t].w);
+                    }
             }
-            put_means<B>(mean, acc, scale, n);
+            mean[0] = mean_of_rows<B, T>(lo, scale, n);
+            mean[1] = mean_of_rows<B, T>(hi, scale, n);
             mean[0].store(own);
             mean[1].store(own + 8);
         } else if (j / g.n_c >= fc) {                 // unchanged page whose chunk is being refreshed
@@ -103,11 +101,37 @@ __global__ __launch_bounds__(256) void quant_summarize_kernel(const uint8_t* __r
     units_above<T>(lds, lds_chunk, g, gk, P, p_lo, c_lo, c_hi, fc, cg, gg, tid);
 }
 
+// The last pages of every sequence, as summarize_recent_kernel does it for bf16: 16 lanes a page, 8 dims a lane.
+// shape: recent | n_c << 5 | n_g << 10 | KV heads << 15.
+template <int B, class T>
+__global__ __launch_bounds__(256) void quant_recent_kernel(uint64_t seq_lens_at, uint64_t block_table_at, uint64_t k_pool_at, uint64_t pages_at,
+                                                           int max_pages, int shape, int rows, int max_chunks, uint32_t inv_nc, uint32_t inv_ng,
+                                                           int max_grids, uint64_t scales_at)
+{
+    refresh_recent<B, T>(seq_lens_at, block_table_at, pages_at, max_pages, shape, rows, max_chunks, inv_nc, inv_ng, max_grids,
+                         [&](int64_t block, int n, int ln) {
+        const uint2* src = reinterpret_cast<const uint2*>(device_pointer<const uint8_t>(k_pool_at) + block * (B * kHeadDim)) + ln;
+        const float scale = device_pointer<const float>(scales_at)[2 * block];
+        uint2 r[B];
+        float sum[8] = {};
+#pragma unroll
+        for (int t = 0; t < B; ++t) r[t] = src[min(t, n - 1) * 16];                  // (rows past the last token repeat it and are not added)
+#pragma unroll
+        for (int t = 0; t < B; ++t)
+            if (t < n) add_bytes(sum, r[t].x, r[t].y);
+        return mean_of_rows<B, T>(sum, scale, n);
+    });
+}
+
 template <int B, class T>
 static hipError_t launch_all(chess_ctx* ctx, const uint8_t* k_pool, const float* scales, const int32_t* block_table, const int32_t* seq_lens,
                              int batch, const int32_t* from_page, int recent, void* pages, void* chunks, void* grids, hipStream_t stream)
 {
     const Geom& g = ctx->geom;
+    if (recent > 0 && fits_recent(g, recent))
+        return launch(quant_recent_kernel<B, T>, dim3(g.n_kv_heads, batch), dim3(256), recent_lds_bytes(g, recent, sizeof(T)), stream, (uint64_t)seq_lens,
+                      (uint64_t)block_table, (uint64_t)k_pool, (uint64_t)pages, g.max_pages, recent | g.n_c << 5 | g.n_g << 10 | g.n_kv_heads << 15,
+                      ctx->cfg.max_batch * g.n_kv_heads, g.max_chunks, g.inv_nc, g.inv_ng, g.max_grids, (uint64_t)scales);
     const int ppg = g.n_c * g.n_g;
     const size_t lds = (size_t)(ppg + g.n_g) * kHeadDim * sizeof(T);
     const int span = recent > 0 ? std::min(g.max_grids, (recent + ppg - 2) / ppg + 1) : g.max_grids;   // grids `recent` pages can touch
