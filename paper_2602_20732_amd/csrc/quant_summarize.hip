@@ -3,8 +3,13 @@
 // e4m3 values are multiples of 2^-9 up to 448, so the sum of up to 32 of them has 23 bits: it is exact in fp32, in whatever order it is
 // formed, and times a power of two still is.  A full page's mean is that number times scale / B; a partial one's is divided in fp64 and
 // rounded once, as the summaries of bf16 pages are.
-// quant_summarize_kernel: one workgroup owns one (sequence, KV head, grid); 8 lanes stream a page, 16 dims a lane (a row is 128 bytes).  Chunk and grid vectors as there.
-// Bound: HBM (one byte an element).
+// quant_summarize_kernel: one workgroup owns one (sequence, KV head, grid); 8 lanes stream a page, 16 dims a lane (a row is 128 bytes).  Chunk
+// and grid vectors as there.
+// Bound: HBM, read and written (a fp32 vector is a quarter of a page of 16).  us, 8 sequences of 30-131K, 8 KV heads, pages of 16, fp32 vectors / 2
+// of 196-222K, 4 heads, pages of 32, bf16 / 3 of 700-2161, 8 heads, of 32, bf16:
+//   256 threads, 16 rows in flight   182 / 56 / 14.9      512 threads, 8 / 16 rows   180 / 53 / 10.1    182 / 56 / 9.9
+//   1024 threads, 8 rows             197 / 61 / 9.9       512, 8, rows as a stream   180 / 49 / 11.1 (hence kOnce: see launch_all)
+// The first is 4.8 to 5.2 TB/s, read and written, from card to card (a copy of 2 GiB: 4.8).  Vectors stored as a stream: 240 where 169 without.
 #include <algorithm>
 
 #include "quant_device.h"
@@ -33,8 +38,10 @@ __device__ __forceinline__ Row8<T> mean_of_rows(const float (&sum)[8], float sca
     return r;
 }
 
-template <int B, class T>
-__global__ __launch_bounds__(256) void quant_summarize_kernel(const uint8_t* __restrict__ k_pool, const float* __restrict__ scales,
+constexpr int kSumThreads = 512;
+constexpr int kSumRows = 8;                           // rows of a page in flight
+template <int B, class T, bool kOnce>
+__global__ __launch_bounds__(kSumThreads) void quant_summarize_kernel(const uint8_t* __restrict__ k_pool, const float* __restrict__ scales,
                                                               const int32_t* __restrict__ block_table, const int32_t* __restrict__ seq_lens,
                                                               const int32_t* __restrict__ from_page, int recent, Geom g, T* __restrict__ pages,
                                                               T* __restrict__ chunks, T* __restrict__ grids)
@@ -62,23 +69,23 @@ __global__ __launch_bounds__(256) void quant_summarize_kernel(const uint8_t* __r
     T* lds_chunk = lds + (size_t)ppg * kHeadDim;
 
     const int grp = tid >> 3, ln = tid & 7;
-    for (int j = p_lo + grp; j < p_hi; j += 32) {
+    for (int j = p_lo + grp; j < p_hi; j += kSumThreads / 8) {
         T* dst = lds + (size_t)(j - p_lo) * kHeadDim + ln * 16;
         T* own = pg + (size_t)j * kHeadDim + ln * 16;
         Row8<T> mean[2];
         if (j >= fp) {
             const int64_t ph = (int64_t)block_table[(size_t)b * g.max_pages + j] * g.n_kv_heads + h;
             const int n = j == P - 1 ? L - j * B : B;
-            const uint4* src = reinterpret_cast<const uint4*>(k_pool + ph * (B * kHeadDim)) + ln;
+            const uint8_t* src = k_pool + ph * (B * kHeadDim) + ln * 16;
             const float scale = scales[2 * ph];
             float lo[8] = {}, hi[8] = {};
 #pragma unroll
-            for (int t0 = 0; t0 < B; t0 += 16) {
-                uint4 r[16];
+            for (int t0 = 0; t0 < B; t0 += kSumRows) {
+                uint4 r[kSumRows];
 #pragma unroll
-                for (int t = 0; t < 16; ++t) r[t] = src[min(t0 + t, n - 1) * 8];     // (rows past the last token repeat it and are not added)
+                for (int t = 0; t < kSumRows; ++t) r[t] = load_16<kOnce>(src + min(t0 + t, n - 1) * kHeadDim);   // (rows past the last token repeat it and are not added)
 #pragma unroll
-                for (int t = 0; t < 16; ++t)
+                for (int t = 0; t < kSumRows; ++t)
                     if (t0 + t < n) {
                         add_bytes(lo, r[t].x, r[t].y);
                         add_bytes(hi, r[t].z, r[t].w);
@@ -98,7 +105,7 @@ __global__ __launch_bounds__(256) void quant_summarize_kernel(const uint8_t* __r
         mean[1].store(dst + 8);
     }
     __syncthreads();
-    units_above<T>(lds, lds_chunk, g, gk, P, p_lo, c_lo, c_hi, fc, cg, gg, tid);
+    units_above<T, kSumThreads>(lds, lds_chunk, g, gk, P, p_lo, c_lo, c_hi, fc, cg, gg, tid);
 }
 
 // The last pages of every sequence, as summarize_recent_kernel does it for bf16: 16 lanes a page, 8 dims a lane.
@@ -135,12 +142,14 @@ static hipError_t launch_all(chess_ctx* ctx, const uint8_t* k_pool, const float*
     const int ppg = g.n_c * g.n_g;
     const size_t lds = (size_t)(ppg + g.n_g) * kHeadDim * sizeof(T);
     const int span = recent > 0 ? std::min(g.max_grids, (recent + ppg - 2) / ppg + 1) : g.max_grids;   // grids `recent` pages can touch
-    const auto kern = quant_summarize_kernel<B, T>;
+    // rows as a stream once they are more than the L2s hold (8 x 4 MB); fewer may still be there from the store that wrote them
+    const bool once = (int64_t)batch * g.max_pages * g.n_kv_heads * B * kHeadDim > 32LL << 20;
+    const auto kern = once ? quant_summarize_kernel<B, T, true> : quant_summarize_kernel<B, T, false>;
     if (lds > 64 * 1024) {
         const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
         if (e != hipSuccess) return e;
     }
-    return launch(kern, dim3(span, g.n_kv_heads, batch), dim3(256), lds, stream, k_pool, scales, block_table, seq_lens, from_page, recent, g,
+    return launch(kern, dim3(span, g.n_kv_heads, batch), dim3(kSumThreads), lds, stream, k_pool, scales, block_table, seq_lens, from_page, recent, g,
                   static_cast<T*>(pages), static_cast<T*>(chunks), static_cast<T*>(grids));
 }
 

@@ -53,12 +53,12 @@ __device__ __forceinline__ void put_mean(float* p, double m) { *p = (float)m; }
 __device__ __forceinline__ void put_mean(uint16_t* p, double m) { *p = (uint16_t)Row8<uint16_t>::bf(m); }
 
 // The chunk vectors [c_lo, c_hi) of grid gk, those from fc on formed from the grid's page vectors in LDS (the first is page p_lo's) and
-// the others read, then the grid's own.  256 threads; the page vectors are in place.
-template <class T>
+// the others read, then the grid's own.  kThreads threads; the page vectors are in place.
+template <class T, int kThreads = 256>
 __device__ __forceinline__ void units_above(const T* lds, T* lds_chunk, const Geom& g, int gk, int P, int p_lo, int c_lo, int c_hi, int fc,
                                             T* __restrict__ cg, T* __restrict__ gg, int tid)
 {
-    for (int idx = tid; idx < (c_hi - c_lo) * kHeadDim; idx += 256) {
+    for (int idx = tid; idx < (c_hi - c_lo) * kHeadDim; idx += kThreads) {
         const int c = c_lo + idx / kHeadDim, dim = idx % kHeadDim;
         T v;
         if (c >= fc) {
