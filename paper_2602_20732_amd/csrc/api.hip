@@ -124,7 +124,7 @@ SplitShape choose_quant_splits(const chess_ctx* ctx, int batch, int64_t max_list
     const chess::Geom& g = ctx->geom;
     const chess::SplitLimits c{ctx->n_cu, ctx->quant_blocks * ctx->n_cu, ctx->max_splits, g.n_kv_heads, g.group,
                                2 * chess::kTileTokens / g.page_size, ctx->force_splits, ctx->force_waves};
-    return chess::choose_splits(c, batch, max_list_pages, listed);
+    return chess::choose_quant_splits(c, batch, max_list_pages, listed);
 }
 
 // Whether the context's device is the current one: a launch goes there.

@@ -26,10 +26,10 @@ __device__ __forceinline__ bf16x8 operand_of(uint32_t lo, uint32_t hi, float sca
     return bf16x8{a.x, a.y, b.x, b.y, c.x, c.y, d.x, d.y};
 }
 
-// Where a lane finds its parts of a tile: the page its key rows lie in (tokens 16 (m16 / 4) ..), the page of its own 16 tokens (16 grp ..) and
-// how many of these exist.
+// Where a lane finds its parts of a tile: the physical page its key rows lie in (tokens 16 (m16 / 4) ..), that of its own 16 tokens (16 grp ..), and
+// the logical page of these.
 struct QuantRef {
-    int pk, pv, nt;
+    int pk, pv, lv;
 };
 
 template <int B>
@@ -37,48 +37,56 @@ struct QuantTile {
     uint4 k[4][2];      // [product][half row]
     uint4 v[8];         // [16-row block of d]
     float2 scale;       // of the lane's own page: keys, values
-    int nt;
+    int nt;             // how many of the lane's own tokens exist (<= 0: none)
 };
 
-// Listed pages of tile t at the lane's two places, as stored in the list (an index beyond the list's last entry is that entry; before the list's
-// length is known, its row's last).
+// A lane's two page slots of tile t: indexes into the list, or logical pages.
+template <int B>
+struct QuantSlots {
+    int k, v;
+    __device__ __forceinline__ QuantSlots(int t, int m16, int grp) : k(t * (kQuantTokens / B) + (m16 >> 2) * 16 / B), v(t * (kQuantTokens / B) + grp * 16 / B) {}
+};
+
+// Listed pages of tile t at the lane's two places, as stored (an index beyond the list's row is its last entry; which entries count is decided later).
+template <int B>
+__device__ __forceinline__ int2 quant_ids(int t, const int32_t* ids, int max_sel, int m16, int grp)
+{
+    const QuantSlots<B> at(t, m16, grp);
+    return make_int2(ids[min(at.k, max_sel - 1)], ids[min(at.v, max_sel - 1)]);
+}
+
+// Their physical pages.  A list: a bad id, or one behind the list's last, must not become a bad address.  Every page: the entry is read before
+// the length is known, and quant_rows replaces those that are beyond it.
 template <int B, bool kList>
-__device__ __forceinline__ void quant_ids(int2& raw, int t, const int32_t* ids, int last, int m16, int grp)
+__device__ __forceinline__ QuantRef quant_pages(int t, const int2& raw, const int32_t* bt_row, int P, int max_pages, int m16, int grp)
 {
-    constexpr int PPT = kQuantTokens / B;
-    const int at_k = t * PPT + (m16 >> 2) * 16 / B, at_v = t * PPT + grp * 16 / B;
-    raw = kList ? make_int2(ids[min(at_k, last)], ids[min(at_v, last)]) : make_int2(at_k, at_v);
+    const QuantSlots<B> at(t, m16, grp);
+    const int lk = kList ? min(max(raw.x, 0), P - 1) : min(at.k, max_pages - 1), lv = kList ? min(max(raw.y, 0), P - 1) : min(at.v, max_pages - 1);
+    return QuantRef{bt_row[lk], bt_row[lv], lv};
 }
 
-template <int B>
-__device__ __forceinline__ QuantRef quant_pages(int t, int n_pages, const int2& raw, const int32_t* bt_row, int L, int P, int m16, int grp)
+template <int B, bool kList, bool kOnce>
+__device__ __forceinline__ void quant_rows(QuantTile<B>& tl, const QuantRef& r, int t, int n_pages, int L, int P, const uint8_t* k_pool,
+                                           const uint8_t* v_pool, const float* scales, int H, int h, int m16, int grp)
 {
-    constexpr int PPT = kQuantTokens / B;
-    // (a page beyond the last, or a bad id, must not become a bad address)
-    const int lk = min(max(raw.x, 0), P - 1), lv = min(max(raw.y, 0), P - 1);
-    const int held = lv == P - 1 ? L - lv * B : B;
-    QuantRef r;
-    r.pk = bt_row[lk];
-    r.pv = bt_row[lv];
-    r.nt = t * PPT + grp * 16 / B < n_pages ? held - 16 * grp % B : 0;
-    return r;
-}
-
-template <int B>
-__device__ __forceinline__ void quant_rows(QuantTile<B>& tl, const QuantRef& r, const uint8_t* k_pool, const uint8_t* v_pool, const float* scales,
-                                           int H, int h, int m16, int grp)
-{
-    const int64_t at_k = ((int64_t)r.pk * H + h) * (B * kHeadDim), at_v = (int64_t)r.pv * H + h;
+    const QuantSlots<B> at(t, m16, grp);
+    int pk = r.pk, pv = r.pv;
+    if constexpr (!kList) {                           // (lane 0 has the tile's first page, which exists)
+        const int first = __builtin_amdgcn_readfirstlane(r.pk);
+        pk = at.k < P ? pk : first;
+        pv = at.v < P ? pv : first;
+    }
+    const int64_t at_k = ((int64_t)pk * H + h) * (B * kHeadDim), at_v = (int64_t)pv * H + h;
     const uint8_t* k_row = k_pool + at_k + ((16 * (m16 >> 2)) % B + (m16 & 3)) * kHeadDim + 16 * grp;
 #pragma unroll
     for (int c = 0; c < 4; ++c)
 #pragma unroll
-        for (int half = 0; half < 2; ++half) tl.k[c][half] = *reinterpret_cast<const uint4*>(k_row + 4 * c * kHeadDim + 64 * half);
+        for (int half = 0; half < 2; ++half) tl.k[c][half] = load_16<kOnce>(k_row + 4 * c * kHeadDim + 64 * half);
     tl.scale = *reinterpret_cast<const float2*>(scales + 2 * at_v);
     const uint8_t* v_row = v_pool + at_v * (B * kHeadDim) + m16 * B + 16 * grp % B;
 #pragma unroll
-    for (int blk = 0; blk < 8; ++blk) tl.v[blk] = *reinterpret_cast<const uint4*>(v_row + blk * 16 * B);
-    tl.nt = r.nt;
+    for (int blk = 0; blk < 8; ++blk) tl.v[blk] = load_16<kOnce>(v_row + blk * 16 * B);
+    tl.nt = at.v < n_pages ? (r.lv == P - 1 ? L - r.lv * B : B) - 16 * grp % B : 0;
 }
 
 // Online-softmax state of one wave: all G heads of one KV head.
@@ -190,8 +198,8 @@ using QuantKernel = void (*)(uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, i
 using QuantLines = ArgLinesOf<QuantKernel, QuantArgs>;
 
 // grid: (n_splits, H_kv, batch), or dealt by length (H_kv, n_slots).  heads: KV heads << 8 | group.
-template <int B, int NW, bool kList, bool kDealt = false>
-__global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2))) void quant_decode_kernel(
+template <int B, int NW, bool kList, bool kDealt = false, bool kOnce = false>
+__global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(kList && NW == 4 ? 3 : 2))) void quant_decode_kernel(
     uint64_t seq_lens_at, uint64_t block_table_at, uint64_t q_at, uint64_t page_ids_at, uint64_t n_selected_at, int heads, int max_sel, int max_pages,
     int n_splits, QuantArgs a)
 {
@@ -225,10 +233,16 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2))) vo
     const int stride = ns * NW;
     int t = split + ns * wave;
     int2 raw_cur, raw_nxt, raw_nn;
+    QuantRef rc, rn;
     if constexpr (!kDealt) L_raw = load_by_lane(seq_lens + b);
     int n_raw = kList ? load_by_lane(device_pointer<const int32_t>(n_selected_at) + row) : 0;
-    quant_ids<B, kList>(raw_cur, t, ids, max_sel - 1, m16, grp);
-    quant_ids<B, kList>(raw_nxt, t + stride, ids, max_sel - 1, m16, grp);
+    if constexpr (kList) {
+        raw_cur = quant_ids<B>(t, ids, max_sel, m16, grp);
+        raw_nxt = quant_ids<B>(t + stride, ids, max_sel, m16, grp);
+    } else {
+        rc = quant_pages<B, false>(t, raw_cur, bt_row, 0, max_pages, m16, grp);
+        rn = quant_pages<B, false>(t + stride, raw_nxt, bt_row, 0, max_pages, m16, grp);
+    }
     QuantAcc acc;
     acc.request(device_pointer<const uint16_t>(q_at) + ((size_t)b * H * G + (size_t)h * G) * kHeadDim, G, m16, grp);
     requested_by_here();
@@ -242,16 +256,17 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2))) vo
     lines.hold();
     acc.start(G, m16);
     if (t < n_tiles) {
-        // block-table entries run one tile ahead of the rows, page numbers one tile ahead of those
-        const int last = kList ? max_sel - 1 : 0;
-        QuantRef rc = quant_pages<B>(t, n_pages, raw_cur, bt_row, L, P, m16, grp);
-        QuantRef rn = quant_pages<B>(t + stride, n_pages, raw_nxt, bt_row, L, P, m16, grp);
-        quant_ids<B, kList>(raw_nn, t + 2 * stride, ids, last, m16, grp);
+        // block-table entries run one tile ahead of the rows, a list's page numbers one tile ahead of those
+        if constexpr (kList) {
+            rc = quant_pages<B, true>(t, raw_cur, bt_row, P, max_pages, m16, grp);
+            rn = quant_pages<B, true>(t + stride, raw_nxt, bt_row, P, max_pages, m16, grp);
+            raw_nn = quant_ids<B>(t + 2 * stride, ids, max_sel, m16, grp);
+        }
         QuantTile<B> tl;
         for (; t < n_tiles; t += stride) {
-            quant_rows<B>(tl, rc, a.k_pool, a.v_pool, a.scales, H, h, m16, grp);
-            const QuantRef rnn = quant_pages<B>(t + 2 * stride, n_pages, raw_nn, bt_row, L, P, m16, grp);
-            quant_ids<B, kList>(raw_nn, t + 3 * stride, ids, last, m16, grp);
+            quant_rows<B, kList, kOnce>(tl, rc, t, n_pages, L, P, a.k_pool, a.v_pool, a.scales, H, h, m16, grp);
+            const QuantRef rnn = quant_pages<B, kList>(t + 2 * stride, raw_nn, bt_row, P, max_pages, m16, grp);
+            if constexpr (kList) raw_nn = quant_ids<B>(t + 3 * stride, ids, max_sel, m16, grp);
             acc.process(tl, a.scale_log2);
             rc = rn;
             rn = rnn;
@@ -280,14 +295,26 @@ hipError_t launch_quant_decode(chess_ctx* ctx, const uint16_t* q, const uint8_t*
     const bool dealt = n_slots > 0;                   // (every page, four waves: see choose_splits)
     const dim3 grid = dealt ? dim3(g.n_kv_heads, n_slots) : dim3(n_splits, g.n_kv_heads, batch), block(64 * waves);
     const size_t lds = quant_lds_bytes(waves, g.group);
-    // [page size 16 / 32][waves 4 / 1][list / every page], eight waves for a list, every page dealt by length
-    static const QuantKernel table[2][2][2] = {
-        {{quant_decode_kernel<16, 4, true>, quant_decode_kernel<16, 4, false>}, {quant_decode_kernel<16, 1, true>, quant_decode_kernel<16, 1, false>}},
-        {{quant_decode_kernel<32, 4, true>, quant_decode_kernel<32, 4, false>}, {quant_decode_kernel<32, 1, true>, quant_decode_kernel<32, 1, false>}}};
-    static const QuantKernel wide[2] = {quant_decode_kernel<16, 8, true>, quant_decode_kernel<32, 8, true>};
-    static const QuantKernel by_length[2] = {quant_decode_kernel<16, 4, false, true>, quant_decode_kernel<32, 4, false, true>};
     const int by_page = g.page_size == 16 ? 0 : 1;
-    const QuantKernel kern = dealt ? by_length[by_page] : waves == 8 ? wide[by_page] : table[by_page][waves == 4 ? 0 : 1][page_ids ? 0 : 1];
+    // Pages as a stream where they are more than stays in the 256 MB behind the L2s from one step to the next (kOnce): us, plain / so, one
+    // sequence of 32768 tokens, 8 KV heads (67 MB) 17.3 / 18.9, 65536 (134 MB) 30.0 / 28.6, 131072 54.6 / 51.9, 262139 of 4 heads, pages of 32,
+    // 56.8 / 53.4; 16 sequences of 8-64K 224 / 218; lists, 96 of 60 pages of 16, 8 heads (188 MB) 40.4 / 37.7, 32 of 108 (113 MB) 23.4 / 24.1.
+    const bool once = (int64_t)batch * (page_ids ? g.max_sel : g.max_pages) * g.page_size * g.n_kv_heads * 2 * kHeadDim > 128LL << 20;
+    // [page size 16 / 32], lists by one, four or eight waves; every page by one, four (short rows, more of them than compute units) or eight; dealt
+    static const QuantKernel lists[3][2] = {{quant_decode_kernel<16, 1, true>, quant_decode_kernel<32, 1, true>},
+                                            {quant_decode_kernel<16, 4, true>, quant_decode_kernel<32, 4, true>},
+                                            {quant_decode_kernel<16, 8, true>, quant_decode_kernel<32, 8, true>}};
+    static const QuantKernel every[3][2] = {{quant_decode_kernel<16, 1, false>, quant_decode_kernel<32, 1, false>},
+                                            {quant_decode_kernel<16, 4, false>, quant_decode_kernel<32, 4, false>},
+                                            {quant_decode_kernel<16, 8, false>, quant_decode_kernel<32, 8, false>}};
+    static const QuantKernel lists_streamed[2] = {quant_decode_kernel<16, 4, true, false, true>, quant_decode_kernel<32, 4, true, false, true>};
+    static const QuantKernel streamed[2][2] = {{quant_decode_kernel<16, 4, false, false, true>, quant_decode_kernel<32, 4, false, false, true>},
+                                               {quant_decode_kernel<16, 8, false, false, true>, quant_decode_kernel<32, 8, false, false, true>}};
+    static const QuantKernel by_length[2][2] = {{quant_decode_kernel<16, 4, false, true>, quant_decode_kernel<32, 4, false, true>},
+                                                {quant_decode_kernel<16, 4, false, true, true>, quant_decode_kernel<32, 4, false, true, true>}};
+    const int by_waves = waves == 8 ? 2 : waves == 4 ? 1 : 0;
+    const QuantKernel kern = dealt ? by_length[once][by_page] : page_ids ? (once && waves == 4 ? lists_streamed[by_page] : lists[by_waves][by_page])
+                                   : once && waves > 1 ? streamed[waves == 8][by_page] : every[by_waves][by_page];
     if (lds > 64 * 1024) {
         const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
         if (e != hipSuccess) return e;

@@ -107,4 +107,22 @@ inline SplitShape choose_splits(const SplitLimits& c, int batch, int64_t max_lis
     return {(int)ns, wide ? 8 : waves, 0};
 }
 
+// The same for 8-bit pages (tiles of 64 tokens, c.tile_pages pages each; c.resident: four-wave workgroups of attention over every page that
+// fit at once).  Lists and batches go by the rules above, which their own sweeps bear out: lists within 3 % of the best of 2 .. 64 splits of four or
+// eight waves, within 6 % of it for 24 rows of 500 pages.  Every page of one sequence: eight waves, at most one workgroup to a compute unit, since each
+// reads as fast alone as two do (us, 262139 tokens, 4 KV heads, G = 7: 64 splits, 256 workgroups, 58; 68, which is 272, 80; 128 76); fewer where the
+// partials outweigh the tiles, in which the merge by twice the threads counts when they have outputs (more than four heads).  us, 8 waves:
+//   2048 tokens, 8 KV heads, G = 4       8 splits  6.9   16  7.3   24  8.3   32  8.7         32768   16 splits 19.0   24 17.6   32 17.3
+//   8192                                 8        12.2   16  9.7   24 10.3   32 10.1        131072   16        67.4   24 54.5   32 54.6
+//   16384, 4 KV heads, G = 7            16        13.5   32 12.2   48 13.2   64 14.2
+inline SplitShape choose_quant_splits(const SplitLimits& c, int batch, int64_t max_list_pages, bool listed)
+{
+    if (c.force_splits > 0) return {c.force_splits, !listed && c.force_waves == 4 ? 8 : c.force_waves, 0};
+    if (listed || batch > 1) return choose_splits(c, batch, max_list_pages, listed);
+    const int64_t tiles = std::max<int64_t>(1, cdiv(max_list_pages, c.tile_pages));
+    const int64_t balanced = (int64_t)std::sqrt((c.group > 4 ? 16.0 : 8.0) * (double)tiles / c.group);
+    const int64_t most = std::min<int64_t>({c.n_cu / c.n_kv_heads, c.max_splits, 1024 / c.group, partial_rows(c.n_cu, c.n_kv_heads) / c.n_kv_heads, tiles});
+    return {(int)clampi(balanced, 1, std::max<int64_t>(most, 1)), 8, 0};
+}
+
 }  // namespace chess

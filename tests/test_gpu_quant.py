@@ -162,7 +162,7 @@ def dealt(rng, lens, pages, B):
     return table, sum(held) + 2
 
 
-def check_attention(rng, lens, Hq, H, B, lists=None, pages=None, splits=(0, 4), scale_spread=True, sm_scale=0.0, q_size=1.0):
+def check_attention(rng, lens, Hq, H, B, lists=None, pages=None, splits=(0, 4), scale_spread=True, sm_scale=0.0, q_size=1.0, room=None):
     """Against fp64 over the listed pages (lists[b][h]) or every page; the bytes behind the last token stay as they fell, NaN among them."""
     G, batch = Hq // H, len(lens)
     pages = pages or max(1, max(-(-n // B) for n in lens))
@@ -175,7 +175,7 @@ def check_attention(rng, lens, Hq, H, B, lists=None, pages=None, splits=(0, 4), 
             m = min(B, n - p * B)
             for page in (cache.k[table[b, p]][:, :m], cache.v[table[b, p]][:, :, :m]):
                 page[page & 127 == 127] = 0x31
-    room = pages if lists is None else max(1, max(len(x) for row in lists for x in row))
+    room = room or (pages if lists is None else max(1, max(len(x) for row in lists for x in row)))
     lib = pk.Chess(pk.Config(Hq, H, B, batch, pages, min(pages, room), sm_scale=sm_scale))
     ws = lib.new_workspace()
     if splits[0]:
@@ -243,6 +243,25 @@ def test_lists_of_any_length(B, splits, Hq, H):
     lists[0][0], lists[0][1] = [], list(range(-(-1000 // B)))    # nothing listed, everything listed
     lists[3][0] = [-(-333 // B) - 1]                             # the tail page alone
     check_attention(rng, lens, Hq, H, B, lists=lists, splits=splits)
+
+
+@pytest.mark.parametrize("B", [16, 32])
+def test_more_rows_than_workgroups(B):
+    rng = np.random.default_rng(21)
+    lens = rng.integers(0, 150, 600).tolist()
+    check_attention(rng, lens, 4, 1, B)
+    check_attention(rng, lens, 4, 1, B, pages=9000 // B)                                  # (pools sized for more than stays in the caches)
+
+
+@pytest.mark.parametrize("B", [16, 32])
+def test_caches_sized_for_long_contexts(B):
+    """Rows of a configuration whose pools are a stream: one sequence, several, lists."""
+    rng = np.random.default_rng(22)
+    check_attention(rng, [2500], 8, 2, B, pages=330000 // B)
+    check_attention(rng, [0, 700, 1, 64, 2100], 8, 2, B, pages=80000 // B)
+    lens = rng.integers(1, 200, 300).tolist()
+    lists = [[sorted(rng.choice(-(-n // B), rng.integers(0, -(-n // B) + 1), replace=False).tolist())] for n in lens]
+    check_attention(rng, lens, 4, 1, B, lists=lists, pages=2000 // B + 1, room=2000 // B)
 
 
 @pytest.mark.parametrize("B", [16, 32])

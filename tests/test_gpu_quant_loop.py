@@ -105,6 +105,22 @@ def test_summaries_of_whole_sequences_and_of_the_last_pages(B, n_c, n_g):
 
 
 @pytest.mark.parametrize("B", [16, 32])
+def test_summaries_in_a_cache_sized_for_long_contexts(B):
+    rng = np.random.default_rng(B)
+    H, lens, pages = 2, [1000, 0, 17], 160000 // B
+    table, k, scales = cache_of(rng, lens, pages, H, B)
+    lib = pk.Chess(pk.Config(4, H, B, 3, pages, 8, summary_dtype=helpers.SUMMARY_DTYPE))
+    summ = lib.new_summaries()
+    lib.quant_summarize(torch.from_numpy(k).cuda(), torch.from_numpy(scales.astype(np.float32)).cuda(), torch.from_numpy(table).cuda(), ints(lens), summ)
+    torch.cuda.synchronize()
+    got = host_views(lib, summ)
+    for b, n in enumerate(lens):
+        for h in range(H):
+            for g, u in zip(got, units_of(ref.rows_of(k, scales, 0, table[b], h, n), B, 8, 8) if n else ()):
+                assert np.array_equal(g[b, h, : len(u)], u) and not g[b, h, len(u):].any()
+
+
+@pytest.mark.parametrize("B", [16, 32])
 def test_a_full_page_of_the_largest_and_smallest_values(B):
     """The sum of a page is exact in fp32 at either end of what a scale can be."""
     k = np.empty((2, 1, B, D), np.uint8)

@@ -4,6 +4,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import subprocess
 
 import numpy as np
 import pytest
@@ -46,6 +47,17 @@ def test_worked_example_of_the_dealing():
     got = ref.map_tokens([15, 0, 0], [2, 17, 1], [[7, -1], [-1, -1], [-1, -1]], [1, 2], 2, 100, 2, 16)
     assert got["lens_after"] == [17, 0, 0] and got["counts"] == [2, 2, 1, 2]
     assert ref.release([17, 5, 3], [1, 0, 1], got["table"][:1] + [[9, -1], [8, -1]], [1, 2, -1, -1, -1], 1, 5, 16) == ([0, 5, 0], [1, 7, 2, 8, -1], 4)
+
+
+def test_split_rule_of_8_bit_pages(tmp_path):
+    """Over device sizes, heads, groups, batches and lengths the partials fit the workspace and one sequence's workgroups the compute units."""
+    exe, root = str(tmp_path / "rule"), os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    res = subprocess.run(["g++", "-std=c++17", "-O1", "-fsanitize=undefined", "-fno-sanitize-recover=all", "-I",
+                          os.path.join(root, "paper_2602_20732_amd", "csrc"), os.path.join(root, "tests", "quant_split_rule_driver.cpp"), "-o", exe],
+                         capture_output=True, text=True)
+    assert res.returncode == 0, res.stderr
+    res = subprocess.run([exe], capture_output=True, text=True, timeout=120)
+    assert res.returncode == 0 and res.stdout.strip() == "ok", res.stdout + res.stderr
 
 
 def test_without_a_context_every_call_is_refused(lib):
