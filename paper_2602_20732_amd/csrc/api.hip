@@ -757,7 +757,8 @@ int chess_release_pages(chess_ctx* ctx, const int32_t* seq_lens, const int32_t* 
     if (batch < 1 || batch > ctx->cfg.max_batch || capacity < 1 || misaligned({workspace}, 15) || !on_device(ctx)) return CHESS_EINVAL;
     if (batch > chess::kPageMost) return CHESS_ENOTSUP;
     const chess::ReleaseArgs a{seq_lens, done, block_table, free_pages, n_free, lens_after, n_left,
-                               reinterpret_cast<int32_t*>(static_cast<char*>(workspace) + ctx->ws_cnt_off), batch, capacity, ctx->geom.max_pages};
+                               reinterpret_cast<int32_t*>(static_cast<char*>(workspace) + ctx->ws_cnt_off), batch, capacity, ctx->geom.max_pages,
+                               lens_after == seq_lens || n_left == n_free};
     return chess::launch_release(ctx, a, static_cast<hipStream_t>(stream)) == hipSuccess ? CHESS_OK : CHESS_EHIP;
 }
 
@@ -773,7 +774,8 @@ int chess_map_tokens(chess_ctx* ctx, const int32_t* seq_lens, const int32_t* new
     if (batch > chess::kPageMost) return CHESS_ENOTSUP;
     const chess::MapArgs a{seq_lens, new_lens, block_table, free_pages, n_free, lens_after, n_left, token_start, slots,
                            reinterpret_cast<int4*>(writes), counts,
-                           reinterpret_cast<int32_t*>(static_cast<char*>(workspace) + ctx->ws_cnt_off), batch, max_tokens, ctx->geom.max_pages};
+                           reinterpret_cast<int32_t*>(static_cast<char*>(workspace) + ctx->ws_cnt_off), batch, max_tokens, ctx->geom.max_pages,
+                           lens_after == seq_lens || n_left == n_free};
     return chess::launch_map(ctx, a, static_cast<hipStream_t>(stream)) == hipSuccess ? CHESS_OK : CHESS_EHIP;
 }
 

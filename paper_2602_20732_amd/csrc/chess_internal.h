@@ -355,7 +355,7 @@ hipError_t launch_decode(chess_ctx* ctx, const uint16_t* q, const uint16_t* k_po
                          float* ws_acc, float* ws_ml, int32_t* arrivals, hipStream_t stream);
 
 // Pages handed out and taken back (pages.hip).  lens_after / n_left may be seq_lens / n_free.
-constexpr int kPageMost = 4096;      // most sequences: their three sums are in LDS
+constexpr int kPageMost = 4096;      // most sequences: their sums are in LDS
 struct MapArgs {
     const int32_t* seq_lens;
     const int32_t* new_lens;
@@ -369,7 +369,7 @@ struct MapArgs {
     int4* writes;
     int32_t* counts;
     int32_t* arrivals;       // one counter, zero between launches
-    int batch, max_tokens, max_pages;
+    int batch, max_tokens, max_pages, in_place;
 };
 struct ReleaseArgs {
     const int32_t* seq_lens;
@@ -380,7 +380,7 @@ struct ReleaseArgs {
     int32_t* lens_after;
     int32_t* n_left;
     int32_t* arrivals;
-    int batch, capacity, max_pages;
+    int batch, capacity, max_pages, in_place;
 };
 // Pages that so many new tokens of `batch` sequences can lie in.
 inline int64_t most_writes(int64_t tokens, int64_t batch, int page_size)

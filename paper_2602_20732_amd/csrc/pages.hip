@@ -4,8 +4,7 @@
 // from the inclusive sums over b of the three.  Every workgroup forms them for itself (one load a sequence, sums by lane shifts and LDS),
 // so there is no pass between counting and writing; then a group of B lanes takes an entry of the write list: finds its sequence in the
 // sums, its page in the free list or the block table, and writes the B slots, the entry and the table.  What is written once a sequence
-// (lengths, starts, counts) is left to the workgroup that arrives last, when nobody reads the lengths or the free count any more: they may
-// be updated in place.  Sums are capped at kSumCap, above every bound they are compared with: they cannot wrap, and stay ordered.
+// (lengths, starts, counts) is one workgroup's; where the lengths or the free count are updated in place, the last one's to arrive.  Sums are capped at kSumCap, above every bound they are compared with: they cannot wrap, and stay ordered.
 // Bound: the chain length -> sums -> search -> page -> slots; 8 bytes a token are little.
 #include "chess_internal.h"
 #include "split_rule.h"
@@ -14,6 +13,7 @@ namespace chess {
 
 constexpr int kPageThreads = 256;
 constexpr int kSumCap = 0x3fffffff;
+constexpr int kFly = 4;              // entries of the write list a group has in hand at a time
 
 __device__ __forceinline__ int capped(int a, int b) { return min(a + b, kSumCap); }
 
@@ -59,16 +59,18 @@ __device__ __forceinline__ void sums_upto(int batch, int* upto, Value value)
     }
 }
 
-// The first of n sums that is above i (the last one is).
-__device__ __forceinline__ int first_above(const int* upto, int n, int i)
+// For each of kN numbers i the first of n sums that is above it (the last one is), in lockstep: log2 n dependent LDS reads for all of them.
+template <int kN>
+__device__ __forceinline__ void first_above(int (&at)[kN], const int* upto, int n, const int (&i)[kN])
 {
-    int lo = 0, hi = n - 1;
-    while (lo < hi) {
-        const int mid = (lo + hi) >> 1;
-        if (upto[mid] > i) hi = mid;
-        else lo = mid + 1;
-    }
-    return lo;
+#pragma unroll
+    for (int x = 0; x < kN; ++x) at[x] = 0;
+    for (int step = 1 << (31 - __builtin_clz(n)); step > 0; step >>= 1)
+#pragma unroll
+        for (int x = 0; x < kN; ++x) {
+            const int to = at[x] + step;
+            if (upto[min(to, n) - 1] <= i[x] && to < n) at[x] = to;
+        }
 }
 
 // How many sequences come before the first that does not fit (fits() never holds again behind that one).
@@ -87,24 +89,28 @@ __device__ __forceinline__ int served(int batch, Fits fits)
     return cut;
 }
 
-__device__ __forceinline__ bool last_here(int32_t* arrivals)
+// Whether this workgroup writes what is written once a sequence: where lengths or the free count are updated in place, the last to arrive, when
+// nobody reads them any more; otherwise any will do.
+__device__ __forceinline__ bool writes_rows(bool in_place, int32_t* arrivals)
 {
     __shared__ int flag;
-    if (gridDim.x > 1) return arrive_last(arrivals, gridDim.x, &flag);
+    if (in_place && gridDim.x > 1) return arrive_last(arrivals, gridDim.x, &flag);
     __syncthreads();
-    return true;
+    return blockIdx.x == 0;
 }
 
 template <int B>
 __global__ __launch_bounds__(kPageThreads) void map_kernel(MapArgs a)
 {
-    extern __shared__ int upto[];                     // [3][batch]: tokens, pages gained, pages touched
+    extern __shared__ int upto[];                     // [3][batch]: tokens, pages gained, pages touched; then [batch] lengths
     __shared__ int n_refused;
     const int batch = a.batch, n_free = max(*a.n_free, 0);
     if (threadIdx.x == 0) n_refused = 0;
     const int *tokens = upto, *gained = upto + batch, *touched = upto + 2 * batch;
+    int* held = upto + 3 * batch;
     sums_upto<3>(batch, upto, [&](int b, int (&v)[3]) {
         const int64_t L = a.seq_lens[b], n = a.new_lens[b];
+        held[b] = (int)L;
         if (L < 0 || n <= 0 || L + n > (int64_t)a.max_pages * B) return;
         v[0] = (int)min(n, (int64_t)kSumCap);
         v[1] = (int)((L + n + B - 1) / B - (L + B - 1) / B);
@@ -113,29 +119,45 @@ __global__ __launch_bounds__(kPageThreads) void map_kernel(MapArgs a)
     const int cut = served(batch, [&](int b) { return tokens[b] <= a.max_tokens && gained[b] <= n_free; });
     const int n_writes = cut > 0 ? touched[cut - 1] : 0;
 
-    const int j = threadIdx.x % B;
-    for (int i = (blockIdx.x * kPageThreads + threadIdx.x) / B; i < n_writes; i += gridDim.x * (kPageThreads / B)) {
-        const int b = first_above(touched, cut, i);
-        const int token0 = b > 0 ? tokens[b - 1] : 0, gained0 = b > 0 ? gained[b - 1] : 0, touched0 = b > 0 ? touched[b - 1] : 0;
-        const int L = a.seq_lens[b], after = L + tokens[b] - token0, had = (L + B - 1) / B;
-        const int page = L / B + i - touched0;
-        const int begin = max(L, page * B), count = min(after, page * B + B) - begin, row = token0 + begin - L;
-        int32_t* entry = a.block_table + (size_t)b * a.max_pages + page;
-        const bool is_new = page >= had;
-        const int phys = is_new ? a.free_pages[n_free - 1 - (gained0 + page - had)] : *entry;
-        if (a.slots != nullptr && j < count) a.slots[row + j] = (int64_t)phys * B + begin % B + j;
-        if (j == 0) {
-            a.writes[i] = make_int4(phys, row, begin % B, count);
-            if (is_new) *entry = phys;
+    const int j = threadIdx.x % B, step = gridDim.x * (kPageThreads / B);
+    for (int i0 = (blockIdx.x * kPageThreads + threadIdx.x) / B; i0 < n_writes; i0 += step * kFly) {
+        // (kFly entries at once: each is a search and two round trips)
+        int4 entry[kFly];
+        int32_t* table_at[kFly];
+        bool is_new[kFly];
+        int i_of[kFly], b_of[kFly];
+#pragma unroll
+        for (int x = 0; x < kFly; ++x) i_of[x] = min(i0 + x * step, n_writes - 1);
+        first_above(b_of, touched, cut, i_of);
+#pragma unroll
+        for (int x = 0; x < kFly; ++x) {
+            const int i = i_of[x], b = b_of[x];
+            const int token0 = b > 0 ? tokens[b - 1] : 0, gained0 = b > 0 ? gained[b - 1] : 0, touched0 = b > 0 ? touched[b - 1] : 0;
+            const int L = held[b], after = L + tokens[b] - token0, had = (L + B - 1) / B;
+            const int page = L / B + i - touched0, begin = max(L, page * B);
+            table_at[x] = a.block_table + (size_t)b * a.max_pages + page;
+            is_new[x] = page >= had;
+            const int32_t* from = is_new[x] ? a.free_pages + (n_free - 1 - (gained0 + page - had)) : table_at[x];
+            entry[x] = make_int4(*from, token0 + begin - L, begin % B, min(after, page * B + B) - begin);
+        }
+#pragma unroll
+        for (int x = 0; x < kFly; ++x) {
+            const int i = i0 + x * step;
+            if (i >= n_writes) break;
+            if (a.slots != nullptr && j < entry[x].w) a.slots[entry[x].y + j] = (int64_t)entry[x].x * B + entry[x].z + j;
+            if (j == 0) {
+                a.writes[i] = entry[x];
+                if (is_new[x]) *table_at[x] = entry[x].x;
+            }
         }
     }
 
-    if (!last_here(a.arrivals)) return;
+    if (!writes_rows(a.in_place, a.arrivals)) return;
     for (int b = threadIdx.x; b < batch; b += kPageThreads) {
         const int upto_b = cut > 0 ? tokens[min(b, cut - 1)] : 0;
         const int got = b < cut ? upto_b - (b > 0 ? tokens[b - 1] : 0) : 0;
         if (a.new_lens[b] > 0 && got == 0) atomicAdd(&n_refused, 1);
-        a.lens_after[b] = a.seq_lens[b] + got;
+        a.lens_after[b] = held[b] + got;
         a.token_start[b + 1] = upto_b;
     }
     __syncthreads();
@@ -150,7 +172,7 @@ __global__ __launch_bounds__(kPageThreads) void map_kernel(MapArgs a)
     }
 }
 
-// The pages of the sequences that ended, behind what the free list holds.  One thread an entry; lengths and counts by the last workgroup, as above.
+// The pages of the sequences that ended, behind what the free list holds.  One thread an entry; lengths and the count by one workgroup, as above.
 template <int B>
 __global__ __launch_bounds__(kPageThreads) void release_kernel(ReleaseArgs a)
 {
@@ -162,10 +184,11 @@ __global__ __launch_bounds__(kPageThreads) void release_kernel(ReleaseArgs a)
     const int cut = served(batch, [&](int b) { return upto[b] <= a.capacity - n_free; });
     const int total = cut > 0 ? upto[cut - 1] : 0;
     for (int i = blockIdx.x * kPageThreads + threadIdx.x; i < total; i += gridDim.x * kPageThreads) {
-        const int b = first_above(upto, cut, i);
-        a.free_pages[n_free + i] = a.block_table[(size_t)b * a.max_pages + i - (b > 0 ? upto[b - 1] : 0)];
+        int b[1];
+        first_above(b, upto, cut, {i});
+        a.free_pages[n_free + i] = a.block_table[(size_t)b[0] * a.max_pages + i - (b[0] > 0 ? upto[b[0] - 1] : 0)];
     }
-    if (!last_here(a.arrivals)) return;
+    if (!writes_rows(a.in_place, a.arrivals)) return;
     for (int b = threadIdx.x; b < batch; b += kPageThreads) a.lens_after[b] = b < cut && a.done[b] != 0 ? 0 : a.seq_lens[b];
     if (threadIdx.x == 0) *a.n_left = n_free + total;
 }
@@ -173,11 +196,14 @@ __global__ __launch_bounds__(kPageThreads) void release_kernel(ReleaseArgs a)
 hipError_t launch_map(chess_ctx* ctx, const MapArgs& a, hipStream_t stream)
 {
     const int B = ctx->geom.page_size;
-    const int64_t entries = most_writes(a.max_tokens, a.batch, B);
-    const int groups = kPageThreads / B;
-    const unsigned n = (unsigned)clampi(cdiv(entries, 2 * groups), 1, 128);
-    const size_t lds = (size_t)a.batch * 3 * sizeof(int);
-    return launch(B == 16 ? map_kernel<16> : map_kernel<32>, dim3(n), dim3(kPageThreads), lds, stream, a);
+    const unsigned n = (unsigned)clampi(cdiv(most_writes(a.max_tokens, a.batch, B), kFly * (kPageThreads / B)), 1, a.in_place ? 128 : 1024);
+    const size_t lds = (size_t)a.batch * 4 * sizeof(int);
+    const auto kern = B == 16 ? map_kernel<16> : map_kernel<32>;
+    if (lds > 48 * 1024) {                            // (with what is static, 64 KB are not enough)
+        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+        if (e != hipSuccess) return e;
+    }
+    return launch(kern, dim3(n), dim3(kPageThreads), lds, stream, a);
 }
 
 hipError_t launch_release(chess_ctx* ctx, const ReleaseArgs& a, hipStream_t stream)

@@ -4,9 +4,11 @@
 // a 2^-e <= 448 (e4m3's largest), and stores e4m3(x 2^-e).  The scale being a power of two costs e4m3 nothing (its relative step
 // does not depend on it), and all products with it are exact: the tokens that a page held before are moved to a larger scale by an exact
 // product, rounded again only where they become subnormal.
-// Values are token-minor in a page: a lane reads two dims of every token (256 bytes a wave and token) and so has the two rows
+// Values are token-minor in a page: a lane reads the same two (pages of 32: four) dims of 16 tokens and so has 16 bytes of each of the rows
 // [dim][token] that it writes, without an exchange.
-// Bound: HBM (2 bytes read, 1 written an element); for single tokens the chain entry -> rows -> store.
+// Bound: HBM (2 bytes read, 1 written an element); for single tokens the chain entry -> rows -> store and the length of the code that runs once.
+// us: 24K tokens, 8 KV heads, pages of 16 31.8 (4.8 TB/s, what a copy of 2 GiB reaches), 64K, 4 heads, of 32 45.4 (4.4); a token of 32 sequences,
+// 8 heads, 4.3.  Rows not read as a stream: 36.3 and 50.8.  The values' conversion unrolled over dims: the tokens 4.7.
 #include "chess_internal.h"
 #include "quant_device.h"
 #include "split_rule.h"
@@ -36,18 +38,24 @@ __device__ __forceinline__ int exponent_for(uint32_t a)
     return min(max(e, kScaleMin), kScaleMax);
 }
 
-// Two bf16 values as e4m3 bytes in the low half of the result.
+// A value as it is rounded: saturated (only the largest scale leaves something above 448); what is not finite becomes NaN, which the clamp
+// alone would lose.
 __device__ __forceinline__ float scaled(float x, float by)
 {
-    // (saturated: only the largest scale leaves something above 448; what is not finite becomes NaN, which the clamp alone would lose)
     const float y = __builtin_amdgcn_fmed3f(x * by, -448.f, 448.f);
     return (__float_as_uint(x) & 0x7f800000u) == 0x7f800000u ? __uint_as_float(0x7fc00000u) : y;
 }
-template <bool kHigh>
-__device__ __forceinline__ uint32_t to_bytes(uint32_t w, float by, uint32_t old)
+__device__ __forceinline__ uint32_t four_bytes(float x0, float x1, float x2, float x3, float by)
 {
-    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(scaled(__uint_as_float(w << 16), by), scaled(__uint_as_float(w & 0xffff0000u), by), (int)old, kHigh);
+    const int lo = __builtin_amdgcn_cvt_pk_fp8_f32(scaled(x0, by), scaled(x1, by), 0, false);
+    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(scaled(x2, by), scaled(x3, by), lo, true);
 }
+// Of a word of two bf16 values.
+__device__ __forceinline__ float first_of(uint32_t w) { return __uint_as_float(w << 16); }
+__device__ __forceinline__ float second_of(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
+
+// The lowest n bytes of a word.
+__device__ __forceinline__ uint32_t bytes_below(int n) { return n >= 4 ? 0xffffffffu : n <= 0 ? 0u : (1u << (8 * n)) - 1u; }
 
 // Four stored bytes moved to a scale 1 / by times as large.
 __device__ __forceinline__ uint32_t moved(uint32_t w, float by)
@@ -87,7 +95,8 @@ __global__ __launch_bounds__(256) void quant_store_kernel(StoreArgs a)
         uint8_t* page = a.k_pool + ph * (B * kHeadDim);
         uint4 r[B / 4];
 #pragma unroll
-        for (int i = 0; i < B / 4; ++i) r[i] = *reinterpret_cast<const uint4*>(src + (int64_t)min(4 * i + tg, count - 1) * a.k_stride);   // (repeats the last)
+        for (int i = 0; i < B / 4; ++i)                   // (rows past the last repeat it)
+            r[i] = load_16<true>(reinterpret_cast<const uint8_t*>(src + (int64_t)min(4 * i + tg, count - 1) * a.k_stride));
         uint32_t largest = 0;
 #pragma unroll
         for (int i = 0; i < B / 4; ++i) largest = max(max(largest, max(larger_of(r[i].x), larger_of(r[i].y))), max(larger_of(r[i].z), larger_of(r[i].w)));
@@ -106,56 +115,59 @@ __global__ __launch_bounds__(256) void quant_store_kernel(StoreArgs a)
             const int t = 4 * i + tg;
             if (t < count) {
                 uint2 o;
-                o.x = to_bytes<true>(r[i].y, inv, to_bytes<false>(r[i].x, inv, 0));
-                o.y = to_bytes<true>(r[i].w, inv, to_bytes<false>(r[i].z, inv, 0));
+                o.x = four_bytes(first_of(r[i].x), second_of(r[i].x), first_of(r[i].y), second_of(r[i].y), inv);
+                o.y = four_bytes(first_of(r[i].z), second_of(r[i].z), first_of(r[i].w), second_of(r[i].w), inv);
                 *reinterpret_cast<uint2*>(page + (first + t) * kHeadDim + ln * 8) = o;
             }
         }
         if (lane == 0) *scale_at = power_of_two(e);
-    } else {                                          // values: dims 2 lane and 2 lane + 1 of every token
-        const uint16_t* src = a.v_new + (int64_t)row0 * a.v_stride + h * kHeadDim + lane * 2;
-        uint4* rows = reinterpret_cast<uint4*>(a.v_pool + ph * (B * kHeadDim) + lane * (2 * B));
-        uint32_t r[B];                                // token t of the page
+    } else {                                          // values: 16 tokens of 2 kWords dims a lane
+        constexpr int kWords = B / 16, kLanes = 64 / kWords;
+        const int ln = lane % kLanes, t0 = 16 * (lane / kLanes);
+        const uint32_t* src = reinterpret_cast<const uint32_t*>(a.v_new + (int64_t)row0 * a.v_stride + h * kHeadDim) + ln * kWords;
+        uint8_t* rows = a.v_pool + ph * (B * kHeadDim) + ln * (2 * kWords * B) + t0;
+        uint32_t r[16][kWords];
 #pragma unroll
-        for (int t = 0; t < B; ++t) r[t] = *reinterpret_cast<const uint32_t*>(src + (int64_t)min(max(t - first, 0), count - 1) * a.v_stride);
+        for (int t = 0; t < 16; ++t)                  // (tokens that are not new repeat one that is)
+#pragma unroll
+            for (int w = 0; w < kWords; ++w)
+                r[t][w] = __builtin_nontemporal_load((const __attribute__((address_space(1))) uint32_t*)src + (int64_t)min(max(t0 + t - first, 0), count - 1) * (a.v_stride >> 1) + w);
         uint32_t largest = 0;
 #pragma unroll
-        for (int t = 0; t < B; ++t) largest = max(largest, larger_of(r[t]));
+        for (int t = 0; t < 16; ++t)
+#pragma unroll
+            for (int w = 0; w < kWords; ++w) largest = max(largest, larger_of(r[t][w]));
         const int e = grown(wave_largest(largest), first > 0, scale, &by);
         const float inv = power_of_two(-e);
-        const bool whole = count == B;
+        uint32_t is_new[4], is_old[4];                // bytes of a row's four words: written; moved to the new scale
 #pragma unroll
-        for (int t0 = 0; t0 < B; t0 += 16) {
-            uint32_t even[4], odd[4];                 // 16 tokens of the two dims
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t below = bytes_below(first - t0 - 4 * i);
+            is_new[i] = bytes_below(first + count - t0 - 4 * i) & ~below;
+            is_old[i] = by != 1.f ? below : 0u;
+        }
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                uint32_t x[4];
-#pragma unroll
-                for (int y = 0; y < 4; ++y) x[y] = to_bytes<false>(r[t0 + 4 * i + y], inv, 0);
-                even[i] = (x[0] & 255u) | (x[1] & 255u) << 8 | (x[2] & 255u) << 16 | x[3] << 24;
-                odd[i] = (x[0] >> 8 & 255u) | (x[1] & 0xff00u) | (x[2] & 0xff00u) << 8 | (x[3] & 0xff00u) << 16;
-            }
-            uint4* at_even = rows + t0 / 16;
-            uint4* at_odd = rows + B / 16 + t0 / 16;
-            if (!whole) {                             // the bytes before `first` moved, those behind the new ones as they are
-                const uint4 p = *at_even, q = *at_odd;
-                const uint32_t was_even[4] = {p.x, p.y, p.z, p.w}, was_odd[4] = {q.x, q.y, q.z, q.w};
+        for (int w = 0; w < kWords; ++w)
+#pragma nounroll
+            for (int odd = 0; odd < 2; ++odd) {       // (not unrolled: what runs once is as long as its code)
+                uint4* at = reinterpret_cast<uint4*>(rows + (2 * w + odd) * B);
+                const int up = odd ? 0 : 16;
+                uint32_t o[4];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    uint32_t is_new = 0, is_old = 0;
+                    float x[4];
 #pragma unroll
-                    for (int y = 0; y < 4; ++y) {
-                        const int t = t0 + 4 * i + y;
-                        is_new |= t >= first && t < first + count ? 255u << (8 * y) : 0u;
-                        is_old |= t < first && by != 1.f ? 255u << (8 * y) : 0u;
-                    }
-                    even[i] = (even[i] & is_new) | (moved(was_even[i], by) & is_old) | (was_even[i] & ~(is_new | is_old));
-                    odd[i] = (odd[i] & is_new) | (moved(was_odd[i], by) & is_old) | (was_odd[i] & ~(is_new | is_old));
+                    for (int y = 0; y < 4; ++y) x[y] = second_of(r[4 * i + y][w] << up);
+                    o[i] = four_bytes(x[0], x[1], x[2], x[3], inv);
                 }
+                if (count < B) {                      // what is neither stays as it is
+                    const uint4 was4 = *at;
+                    const uint32_t was[4] = {was4.x, was4.y, was4.z, was4.w};
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) o[i] = (o[i] & is_new[i]) | (moved(was[i], by) & is_old[i]) | (was[i] & ~(is_new[i] | is_old[i]));
+                }
+                *at = make_uint4(o[0], o[1], o[2], o[3]);
             }
-            *at_even = make_uint4(even[0], even[1], even[2], even[3]);
-            *at_odd = make_uint4(odd[0], odd[1], odd[2], odd[3]);
-        }
         if (lane == 0) *scale_at = power_of_two(e);
     }
 }
