@@ -343,18 +343,19 @@ int chess_sparse_decode_static(chess_ctx* ctx, const void* q, const void* k_pool
  * ---- Pages handed out on the device ----------------------------------------------------------------------------
  * Block tables and slot maps from request lengths, without the host: a list of free physical pages and its length live in device
  * memory, chess_release_pages puts the pages of ended sequences back, chess_map_tokens deals pages to the tokens of the next step and says
- * where each token goes.  A page belongs to one sequence at a time.  lens_after may be seq_lens and n_left may be n_free (in place).
+ * where each token goes.  A page belongs to one sequence at a time.  lens_after may be seq_lens and n_left may be n_free (in place);
+ * otherwise no output may overlap an input or another output.
  * Both use the workspace (an arrival counter).  CHESS_EINVAL on null or misaligned pointers, sizes outside the configuration, or when the
  * context's device is not the current one; CHESS_ENOTSUP for batch above 4096.
  */
-#define CHESS_MAX_TOKENS (1 << 29)   /* most new tokens of one chess_map_tokens call */
+#define CHESS_MAX_TOKENS (1 << 29)   /* most new tokens of one chess_map_tokens call, most entries of a free list */
 
 /* Entries that the `writes` array of chess_map_tokens must have room for: min(max_tokens, max_tokens / B + 2 batch). */
 int chess_write_rows(const chess_ctx* ctx, int32_t max_tokens, int32_t batch, size_t* rows);
 
 /*
  * done: device int32 [batch].  For every sequence with done[b] != 0, in order: its ceil(seq_lens[b] / B) pages, in logical order, are appended
- * to free_pages [capacity] behind the *n_free entries it holds, and lens_after[b] = 0; the other lengths are copied.  The block table
+ * to free_pages [capacity, at most CHESS_MAX_TOKENS] behind the *n_free entries it holds, and lens_after[b] = 0; the other lengths are copied.  The block table
  * is not changed.  Should the list be too short for a sequence's pages, that sequence and those behind it keep theirs.
  * *n_left = the list's new length.
  */

@@ -331,6 +331,7 @@ class Chess:
         _need(n_free, "n_free", _INT, 1, dev)
         _need(lens_after, "lens_after", _INT, batch, dev)
         _need(n_left, "n_left", _INT, 1, dev)
+        _need(workspace, "workspace", _BYTE, self.workspace_bytes, dev)
         self._check(self.lib.chess_release_pages(self._h, seq_lens.data_ptr(), done.data_ptr(), batch, block_table.data_ptr(), free_pages.data_ptr(),
                                                  free_pages.numel(), n_free.data_ptr(), lens_after.data_ptr(), n_left.data_ptr(),
                                                  workspace.data_ptr(), torch._C._cuda_getCurrentRawStream(dev)))
@@ -350,6 +351,7 @@ class Chess:
         _need(n_free, "n_free", _INT, 1, dev)
         _need(lens_after, "lens_after", _INT, batch, dev)
         _need(n_left, "n_left", _INT, 1, dev)
+        _need(workspace, "workspace", _BYTE, self.workspace_bytes, dev)
         _need(token_start, "token_start", _INT, batch + 1, dev)
         if slots is not None:
             _need(slots, "slots", _LONG, max_tokens, dev)
@@ -398,7 +400,7 @@ class Chess:
         self._check(self.lib.chess_quant_summarize(self._h, k_pool.data_ptr(), scales.data_ptr(), block_table.data_ptr(), seq_lens.data_ptr(), batch,
                                                    _ptr(from_page), recent_pages, summaries.data_ptr(), torch._C._cuda_getCurrentRawStream(dev)))
 
-    def _need_attention(self, q, k_pool, v_pool, scales, block_table, seq_lens, out, batch, dev):
+    def _need_attention(self, q, k_pool, v_pool, scales, block_table, seq_lens, out, workspace, batch, dev):
         c = self.cfg
         values = batch * c.n_q_heads * c.head_dim
         _need(q, "q", _BF16, values, dev)
@@ -408,10 +410,11 @@ class Chess:
         _need(block_table, "block_table", _INT, batch * c.max_pages_per_seq, dev)
         _need(seq_lens, "seq_lens", _INT, batch, dev)
         _need(out, "out", _FLOAT, values, dev)
+        _need(workspace, "workspace", _BYTE, self.workspace_bytes, dev)
 
     def quant_sparse_decode(self, q, k_pool, v_pool, scales, block_table, seq_lens, page_ids, n_selected, out, workspace):
         batch, dev = seq_lens.shape[0], self.device
-        self._need_attention(q, k_pool, v_pool, scales, block_table, seq_lens, out, batch, dev)
+        self._need_attention(q, k_pool, v_pool, scales, block_table, seq_lens, out, workspace, batch, dev)
         _need(page_ids, "page_ids", _INT, batch * self.cfg.n_kv_heads * self.cfg.max_selected_pages, dev)
         _need(n_selected, "n_selected", _INT, batch * self.cfg.n_kv_heads, dev)
         self._check(self.lib.chess_quant_sparse_decode(self._h, q.data_ptr(), k_pool.data_ptr(), v_pool.data_ptr(), scales.data_ptr(),
@@ -420,7 +423,7 @@ class Chess:
 
     def quant_dense_decode(self, q, k_pool, v_pool, scales, block_table, seq_lens, out, workspace):
         batch, dev = seq_lens.shape[0], self.device
-        self._need_attention(q, k_pool, v_pool, scales, block_table, seq_lens, out, batch, dev)
+        self._need_attention(q, k_pool, v_pool, scales, block_table, seq_lens, out, workspace, batch, dev)
         self._check(self.lib.chess_quant_dense_decode(self._h, q.data_ptr(), k_pool.data_ptr(), v_pool.data_ptr(), scales.data_ptr(),
                                                       block_table.data_ptr(), seq_lens.data_ptr(), batch, out.data_ptr(), workspace.data_ptr(),
                                                       torch._C._cuda_getCurrentRawStream(dev)))

@@ -754,7 +754,7 @@ int chess_release_pages(chess_ctx* ctx, const int32_t* seq_lens, const int32_t* 
                         void* stream)
 {
     if (!ctx || !seq_lens || !done || !block_table || !free_pages || !n_free || !lens_after || !n_left || !workspace) return CHESS_EINVAL;
-    if (batch < 1 || batch > ctx->cfg.max_batch || capacity < 1 || misaligned({workspace}, 15) || !on_device(ctx)) return CHESS_EINVAL;
+    if (batch < 1 || batch > ctx->cfg.max_batch || capacity < 1 || capacity > CHESS_MAX_TOKENS || misaligned({workspace}, 15) || !on_device(ctx)) return CHESS_EINVAL;
     if (batch > chess::kPageMost) return CHESS_ENOTSUP;
     const chess::ReleaseArgs a{seq_lens, done, block_table, free_pages, n_free, lens_after, n_left,
                                reinterpret_cast<int32_t*>(static_cast<char*>(workspace) + ctx->ws_cnt_off), batch, capacity, ctx->geom.max_pages,

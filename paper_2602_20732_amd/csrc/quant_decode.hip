@@ -16,6 +16,9 @@
 namespace chess {
 
 constexpr int kQuantTokens = 64;     // of a tile
+// The weighted sums and the sums of weights are both kept in units of 2^32: weights reach 1 and there are fewer than 2^31 of them, so that no sum of
+// finite values leaves fp32 before it is divided (values reach 448 2^119; the smallest, 2^-73, are normal numbers either way).
+constexpr float kSumUnit = 0x1p-32f;
 typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
 
 // Eight stored bytes, times a power of two, as a MFMA operand.
@@ -130,7 +133,7 @@ struct QuantAcc {
                 s[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(operand_of(w.z, w.w, 1.f), qop[2 * half + 1], s[c], 0, 0, 0);
             }
         }
-        const float by = tl.scale.x * scale_log2;
+        const float by = tl.scale.x * scale_log2, v_scale = tl.scale.y * kSumUnit;
         float x[16];
 #pragma unroll
         for (int e = 0; e < 16; ++e) x[e] = e < tl.nt ? s[e >> 2][e & 3] * by : -INFINITY;
@@ -172,7 +175,7 @@ struct QuantAcc {
         for (int blk = 0; blk < 8; ++blk) {
             f32x4 acc = o[blk] * alpha;
             const uint4 w = tl.v[blk];
-            const bf16x8 v0 = operand_of(w.x, w.y, tl.scale.y), v1 = operand_of(w.z, w.w, tl.scale.y);
+            const bf16x8 v0 = operand_of(w.x, w.y, v_scale), v1 = operand_of(w.z, w.w, v_scale);
 #pragma unroll
             for (int part = 0; part < 3; ++part) {
                 acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v0, p[0][part], acc, 0, 0, 0);
@@ -274,6 +277,7 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(kList &
     }
     acc.l_run += __shfl_xor(acc.l_run, 16);
     acc.l_run += __shfl_xor(acc.l_run, 32);
+    acc.l_run *= kSumUnit;
 
     float* out_rows = a.out + ((size_t)b * H * G + (size_t)h * G) * kHeadDim;
     if (!combine_waves<NW>(acc.o, acc.m_run, acc.l_run, lds, G, ns, split, part0, out_rows, a.ws_acc, a.ws_ml)) return;

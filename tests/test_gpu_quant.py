@@ -132,10 +132,10 @@ def test_nothing_to_store_and_refusals():
     q, table, lens = torch.zeros((2, 4, D), dtype=torch.bfloat16, device="cuda"), ints(np.zeros((2, 4))), ints([3, 4])
     lib.quant_dense_decode(q, k, v, scales, table, lens, out, ws)
     for bad in (dict(q=q.float()), dict(q=q[:1]), dict(k=k[:2]), dict(v=v.transpose(2, 3)), dict(scales=scales[:, :1]), dict(scales=scales.half()),
-                dict(table=table[:, :3]), dict(lens=ints([1, 2, 3])), dict(out=out[:, ::2])):
-        a = dict(q=q, k=k, v=v, scales=scales, table=table, lens=lens, out=out) | bad
+                dict(table=table[:, :3]), dict(lens=ints([1, 2, 3])), dict(out=out[:, ::2]), dict(ws=ws[:-256])):
+        a = dict(q=q, k=k, v=v, scales=scales, table=table, lens=lens, out=out, ws=ws) | bad
         with pytest.raises(pk.ChessError):
-            lib.quant_dense_decode(a["q"], a["k"], a["v"], a["scales"], a["table"], a["lens"], a["out"], ws)
+            lib.quant_dense_decode(a["q"], a["k"], a["v"], a["scales"], a["table"], a["lens"], a["out"], a["ws"])
     with pytest.raises(pk.ChessError, match="page_ids"):
         lib.quant_sparse_decode(q, k, v, scales, table, lens, ints(np.zeros((2, 2, 3))), ints(np.zeros((2, 2))), out, ws)
     with pytest.raises(pk.ChessError):                           # both kinds of catch-up at once
@@ -162,7 +162,7 @@ def dealt(rng, lens, pages, B):
     return table, sum(held) + 2
 
 
-def check_attention(rng, lens, Hq, H, B, lists=None, pages=None, splits=(0, 4), scale_spread=True, sm_scale=0.0, q_size=1.0, room=None):
+def check_attention(rng, lens, Hq, H, B, lists=None, pages=None, splits=(0, 4), scale_spread=True, sm_scale=0.0, q_size=1.0, room=None, scales_of=None):
     """Against fp64 over the listed pages (lists[b][h]) or every page; the bytes behind the last token stay as they fell, NaN among them."""
     G, batch = Hq // H, len(lens)
     pages = pages or max(1, max(-(-n // B) for n in lens))
@@ -170,6 +170,8 @@ def check_attention(rng, lens, Hq, H, B, lists=None, pages=None, splits=(0, 4), 
     cache = Cache(rng, n_phys, H, B)
     if not scale_spread:
         cache.scales[:] = 2.0 ** -6
+    if scales_of is not None:
+        scales_of(cache.scales)
     for b, n in enumerate(lens):                                 # the tokens that exist are finite
         for p in range(-(-n // B)):
             m = min(B, n - p * B)
@@ -222,6 +224,26 @@ def test_every_page_of_short_and_odd_lengths(B, Hq, H):
 @pytest.mark.parametrize("n", [1, 40, 64, 700, 3001])
 def test_one_sequence(B, n):
     check_attention(np.random.default_rng(n), [n], 8, 2, B)
+
+
+@pytest.mark.parametrize("B", [16, 32])
+@pytest.mark.parametrize("Hq,H", [(1, 1), (7, 1), (10, 2), (16, 1), (32, 2)])
+def test_one_sequence_of_any_group(B, Hq, H):
+    """Eight waves a workgroup; with sixteen heads their exchange takes more than 64 KB."""
+    rng = np.random.default_rng(Hq)
+    check_attention(rng, [1500], Hq, H, B)
+    check_attention(rng, [1500], Hq, H, B, pages=330000 // B)
+    check_attention(rng, [1500], Hq, H, B, lists=[[list(range(0, -(-1500 // B), 2)) for _ in range(H)]], splits=(2, 8))
+
+
+@pytest.mark.parametrize("B", [16, 32])
+@pytest.mark.parametrize("e", [-64, 119])
+def test_scales_at_either_end(B, e):
+    """Values of the largest and the smallest scale; keys of the smallest."""
+    rng = np.random.default_rng(33)
+    check_attention(rng, [200, 65, 3], 8, 2, B, scales_of=lambda s: s.__setitem__((slice(None), slice(None), 1), 2.0 ** e))
+    if e < 0:
+        check_attention(rng, [200, 65, 3], 8, 2, B, q_size=2.0 ** 60, scales_of=lambda s: s.__setitem__((slice(None), slice(None), 0), 2.0 ** e))
 
 
 @pytest.mark.parametrize("B", [16, 32])
