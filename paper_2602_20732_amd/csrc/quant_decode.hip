@@ -296,7 +296,7 @@ hipError_t launch_quant_decode(chess_ctx* ctx, const uint16_t* q, const uint8_t*
                                int n_splits, int waves, int n_slots, float* out, float* ws_acc, float* ws_ml, int32_t* arrivals, hipStream_t stream)
 {
     const Geom& g = ctx->geom;
-    const bool dealt = n_slots > 0;                   // (every page, four waves: see choose_splits)
+    const bool dealt = n_slots > 0;                   // (every page: see choose_quant_splits)
     const dim3 grid = dealt ? dim3(g.n_kv_heads, n_slots) : dim3(n_splits, g.n_kv_heads, batch), block(64 * waves);
     const size_t lds = quant_lds_bytes(waves, g.group);
     const int by_page = g.page_size == 16 ? 0 : 1;
@@ -314,10 +314,13 @@ hipError_t launch_quant_decode(chess_ctx* ctx, const uint16_t* q, const uint8_t*
     static const QuantKernel lists_streamed[2] = {quant_decode_kernel<16, 4, true, false, true>, quant_decode_kernel<32, 4, true, false, true>};
     static const QuantKernel streamed[2][2] = {{quant_decode_kernel<16, 4, false, false, true>, quant_decode_kernel<32, 4, false, false, true>},
                                                {quant_decode_kernel<16, 8, false, false, true>, quant_decode_kernel<32, 8, false, false, true>}};
-    static const QuantKernel by_length[2][2] = {{quant_decode_kernel<16, 4, false, true>, quant_decode_kernel<32, 4, false, true>},
-                                                {quant_decode_kernel<16, 4, false, true, true>, quant_decode_kernel<32, 4, false, true, true>}};
+    // [streamed][four / eight waves]
+    static const QuantKernel by_length[2][2][2] = {{{quant_decode_kernel<16, 4, false, true>, quant_decode_kernel<32, 4, false, true>},
+                                                    {quant_decode_kernel<16, 8, false, true>, quant_decode_kernel<32, 8, false, true>}},
+                                                   {{quant_decode_kernel<16, 4, false, true, true>, quant_decode_kernel<32, 4, false, true, true>},
+                                                    {quant_decode_kernel<16, 8, false, true, true>, quant_decode_kernel<32, 8, false, true, true>}}};
     const int by_waves = waves == 8 ? 2 : waves == 4 ? 1 : 0;
-    const QuantKernel kern = dealt ? by_length[once][by_page] : page_ids ? (once && waves == 4 ? lists_streamed[by_page] : lists[by_waves][by_page])
+    const QuantKernel kern = dealt ? by_length[once][waves == 8][by_page] : page_ids ? (once && waves == 4 ? lists_streamed[by_page] : lists[by_waves][by_page])
                                    : once && waves > 1 ? streamed[waves == 8][by_page] : every[by_waves][by_page];
     if (lds > 64 * 1024) {
         const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);

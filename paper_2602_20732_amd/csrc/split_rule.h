@@ -115,14 +115,19 @@ inline SplitShape choose_splits(const SplitLimits& c, int batch, int64_t max_lis
 //   2048 tokens, 8 KV heads, G = 4       8 splits  6.9   16  7.3   24  8.3   32  8.7         32768   16 splits 19.0   24 17.6   32 17.3
 //   8192                                 8        12.2   16  9.7   24 10.3   32 10.1        131072   16        67.4   24 54.5   32 54.6
 //   16384, 4 KV heads, G = 7            16        13.5   32 12.2   48 13.2   64 14.2
+// Several sequences: dealt by length (share_slots), as such workgroups too where that leaves five of them to a sequence, so that their rounding costs
+// little; otherwise as four-wave ones, twice as many.  us, four / eight waves, sequences and workgroups a sequence of the latter: 2 of 25K and 192K
+// tokens, 4 KV heads, G = 7 (32) 62.5 / 50.5; 4 of 20-131K, 8 heads, G = 4 (8) 117.0 / 116.6; 4 of 5-21K (8) 25.2 / 23.5; 10 of 45-48K, 4 heads, G = 7
+// (6.4) 92.2 / 90.0; 6 of 6-7K, 8 heads (5.3) 20.4 / 19.8; 13 of 7-14K (2.5) 52 / 56; 16 of 8-64K (2) 218 / 243.
 inline SplitShape choose_quant_splits(const SplitLimits& c, int batch, int64_t max_list_pages, bool listed)
 {
     if (c.force_splits > 0) return {c.force_splits, !listed && c.force_waves == 4 ? 8 : c.force_waves, 0};
-    if (listed || batch > 1) return choose_splits(c, batch, max_list_pages, listed);
+    const int64_t slots = c.n_cu / c.n_kv_heads;      // (with the partials' rows, four times as many, there is always room for them)
+    if (listed || (batch > 1 && slots < 5LL * batch)) return choose_splits(c, batch, max_list_pages, listed);
     const int64_t tiles = std::max<int64_t>(1, cdiv(max_list_pages, c.tile_pages));
     const int64_t balanced = (int64_t)std::sqrt((c.group > 4 ? 16.0 : 8.0) * (double)tiles / c.group);
-    const int64_t most = std::min<int64_t>({c.n_cu / c.n_kv_heads, c.max_splits, 1024 / c.group, partial_rows(c.n_cu, c.n_kv_heads) / c.n_kv_heads, tiles});
-    return {(int)clampi(balanced, 1, std::max<int64_t>(most, 1)), 8, 0};
+    const int64_t most = std::min<int64_t>({slots, c.max_splits, 1024 / c.group, tiles});
+    return {(int)clampi(balanced, 1, std::max<int64_t>(most, 1)), 8, batch > 1 ? (int)slots : 0};
 }
 
 }  // namespace chess

@@ -23,7 +23,7 @@ int main()
                                     if (ns < 1 || ns > 256 || ns * group > 1024) bad = "split count";
                                     else if ((ns > 1 || s.n_slots > 0) && used > partial_rows(n_cu, pairs)) bad = "partials outgrow the workspace";
                                     else if (s.waves != 4 && s.waves != 8) bad = "waves";
-                                    else if (s.n_slots > 0 && (listed || batch < 2 || s.waves != 4 || used > blocks * n_cu)) bad = "dealt slots";
+                                    else if (s.n_slots > 0 && (listed || batch < 2 || s.n_slots < batch || used > (s.waves == 8 ? 1 : blocks) * n_cu)) bad = "dealt slots";
                                     else if (!listed && batch == 1 && (s.waves != 8 || s.n_slots != 0 || ns > tiles || (ns > 1 && pairs * ns > n_cu))) bad = "one sequence";
                                     if (bad != nullptr) {
                                         std::printf("%s: cu %d blocks %d heads %d G %d tile pages %d batch %d pages %lld listed %d -> ns %d waves %d slots %d\n",

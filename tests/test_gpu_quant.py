@@ -237,6 +237,16 @@ def test_one_sequence_of_any_group(B, Hq, H):
 
 
 @pytest.mark.parametrize("B", [16, 32])
+@pytest.mark.parametrize("Hq,H", [(1, 1), (14, 2), (16, 1)])
+def test_batches_dealt_to_four_and_to_eight_waves(B, Hq, H):
+    """Few sequences (eight waves a workgroup) and many (four), of equal and of very different lengths."""
+    rng = np.random.default_rng(Hq + 50)
+    for lens in ([3000, 5], [700, 700, 700], [0, 1, 2222], rng.integers(0, 400, 40).tolist(), [130] * 60):
+        check_attention(rng, lens, Hq, H, B)
+    check_attention(rng, [2000, 0, 65], Hq, H, B, pages=330000 // B)
+
+
+@pytest.mark.parametrize("B", [16, 32])
 @pytest.mark.parametrize("e", [-64, 119])
 def test_scales_at_either_end(B, e):
     """Values of the largest and the smallest scale; keys of the smallest."""
