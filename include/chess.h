@@ -410,7 +410,9 @@ int chess_quant_summarize(chess_ctx* ctx, const void* k_pool, const float* scale
                           int32_t batch, const int32_t* from_page, int32_t recent_pages, void* summaries, void* stream);
 
 /* chess_sparse_decode and chess_dense_decode on the values that 8-bit pages stand for: bf16 queries, fp32 accumulation, fp32 out; no other
- * rounding to fewer bits.  Arguments otherwise as for those. */
+ * rounding to fewer bits.  Arguments otherwise as for those.  In a batch, attention over every page deals the tokens of all its sequences to the
+ * workgroups, so the order in which a sequence's are summed, and with it the last bits of its output, depends on the lengths of its batch mates; the
+ * same batch gives the same bits on every call. */
 int chess_quant_sparse_decode(chess_ctx* ctx, const void* q, const void* k_pool, const void* v_pool, const float* scales,
                               const int32_t* block_table, const int32_t* seq_lens, const int32_t* page_ids, const int32_t* n_selected,
                               int32_t batch, float* out, void* workspace, void* stream);

@@ -200,6 +200,48 @@ struct QuantArgs {
 using QuantKernel = void (*)(uint64_t, uint64_t, uint64_t, uint64_t, uint64_t, int, int, int, int, QuantArgs);
 using QuantLines = ArgLinesOf<QuantKernel, QuantArgs>;
 
+// Attention over tiles t0, t0 + stride, ... < t_end of one row by one wave.
+template <int B, bool kList, bool kOnce>
+struct QuantWalk {
+    int2 raw_cur, raw_nxt, raw_nn;
+    QuantRef rc, rn;
+    // what does not wait for lengths
+    __device__ __forceinline__ void ask(int t, int stride, const int32_t* ids, int max_sel, const int32_t* bt_row, int max_pages, int m16, int grp)
+    {
+        if constexpr (kList) {
+            raw_cur = quant_ids<B>(t, ids, max_sel, m16, grp);
+            raw_nxt = quant_ids<B>(t + stride, ids, max_sel, m16, grp);
+        } else {
+            rc = quant_pages<B, false>(t, raw_cur, bt_row, 0, max_pages, m16, grp);
+            rn = quant_pages<B, false>(t + stride, raw_nxt, bt_row, 0, max_pages, m16, grp);
+        }
+    }
+    __device__ __forceinline__ void run(QuantAcc& acc, int t, int t_end, int stride, int n_pages, int L, int P, const int32_t* ids, int max_sel,
+                                        const int32_t* bt_row, int max_pages, const QuantArgs& a, int H, int h, int m16, int grp)
+    {
+        if (t < t_end) {
+            // block-table entries run one tile ahead of the rows, a list's page numbers one tile ahead of those
+            if constexpr (kList) {
+                rc = quant_pages<B, true>(t, raw_cur, bt_row, P, max_pages, m16, grp);
+                rn = quant_pages<B, true>(t + stride, raw_nxt, bt_row, P, max_pages, m16, grp);
+                raw_nn = quant_ids<B>(t + 2 * stride, ids, max_sel, m16, grp);
+            }
+            QuantTile<B> tl;
+            for (; t < t_end; t += stride) {
+                quant_rows<B, kList, kOnce>(tl, rc, t, n_pages, L, P, a.k_pool, a.v_pool, a.scales, H, h, m16, grp);
+                const QuantRef rnn = quant_pages<B, kList>(t + 2 * stride, raw_nn, bt_row, P, max_pages, m16, grp);
+                if constexpr (kList) raw_nn = quant_ids<B>(t + 3 * stride, ids, max_sel, m16, grp);
+                acc.process(tl, a.scale_log2);
+                rc = rn;
+                rn = rnn;
+            }
+        }
+        acc.l_run += __shfl_xor(acc.l_run, 16);
+        acc.l_run += __shfl_xor(acc.l_run, 32);
+        acc.l_run *= kSumUnit;
+    }
+};
+
 // grid: (n_splits, H_kv, batch), or dealt by length (H_kv, n_slots).  heads: KV heads << 8 | group.
 template <int B, int NW, bool kList, bool kDealt = false, bool kOnce = false>
 __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(kList && NW == 4 ? 3 : 2))) void quant_decode_kernel(
@@ -233,19 +275,11 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(kList &
     const int32_t* ids = kList ? device_pointer<const int32_t>(page_ids_at) + row * max_sel : nullptr;
     const int32_t* bt_row = device_pointer<const int32_t>(block_table_at) + (size_t)b * max_pages;
     // tiles are dealt round-robin over splits and waves: the first of a wave is known before the list's length is
-    const int stride = ns * NW;
-    int t = split + ns * wave;
-    int2 raw_cur, raw_nxt, raw_nn;
-    QuantRef rc, rn;
+    const int stride = ns * NW, t = split + ns * wave;
     if constexpr (!kDealt) L_raw = load_by_lane(seq_lens + b);
     int n_raw = kList ? load_by_lane(device_pointer<const int32_t>(n_selected_at) + row) : 0;
-    if constexpr (kList) {
-        raw_cur = quant_ids<B>(t, ids, max_sel, m16, grp);
-        raw_nxt = quant_ids<B>(t + stride, ids, max_sel, m16, grp);
-    } else {
-        rc = quant_pages<B, false>(t, raw_cur, bt_row, 0, max_pages, m16, grp);
-        rn = quant_pages<B, false>(t + stride, raw_nxt, bt_row, 0, max_pages, m16, grp);
-    }
+    QuantWalk<B, kList, kOnce> walk;
+    walk.ask(t, stride, ids, max_sel, bt_row, max_pages, m16, grp);
     QuantAcc acc;
     acc.request(device_pointer<const uint16_t>(q_at) + ((size_t)b * H * G + (size_t)h * G) * kHeadDim, G, m16, grp);
     requested_by_here();
@@ -254,30 +288,10 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(kList &
     const int L = min(max(L_raw, 0), max_pages * B);
     const int P = (L + B - 1) / B;
     const int n_pages = P == 0 ? 0 : (kList ? min(max(n_raw, 0), max_sel) : P);
-    const int n_tiles = (n_pages + PPT - 1) / PPT;
 
     lines.hold();
     acc.start(G, m16);
-    if (t < n_tiles) {
-        // block-table entries run one tile ahead of the rows, a list's page numbers one tile ahead of those
-        if constexpr (kList) {
-            rc = quant_pages<B, true>(t, raw_cur, bt_row, P, max_pages, m16, grp);
-            rn = quant_pages<B, true>(t + stride, raw_nxt, bt_row, P, max_pages, m16, grp);
-            raw_nn = quant_ids<B>(t + 2 * stride, ids, max_sel, m16, grp);
-        }
-        QuantTile<B> tl;
-        for (; t < n_tiles; t += stride) {
-            quant_rows<B, kList, kOnce>(tl, rc, t, n_pages, L, P, a.k_pool, a.v_pool, a.scales, H, h, m16, grp);
-            const QuantRef rnn = quant_pages<B, kList>(t + 2 * stride, raw_nn, bt_row, P, max_pages, m16, grp);
-            if constexpr (kList) raw_nn = quant_ids<B>(t + 3 * stride, ids, max_sel, m16, grp);
-            acc.process(tl, a.scale_log2);
-            rc = rn;
-            rn = rnn;
-        }
-    }
-    acc.l_run += __shfl_xor(acc.l_run, 16);
-    acc.l_run += __shfl_xor(acc.l_run, 32);
-    acc.l_run *= kSumUnit;
+    walk.run(acc, t, (n_pages + PPT - 1) / PPT, stride, n_pages, L, P, ids, max_sel, bt_row, max_pages, a, H, h, m16, grp);
 
     float* out_rows = a.out + ((size_t)b * H * G + (size_t)h * G) * kHeadDim;
     if (!combine_waves<NW>(acc.o, acc.m_run, acc.l_run, lds, G, ns, split, part0, out_rows, a.ws_acc, a.ws_ml)) return;
@@ -289,6 +303,109 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(kList &
     merge_splits<NW, kDealt ? kMergeDealt : kMergePlain>(G, ns, part0, out_rows, a.ws_acc, a.ws_ml);
 }
 
+// The tiles of a batch in a line, sequence after sequence (one without tokens counts for a tile), cut into shares that differ by at most one tile.
+// Every wave works it out from the lengths in device memory, 64 sequences a round.
+struct TileLine {
+    int q, r;                        // a share is q tiles, the first r of them one more
+    int b0;                          // the 64 sequences a lane has one of
+    int len, tiles, upto;            // of the lane's sequence: tokens, tiles, the line's tiles up to its end
+
+    template <int B>
+    __device__ __forceinline__ void read(const int32_t* seq_lens, int batch, int max_pages, int lane)
+    {
+        len = min(max(seq_lens[min(b0 + lane, batch - 1)], 0), max_pages * B);
+        tiles = b0 + lane < batch ? max((len + kQuantTokens - 1) / kQuantTokens, 1) : 0;
+    }
+    __device__ __forceinline__ int begin_of(int slot) const { return slot * q + min(slot, r); }
+    __device__ __forceinline__ int slot_of(int tile) const
+    {
+        const int wide = r * (q + 1);
+        return tile < wide ? tile / (q + 1) : r + (tile - wide) / q;
+    }
+};
+
+// Attention over every page of a batch: grid (H_kv, slots), each workgroup a share of its KV head's tiles, which may end one sequence, hold several
+// whole ones and begin another.  A sequence's parts are one a slot, in slot order, so the partials of sequence b start at the first of its slots
+// plus b (its last slot may be the next one's first).
+template <int B, int NW, bool kOnce>
+__global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2))) void quant_line_kernel(
+    uint64_t seq_lens_at, uint64_t block_table_at, uint64_t q_at, uint64_t, uint64_t, int heads, int, int max_pages, int batch, QuantArgs a)
+{
+    extern __shared__ float lds_f[];                  // DecodeLds<NW>::floats(G)
+    __shared__ int lds_last;
+    const int G = heads & 255, H = heads >> 8, h = blockIdx.x, slot = blockIdx.y, slots = gridDim.y;
+    QuantLines lines;
+    lines.ask();
+    DecodeLds<NW> lds(lds_f, G);
+    const int32_t* seq_lens = device_pointer<const int32_t>(seq_lens_at);
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int m16 = lane & 15, grp = lane >> 4;
+
+    TileLine line;
+    int total = 0;
+    if (batch > 64) {
+#pragma unroll 4
+        for (line.b0 = 0; line.b0 < batch; line.b0 += 64) {
+            line.read<B>(seq_lens, batch, max_pages, lane);
+            total += line.tiles;
+        }
+    } else {
+        line.b0 = 0;
+        line.read<B>(seq_lens, batch, max_pages, lane);
+        total = line.tiles;
+    }
+    line.upto = lanes_upto(total);
+    total = lane_of(line.upto, 63);
+    // (a share has a tile for every wave at least)
+    const int used = min((int)gridDim.y, (total + NW - 1) / NW);
+    if (slot >= used) return;
+    line.q = total / used;
+    line.r = total - line.q * used;
+    int at = line.begin_of(slot);
+    const int end = line.begin_of(slot + 1);
+    if (at >= end) return;
+    if (batch > 64) {                                 // the 64 sequences the share begins in
+        total = 0;
+        for (line.b0 = 0;; line.b0 += 64) {
+            line.read<B>(seq_lens, batch, max_pages, lane);
+            line.upto = total + lanes_upto(line.tiles);
+            total = lane_of(line.upto, 63);
+            if (total > at) break;
+        }
+    } else line.b0 = 0;
+    lines.hold();
+    int i = __builtin_ctzll(__ballot(line.upto > at));
+    for (;;) {
+        const int b = line.b0 + i, L = lane_of(line.len, i), tiles = lane_of(line.tiles, i), upto = lane_of(line.upto, i), begin = upto - tiles;
+        const int t0 = at - begin, t_end = min(end, upto) - begin;
+        const int first = t0 == 0 && t_end == tiles ? slot : line.slot_of(begin), n_splits = t0 == 0 && t_end == tiles ? 1 : line.slot_of(upto - 1) - first + 1;
+        const int32_t* bt_row = device_pointer<const int32_t>(block_table_at) + (size_t)b * max_pages;
+        const int P = (L + B - 1) / B;
+        QuantWalk<B, false, kOnce> walk;
+        QuantAcc acc;
+        walk.ask(t0 + wave, NW, nullptr, 0, bt_row, max_pages, m16, grp);
+        acc.request(device_pointer<const uint16_t>(q_at) + ((size_t)b * H * G + (size_t)h * G) * kHeadDim, G, m16, grp);
+        acc.start(G, m16);
+        walk.run(acc, t0 + wave, min(t_end, P == 0 ? 0 : t_end), NW, P, L, P, nullptr, 0, bt_row, max_pages, a, H, h, m16, grp);
+
+        float* out_rows = a.out + ((size_t)b * H * G + (size_t)h * G) * kHeadDim;
+        const size_t part0 = own_reg((unsigned)(h * (slots + batch) + first + b));
+        if (combine_waves<NW>(acc.o, acc.m_run, acc.l_run, lds, G, n_splits, slot - first, part0, out_rows, a.ws_acc, a.ws_ml) &&
+            arrive_last(a.arrivals + ((size_t)b * H + h) * kArrivalStride, n_splits, &lds_last))
+            merge_splits<NW, kMergeDealt>(G, n_splits, part0, out_rows, a.ws_acc, a.ws_ml);
+        at = begin + t_end;
+        if (at >= end) return;
+        __syncthreads();                              // the next sequence's waves meet in the same LDS
+        if (++i == 64) {
+            i = 0;
+            line.b0 += 64;
+            const int before = upto;
+            line.read<B>(seq_lens, batch, max_pages, lane);
+            line.upto = before + lanes_upto(line.tiles);
+        }
+    }
+}
+
 static size_t quant_lds_bytes(int waves, int group) { return (size_t)(waves * group * kHeadDim + 2 * waves * group) * sizeof(float); }
 
 hipError_t launch_quant_decode(chess_ctx* ctx, const uint16_t* q, const uint8_t* k_pool, const uint8_t* v_pool, const float* scales,
@@ -296,55 +413,42 @@ hipError_t launch_quant_decode(chess_ctx* ctx, const uint16_t* q, const uint8_t*
                                int n_splits, int waves, int n_slots, float* out, float* ws_acc, float* ws_ml, int32_t* arrivals, hipStream_t stream)
 {
     const Geom& g = ctx->geom;
-    const bool dealt = n_slots > 0;                   // (every page: see choose_quant_splits)
+    const bool dealt = n_slots > 0, line = dealt && waves == 4;   // (every page of a batch: see choose_quant_splits)
     const dim3 grid = dealt ? dim3(g.n_kv_heads, n_slots) : dim3(n_splits, g.n_kv_heads, batch), block(64 * waves);
     const size_t lds = quant_lds_bytes(waves, g.group);
-    const int by_page = g.page_size == 16 ? 0 : 1;
-    // Pages as a stream where they are more than stays in the 256 MB behind the L2s from one step to the next (kOnce): us, plain / so, one
-    // sequence of 32768 tokens, 8 KV heads (67 MB) 17.3 / 18.9, 65536 (134 MB) 30.0 / 28.6, 131072 54.6 / 51.9, 262139 of 4 heads, pages of 32,
-    // 56.8 / 53.4; 16 sequences of 8-64K 224 / 218; lists, 96 of 60 pages of 16, 8 heads (188 MB) 40.4 / 37.7, 32 of 108 (113 MB) 23.4 / 24.1.
+    const int by_page = g.page_size == 16 ? 0 : 1, wide = waves == 8;
+    // Pages as a stream where they are more than stays in the 256 MB behind the L2s from one step to the next: us, plain / so, one sequence of 32768
+    // tokens, 8 KV heads (67 MB) 17.3 / 18.9, 65536 (134 MB) 30.0 / 28.6, 131072 54.6 / 51.9, 262139 of 4 heads, pages of 32, 56.8 / 53.4; 16 sequences
+    // of 8-64K 224 / 218; lists, 96 of 60 pages of 16, 8 heads (188 MB) 40.4 / 37.7, 32 of 108 (113 MB; eight waves) 23.4 / 24.1.
     const bool once = (int64_t)batch * (page_ids ? g.max_sel : g.max_pages) * g.page_size * g.n_kv_heads * 2 * kHeadDim > 128LL << 20;
-    // [page size 16 / 32], lists by one, four or eight waves; every page by one, four (short rows, more of them than compute units) or eight; dealt
-    static const QuantKernel lists[3][2] = {{quant_decode_kernel<16, 1, true>, quant_decode_kernel<32, 1, true>},
-                                            {quant_decode_kernel<16, 4, true>, quant_decode_kernel<32, 4, true>},
+    // [page size 16 / 32]
+    static const QuantKernel lists[2][2] = {{quant_decode_kernel<16, 4, true>, quant_decode_kernel<32, 4, true>},
                                             {quant_decode_kernel<16, 8, true>, quant_decode_kernel<32, 8, true>}};
-    static const QuantKernel every[3][2] = {{quant_decode_kernel<16, 1, false>, quant_decode_kernel<32, 1, false>},
-                                            {quant_decode_kernel<16, 4, false>, quant_decode_kernel<32, 4, false>},
-                                            {quant_decode_kernel<16, 8, false>, quant_decode_kernel<32, 8, false>}};
     static const QuantKernel lists_streamed[2] = {quant_decode_kernel<16, 4, true, false, true>, quant_decode_kernel<32, 4, true, false, true>};
-    static const QuantKernel streamed[2][2] = {{quant_decode_kernel<16, 4, false, false, true>, quant_decode_kernel<32, 4, false, false, true>},
-                                               {quant_decode_kernel<16, 8, false, false, true>, quant_decode_kernel<32, 8, false, false, true>}};
-    // [streamed][four / eight waves]
-    static const QuantKernel by_length[2][2][2] = {{{quant_decode_kernel<16, 4, false, true>, quant_decode_kernel<32, 4, false, true>},
-                                                    {quant_decode_kernel<16, 8, false, true>, quant_decode_kernel<32, 8, false, true>}},
-                                                   {{quant_decode_kernel<16, 4, false, true, true>, quant_decode_kernel<32, 4, false, true, true>},
-                                                    {quant_decode_kernel<16, 8, false, true, true>, quant_decode_kernel<32, 8, false, true, true>}}};
-    const int by_waves = waves == 8 ? 2 : waves == 4 ? 1 : 0;
-    const QuantKernel kern = dealt ? by_length[once][waves == 8][by_page] : page_ids ? (once && waves == 4 ? lists_streamed[by_page] : lists[by_waves][by_page])
-                                   : once && waves > 1 ? streamed[waves == 8][by_page] : every[by_waves][by_page];
+    static const QuantKernel every[2][2][2] = {{{quant_decode_kernel<16, 4, false>, quant_decode_kernel<32, 4, false>},
+                                                {quant_decode_kernel<16, 8, false>, quant_decode_kernel<32, 8, false>}},
+                                               {{quant_decode_kernel<16, 4, false, false, true>, quant_decode_kernel<32, 4, false, false, true>},
+                                                {quant_decode_kernel<16, 8, false, false, true>, quant_decode_kernel<32, 8, false, false, true>}}};
+    static const QuantKernel by_length[2][2] = {{quant_decode_kernel<16, 8, false, true>, quant_decode_kernel<32, 8, false, true>},
+                                                {quant_decode_kernel<16, 8, false, true, true>, quant_decode_kernel<32, 8, false, true, true>}};
+    static const QuantKernel in_line[2][2] = {{quant_line_kernel<16, 4, false>, quant_line_kernel<32, 4, false>},
+                                              {quant_line_kernel<16, 4, true>, quant_line_kernel<32, 4, true>}};
+    const QuantKernel kern = line ? in_line[once][by_page] : dealt ? by_length[once][by_page] : !page_ids ? every[once][wide][by_page]
+                                  : once && !wide ? lists_streamed[by_page] : lists[wide][by_page];
     if (lds > 64 * 1024) {
         const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
         if (e != hipSuccess) return e;
     }
     return launch(kern, grid, block, lds, stream, (uint64_t)seq_lens, (uint64_t)block_table, (uint64_t)q, (uint64_t)page_ids, (uint64_t)n_selected,
-                  g.n_kv_heads << 8 | g.group, g.max_sel, g.max_pages, n_splits,
+                  g.n_kv_heads << 8 | g.group, g.max_sel, g.max_pages, line ? batch : n_splits,
                   QuantArgs{k_pool, v_pool, scales, out, ws_acc, ws_ml, arrivals, ctx->sm_scale * 1.4426950408889634f, batch});
 }
 
-// Four-wave workgroups of attention over every page that fit on a compute unit, dealt or not, whichever are fewer.
+// Four-wave workgroups of attention over every page of a batch that fit on a compute unit.
 hipError_t quant_occupancy(int page_size, int group, int* blocks_per_cu)
 {
-    const size_t lds = quant_lds_bytes(4, group);
-    const QuantKernel fixed = page_size == 16 ? quant_decode_kernel<16, 4, false> : quant_decode_kernel<32, 4, false>;
-    const QuantKernel dealt = page_size == 16 ? quant_decode_kernel<16, 4, false, true> : quant_decode_kernel<32, 4, false, true>;
-    int n = 0;
-    *blocks_per_cu = 1 << 30;
-    for (const QuantKernel kern : {fixed, dealt}) {
-        const hipError_t e = hipOccupancyMaxActiveBlocksPerMultiprocessor(&n, kern, 256, lds);
-        if (e != hipSuccess) return e;
-        *blocks_per_cu = n < *blocks_per_cu ? n : *blocks_per_cu;
-    }
-    return hipSuccess;
+    const QuantKernel kern = page_size == 16 ? quant_line_kernel<16, 4, false> : quant_line_kernel<32, 4, false>;
+    return hipOccupancyMaxActiveBlocksPerMultiprocessor(blocks_per_cu, kern, 256, quant_lds_bytes(4, group));
 }
 
 }  // namespace chess

@@ -111,20 +111,29 @@ inline SplitShape choose_splits(const SplitLimits& c, int batch, int64_t max_lis
 // fit at once).  Lists and batches go by the rules above, which their own sweeps bear out: lists within 3 % of the best of 2 .. 64 splits of four or
 // eight waves, within 6 % of it for 24 rows of 500 pages.  Every page of one sequence: eight waves, at most one workgroup to a compute unit, since each
 // reads as fast alone as two do (us, 262139 tokens, 4 KV heads, G = 7: 64 splits, 256 workgroups, 58; 68, which is 272, 80; 128 76); fewer where the
-// partials outweigh the tiles, in which the merge by twice the threads counts when they have outputs (more than four heads).  us, 8 waves:
+// partials outweigh the tiles, in which the merge by twice the threads counts when they have outputs (more than four heads).  us, eight waves:
 //   2048 tokens, 8 KV heads, G = 4       8 splits  6.9   16  7.3   24  8.3   32  8.7         32768   16 splits 19.0   24 17.6   32 17.3
 //   8192                                 8        12.2   16  9.7   24 10.3   32 10.1        131072   16        67.4   24 54.5   32 54.6
 //   16384, 4 KV heads, G = 7            16        13.5   32 12.2   48 13.2   64 14.2
-// Several sequences: dealt by length (share_slots), as such workgroups too where that leaves five of them to a sequence, so that their rounding costs
-// little; otherwise as four-wave ones, twice as many.  us, four / eight waves, sequences and workgroups a sequence of the latter: 2 of 25K and 192K
-// tokens, 4 KV heads, G = 7 (32) 62.5 / 50.5; 4 of 20-131K, 8 heads, G = 4 (8) 117.0 / 116.6; 4 of 5-21K (8) 25.2 / 23.5; 10 of 45-48K, 4 heads, G = 7
-// (6.4) 92.2 / 90.0; 6 of 6-7K, 8 heads (5.3) 20.4 / 19.8; 13 of 7-14K (2.5) 52 / 56; 16 of 8-64K (2) 218 / 243.
+// Several sequences: dealt by length (share_slots), as such workgroups too, where that leaves five of them to a sequence, so that their rounding costs
+// little.  Otherwise the batch's tiles in a line, an equal share to each of the four-wave workgroups that fit at once (quant_line_kernel); or, short
+// rows in great number, a workgroup each.  us, dealt to eight waves / in a line / (where measured) dealt to four waves or a workgroup a row:
+//   2 of 25K and 192K tokens, 4 KV heads, G = 7   50.8 /  62.3 /  62.5      16 of 8-64K, 8 heads              243 / 212 / 218
+//   4 of 5-21K, 8 heads                           23.6 /  27.2 /  25.2      45 of 3-7K, 8 heads, pages of 32  114 /  88 / 100
+//   6 of 6-7K, 8 heads                            20.0 /  21.3 /  20.4      96 of 1-8K, 8 heads, of 32              160 / 187
+//   13 of 7-14K, 8 heads, G = 1                   56   /  53   /  52        300 of 500-3000, 8 heads                206 / 207
+//   200 of 100-600, 4 heads, G = 7                        25.7 /  19.4      2000 of 1-2000, one head                127 / 111
 inline SplitShape choose_quant_splits(const SplitLimits& c, int batch, int64_t max_list_pages, bool listed)
 {
-    if (c.force_splits > 0) return {c.force_splits, !listed && c.force_waves == 4 ? 8 : c.force_waves, 0};
-    const int64_t slots = c.n_cu / c.n_kv_heads;      // (with the partials' rows, four times as many, there is always room for them)
-    if (listed || (batch > 1 && slots < 5LL * batch)) return choose_splits(c, batch, max_list_pages, listed);
-    const int64_t tiles = std::max<int64_t>(1, cdiv(max_list_pages, c.tile_pages));
+    if (c.force_splits > 0) return {c.force_splits, !listed || c.force_waves == 8 ? 8 : 4, 0};
+    if (listed) return choose_splits(c, batch, max_list_pages, true);
+    const int64_t tiles = std::max<int64_t>(1, cdiv(max_list_pages, c.tile_pages)), rows = (int64_t)batch * c.n_kv_heads;
+    const int64_t slots = c.n_cu / c.n_kv_heads;      // (with the partials' rows, four a compute unit and one a row, there is always room)
+    if (batch > 1 && slots < 5LL * batch) {
+        const int64_t shares = std::min(c.resident, 4 * c.n_cu) / c.n_kv_heads;
+        if (shares < 1 || (rows >= 2LL * c.n_cu && tiles <= 32)) return {1, 4, 0};
+        return {1, 4, (int)shares};
+    }
     const int64_t balanced = (int64_t)std::sqrt((c.group > 4 ? 16.0 : 8.0) * (double)tiles / c.group);
     const int64_t most = std::min<int64_t>({slots, c.max_splits, 1024 / c.group, tiles});
     return {(int)clampi(balanced, 1, std::max<int64_t>(most, 1)), 8, batch > 1 ? (int)slots : 0};

@@ -247,6 +247,15 @@ def test_batches_dealt_to_four_and_to_eight_waves(B, Hq, H):
 
 
 @pytest.mark.parametrize("B", [16, 32])
+@pytest.mark.parametrize("Hq,H", [(2, 1), (14, 2), (32, 8)])
+def test_shares_that_hold_ends_whole_sequences_and_beginnings(B, Hq, H):
+    """Many sequences in a line: empty ones, ones of a tile, and long ones that many workgroups share."""
+    rng = np.random.default_rng(Hq + 60)
+    for lens in ([0] * 30 + [5000] + [0, 1] * 20 + [900] * 10, [64] * 130, rng.integers(1, 3000, 70).tolist(), [3000] + [1] * 200 + [3000]):
+        check_attention(rng, lens if H < 8 else lens[25:60], Hq, H, B, pages=6000 // B)
+
+
+@pytest.mark.parametrize("B", [16, 32])
 @pytest.mark.parametrize("e", [-64, 119])
 def test_scales_at_either_end(B, e):
     """Values of the largest and the smallest scale; keys of the smallest."""
