@@ -852,7 +852,7 @@ const char* chess_strerror(int code)
     switch (code) {
     case CHESS_OK: return "ok";
     case CHESS_EINVAL: return "invalid argument (null pointer, misaligned buffer, or shape outside the configuration)";
-    case CHESS_ENOTSUP: return "not supported (a selection level would have more candidates than fit in LDS)";
+    case CHESS_ENOTSUP: return "not supported (a selection level with more candidates than fit in LDS, or more sequences or entries than the call takes)";
     case CHESS_EHIP: return "HIP runtime error at kernel launch";
     case CHESS_ENOMEM: return "out of host memory";
     case CHESS_ESCRATCH: return "the call needs more device scratch than chess_sparse_decode_static owns (CHESS_STATIC_SCRATCH_BYTES)";

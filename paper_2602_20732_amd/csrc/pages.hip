@@ -111,7 +111,7 @@ __global__ __launch_bounds__(kPageThreads) void map_kernel(MapArgs a)
     sums_upto<3>(batch, upto, [&](int b, int (&v)[3]) {
         const int64_t L = a.seq_lens[b], n = a.new_lens[b];
         held[b] = (int)L;
-        if (L < 0 || n <= 0 || L + n > (int64_t)a.max_pages * B) return;
+        if (L < 0 || n <= 0 || L + n > min((int64_t)a.max_pages * B, (int64_t)INT32_MAX - B)) return;
         v[0] = (int)min(n, (int64_t)kSumCap);
         v[1] = (int)((L + n + B - 1) / B - (L + B - 1) / B);
         v[2] = (int)((L + n - 1) / B - L / B + 1);
@@ -179,7 +179,7 @@ __global__ __launch_bounds__(kPageThreads) void release_kernel(ReleaseArgs a)
     extern __shared__ int upto[];                     // [batch]: pages pushed
     const int batch = a.batch, n_free = max(*a.n_free, 0);
     sums_upto<1>(batch, upto, [&](int b, int (&v)[1]) {
-        if (a.done[b] != 0) v[0] = (min(max(a.seq_lens[b], 0), a.max_pages * B) + B - 1) / B;
+        if (a.done[b] != 0) v[0] = (int)min(((int64_t)max(a.seq_lens[b], 0) + B - 1) / B, (int64_t)a.max_pages);
     });
     const int cut = served(batch, [&](int b) { return upto[b] <= a.capacity - n_free; });
     const int total = cut > 0 ? upto[cut - 1] : 0;

@@ -381,3 +381,31 @@ def test_the_same_bits_on_every_call_and_from_a_graph():
             torch.cuda.current_stream().wait_stream(side)
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(first, outs)), i
+
+
+@pytest.mark.parametrize("B", [16, 32])
+def test_a_value_that_was_not_finite_stays_where_it_belongs(B):
+    """Stored as NaN: in a value it spoils one output of its head group, in a key its sequence and KV head, and nothing else."""
+    rng = np.random.default_rng(3)
+    H, Hq, lens = 2, 8, [200, 90, 300]
+    table, n_phys = dealt(rng, lens, 20, B)
+    lib = pk.Chess(pk.Config(Hq, H, B, 3, 20, 20))
+    ws, bt, sl = lib.new_workspace(), torch.from_numpy(table).cuda(), ints(lens)
+    q = bf16(rng.normal(0, 1, (3, Hq, D))).cuda()
+    k, v, scales = Cache(rng, n_phys, H, B).clean().cuda()
+    ids, n = ints(np.tile(np.arange(20), (3, H, 1))), ints(np.tile(-(-np.array(lens) // B)[:, None], (1, H)))
+    rows = [bf16(rng.normal(0, 1, (1, H, D))) for _ in range(2)]
+    rows[0][0, 1, 5], rows[1][0, 0, 77] = float("inf"), float("nan")             # a key of head 1, a value of head 0
+
+    def attend():
+        outs = [torch.empty((3, Hq, D), device="cuda") for _ in range(2)]
+        lib.quant_sparse_decode(q, k, v, scales, bt, sl, ids, n, outs[0], ws)
+        lib.quant_dense_decode(q, k, v, scales, bt, sl, outs[1], ws)
+        torch.cuda.synchronize()
+        return [o.cpu() for o in outs]
+
+    before = attend()
+    lib.quant_store(rows[0].cuda(), rows[1].cuda(), ints([[int(table[0, 50 // B]), 0, 50 % B, 1]]), ints([1, 1, 0, 0]), k, v, scales)
+    for old, new in zip(before, attend()):
+        assert torch.equal(old[1:], new[1:]) and bool(new[0, 4:].isnan().all())
+        assert bool(new[0, :4, 77].isnan().all()) and not new[0, :4, :77].isnan().any() and not new[0, :4, 78:].isnan().any()

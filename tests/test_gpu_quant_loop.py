@@ -199,3 +199,71 @@ def test_a_server_over_an_8_bit_cache(B):
                 o, off = ref.attention(qn[b, 4 * h:4 * h + 4], kl, vl, 1 / math.sqrt(D))
                 assert (np.abs(got_out[b, 4 * h:4 * h + 4] - o) <= off).all(), (step, b, h)
     assert lib.workspace_error(ws) == 0
+
+
+@pytest.mark.parametrize("B", [16, 32])
+def test_a_captured_step_of_the_8_bit_cache(B):
+    """The chain from the dealing of pages to attention as one graph, replayed between other work while its inputs change, against the same calls
+    made one by one on a second set of buffers: the same bits in every buffer after every step."""
+    rng = np.random.default_rng(B + 7)
+    H, Hq, batch, pages, n_phys, room, most = 2, 8, 5, 12, 70, 9, 80
+    lib = pk.Chess(pk.Config(Hq, H, B, batch, pages, room, 4, 4, summary_dtype=helpers.SUMMARY_DTYPE))
+    plan = pk.SelectPlan(budget_pages=3, window_pages=2)
+
+    class Side:
+        def __init__(self):
+            self.ws, self.summ = lib.new_workspace(), lib.new_summaries()
+            self.k = torch.zeros((n_phys, H, B, D), dtype=torch.uint8, device="cuda")
+            self.v = torch.zeros((n_phys, H, D, B), dtype=torch.uint8, device="cuda")
+            self.scales = torch.ones((n_phys, H, 2), device="cuda")
+            self.table = torch.full((batch, pages), -1, dtype=torch.int32, device="cuda")
+            self.free, self.n_free = ints(np.arange(n_phys)), ints([n_phys])
+            self.lens, self.done, self.new = ints([0] * batch), ints([0] * batch), ints([0] * batch)
+            self.starts, self.counts = ints([0] * (batch + 1)), ints([0] * 4)
+            self.slots = torch.zeros(most, dtype=torch.int64, device="cuda")
+            self.writes = torch.zeros((lib.write_rows(most, batch), 4), dtype=torch.int32, device="cuda")
+            self.x = torch.zeros((2, most, H, D), dtype=torch.bfloat16, device="cuda")
+            self.q = torch.zeros((batch, Hq, D), dtype=torch.bfloat16, device="cuda")
+            self.ids, self.n = ints(np.zeros((batch, H, room))), ints(np.zeros((batch, H)))
+            self.outs = [torch.zeros((batch, Hq, D), device="cuda") for _ in range(2)]
+
+        def step(self):
+            lib.release_pages(self.lens, self.done, self.table, self.free, self.n_free, self.lens, self.n_free, self.ws)
+            lib.map_tokens(self.lens, self.new, self.table, self.free, self.n_free, self.lens, self.n_free, self.starts, self.slots, self.writes,
+                           self.counts, self.ws)
+            lib.quant_store(self.x[0], self.x[1], self.writes, self.counts, self.k, self.v, self.scales)
+            lib.quant_summarize(self.k, self.scales, self.table, self.lens, self.summ, recent_pages=6)
+            lib.select(self.q, self.summ, self.lens, plan, self.ids, self.n, self.ws)
+            lib.quant_sparse_decode(self.q, self.k, self.v, self.scales, self.table, self.lens, self.ids, self.n, self.outs[0], self.ws)
+            lib.quant_dense_decode(self.q, self.k, self.v, self.scales, self.table, self.lens, self.outs[1], self.ws)
+
+        def buffers(self):
+            return [self.k, self.v, self.scales, self.table, self.free, self.n_free, self.lens, self.starts, self.counts, self.slots, self.writes,
+                    self.ids, self.n, *self.outs]
+
+    eager, replayed = Side(), Side()
+    for s in (eager, replayed):
+        s.step()                                                                 # (no tokens: everything is loaded)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        replayed.step()
+    held = np.zeros(batch, int)
+    for i in range(14):
+        done = (held > 4 * B) & (rng.random(batch) < 0.4)
+        new = np.where(done | (held == 0), rng.integers(1, 2 * B if B == 16 else B // 2, batch), 1)
+        x = torch.from_numpy(rng.normal(0, 1, (2, most, H, D)).astype(np.float32)).to(torch.bfloat16)
+        q = torch.from_numpy(rng.normal(0, 0.5, (batch, Hq, D)).astype(np.float32)).to(torch.bfloat16)
+        for s in (eager, replayed):
+            s.done.copy_(ints(done.astype(int)))
+            s.new.copy_(ints(new))
+            s.x.copy_(x)
+            s.q.copy_(q)
+        eager.step()
+        graph.replay()
+        torch.cuda.synchronize()
+        held = eager.lens.cpu().numpy()
+        assert held.any()
+        for a, b in zip(eager.buffers(), replayed.buffers()):
+            assert torch.equal(a, b), i
+        assert torch.equal(eager.summ, replayed.summ), i
