@@ -323,7 +323,7 @@ class Chess:
         return n.value
 
     def release_pages(self, seq_lens, done, block_table, free_pages, n_free, lens_after, n_left, workspace):
-        batch, dev = seq_lens.shape[0], self.device
+        batch, dev = seq_lens.numel(), self.device
         _need(seq_lens, "seq_lens", _INT, batch, dev)
         _need(done, "done", _INT, batch, dev)
         _need(block_table, "block_table", _INT, batch * self.cfg.max_pages_per_seq, dev)
@@ -343,7 +343,7 @@ class Chess:
             if slots is None:
                 raise ChessError("map_tokens: slots or max_tokens is wanted")
             max_tokens = slots.numel()
-        batch, dev = seq_lens.shape[0], self.device
+        batch, dev = seq_lens.numel(), self.device
         _need(seq_lens, "seq_lens", _INT, batch, dev)
         _need(new_lens, "new_lens", _INT, batch, dev)
         _need(block_table, "block_table", _INT, batch * self.cfg.max_pages_per_seq, dev)
@@ -372,9 +372,11 @@ class Chess:
     def quant_store(self, k_new, v_new, writes, counts, k_pool, v_pool, scales):
         """k_new / v_new: bf16 [tokens, H_kv, 128], the rows of a token contiguous (slices of a wider projection will do); no tokens, nothing
         stored."""
-        n, H, d, dev = k_new.shape[0], self.cfg.n_kv_heads, self.cfg.head_dim, self.device
+        cfg, dev = self.cfg, self.device
+        n, H, d = k_new.size(0), cfg.n_kv_heads, cfg.head_dim
         for t, name in ((k_new, "k_new"), (v_new, "v_new")):
-            if t.dtype is not torch.bfloat16 or t.shape != (n, H, d) or t.stride(2) != 1 or (t.stride(1) != d and H > 1) or t.get_device() != dev:
+            if (t.dtype is not torch.bfloat16 or t.dim() != 3 or t.size(0) != n or t.size(1) != H or t.size(2) != d or t.stride(2) != 1 or
+                    (t.stride(1) != d and H > 1) or t.get_device() != dev):
                 raise ChessError(f"{name}: a bf16 tensor [{n}, {H}, {d}] on the context's device with contiguous token rows is wanted, "
                                  f"got {t.dtype} {tuple(t.shape)} of strides {t.stride()} on {t.device}")
         _need(writes, "writes", _INT, 4, dev)
@@ -389,7 +391,7 @@ class Chess:
                                                torch._C._cuda_getCurrentRawStream(dev)))
 
     def quant_summarize(self, k_pool, scales, block_table, seq_lens, summaries, from_page=None, recent_pages: int = 0):
-        batch, dev = seq_lens.shape[0], self.device
+        batch, dev = seq_lens.numel(), self.device
         _need(scales, "scales", _FLOAT, 2 * self.cfg.n_kv_heads, dev)
         self._need_pool(k_pool, scales, "k_pool", dev)
         _need(block_table, "block_table", _INT, batch * self.cfg.max_pages_per_seq, dev)
@@ -413,7 +415,7 @@ class Chess:
         _need(workspace, "workspace", _BYTE, self.workspace_bytes, dev)
 
     def quant_sparse_decode(self, q, k_pool, v_pool, scales, block_table, seq_lens, page_ids, n_selected, out, workspace):
-        batch, dev = seq_lens.shape[0], self.device
+        batch, dev = seq_lens.numel(), self.device
         self._need_attention(q, k_pool, v_pool, scales, block_table, seq_lens, out, workspace, batch, dev)
         _need(page_ids, "page_ids", _INT, batch * self.cfg.n_kv_heads * self.cfg.max_selected_pages, dev)
         _need(n_selected, "n_selected", _INT, batch * self.cfg.n_kv_heads, dev)
@@ -422,7 +424,7 @@ class Chess:
                                                        batch, out.data_ptr(), workspace.data_ptr(), torch._C._cuda_getCurrentRawStream(dev)))
 
     def quant_dense_decode(self, q, k_pool, v_pool, scales, block_table, seq_lens, out, workspace):
-        batch, dev = seq_lens.shape[0], self.device
+        batch, dev = seq_lens.numel(), self.device
         self._need_attention(q, k_pool, v_pool, scales, block_table, seq_lens, out, workspace, batch, dev)
         self._check(self.lib.chess_quant_dense_decode(self._h, q.data_ptr(), k_pool.data_ptr(), v_pool.data_ptr(), scales.data_ptr(),
                                                       block_table.data_ptr(), seq_lens.data_ptr(), batch, out.data_ptr(), workspace.data_ptr(),

@@ -409,3 +409,35 @@ def test_a_value_that_was_not_finite_stays_where_it_belongs(B):
     for old, new in zip(before, attend()):
         assert torch.equal(old[1:], new[1:]) and bool(new[0, 4:].isnan().all())
         assert bool(new[0, :4, 77].isnan().all()) and not new[0, :4, :77].isnan().any() and not new[0, :4, 78:].isnan().any()
+
+
+def test_kernels_with_much_lds_can_be_captured():
+    """Sixteen heads by eight waves, and the sums of 4096 sequences: more than 64 KB, asked for at the launch."""
+    rng = np.random.default_rng(14)
+    table, n_phys = dealt(rng, [700], 50, 16)
+    k, v, scales = Cache(rng, n_phys, 1, 16).clean().cuda()
+    lib = pk.Chess(pk.Config(16, 1, 16, 4096, 50, 50))
+    ws, q, out = lib.new_workspace(), bf16(rng.normal(0, 0.05, (1, 16, D))).cuda(), torch.zeros((1, 16, D), device="cuda")
+    bt, sl = torch.from_numpy(table).cuda(), ints([700])
+    n = 4096
+    big, free, left, counts = ints(np.full((n, 50), -1)), ints(np.arange(n)), ints([0]), ints([0] * 4)
+    after, starts, writes = ints([0] * n), ints([0] * (n + 1)), ints(np.zeros((n, 4)))
+    zero, one, n_free = ints([0] * n), ints([1] * n), ints([n])
+
+    def both():
+        lib.quant_dense_decode(q, k, v, scales, bt, sl, out, ws)
+        lib.map_tokens(zero, one, big, free, n_free, after, left, starts, None, writes, counts, ws, max_tokens=n)
+
+    both()
+    torch.cuda.synchronize()
+    first = out.clone()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        both()
+    for _ in range(3):
+        out.zero_()
+        counts.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, first) and counts.tolist() == [n, n, n, 0] and left.item() == 0
+        assert torch.equal(big[:, 0], torch.arange(n - 1, -1, -1, dtype=torch.int32, device="cuda"))
