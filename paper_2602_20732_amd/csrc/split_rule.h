@@ -116,27 +116,35 @@ inline SplitShape choose_splits(const SplitLimits& c, int batch, int64_t max_lis
 //   8192                                 8        12.2   16  9.7   24 10.3   32 10.1        131072   16        67.4   24 54.5   32 54.6
 //   16384, 4 KV heads, G = 7            16        13.5   32 12.2   48 13.2   64 14.2
 // Several sequences: dealt by length (share_slots), as such workgroups too, where that leaves five of them to a sequence, so that their rounding costs
-// little.  Otherwise the batch's tiles in a line, an equal share to each of the four-wave workgroups that fit at once (quant_line_kernel); or, short
-// rows in great number, a workgroup each.  us, dealt to eight waves / in a line / (where measured) dealt to four waves or a workgroup a row:
+// little.  Otherwise the batch's tiles in a line, an equal share to each of the four-wave workgroups that fit at once (quant_line_kernel).  us, dealt to
+// eight waves / in a line / (where measured) dealt to four waves or a workgroup a row:
 //   2 of 25K and 192K tokens, 4 KV heads, G = 7   50.8 /  62.3 /  62.5      16 of 8-64K, 8 heads              243 / 212 / 218
 //   4 of 5-21K, 8 heads                           23.6 /  27.2 /  25.2      45 of 3-7K, 8 heads, pages of 32  114 /  88 / 100
 //   6 of 6-7K, 8 heads                            20.0 /  21.3 /  20.4      96 of 1-8K, 8 heads, of 32              160 / 187
 //   13 of 7-14K, 8 heads, G = 1                   56   /  53   /  52        300 of 500-3000, 8 heads                206 / 207
-//   200 of 100-600, 4 heads, G = 7                        25.7 /  19.4      2000 of 1-2000, one head                127 / 111
+// Short rows (the configuration's longest, in tiles), where dealing and sharing cost more than they save: four-wave workgroups, as many a row as
+// its tiles and merge balance and as fit at once; between 17 and 32 tiles not where that would be one, with less than two a compute unit.  us, as above / so:
+//   60 of 50-150 tokens, 8 heads   13.6 /  7.1      4 of 748-1150, 4 heads, pages of 32  10.0 / 8.3     16 of 300-2000, 8 heads, G = 1   14.9 / 12.1
+//   200 of 100-600, 4 heads        25.7 / 19.3      4 of 1000-2000, 8 heads              10.7 / 7.6     60 of the same (480 rows)        32.9 / 35.9
+//   2000 of 1-2000, one head       127  / 111       3 of 10-200, 8 heads                  6.4 / 4.9     100 of 64-2000, 4 heads, G = 7   33.7 / 36.1
 inline SplitShape choose_quant_splits(const SplitLimits& c, int batch, int64_t max_list_pages, bool listed)
 {
     if (c.force_splits > 0) return {c.force_splits, !listed || c.force_waves == 8 ? 8 : 4, 0};
     if (listed) return choose_splits(c, batch, max_list_pages, true);
     const int64_t tiles = std::max<int64_t>(1, cdiv(max_list_pages, c.tile_pages)), rows = (int64_t)batch * c.n_kv_heads;
+    const int64_t limit = std::min<int64_t>(c.max_splits, 1024 / c.group);
+    const double balanced = std::sqrt(8.0 * (double)tiles / c.group);
+    if (batch > 1 && (tiles <= 16 || (tiles <= 32 && (2 * rows <= c.n_cu || rows >= 2LL * c.n_cu)))) {
+        const int64_t most = std::min<int64_t>({c.resident / rows, partial_rows(c.n_cu, rows) / rows, cdiv(tiles, 4), limit});
+        return {(int)clampi(std::llround(balanced), 1, std::max<int64_t>(most, 1)), 4, 0};
+    }
     const int64_t slots = c.n_cu / c.n_kv_heads;      // (with the partials' rows, four a compute unit and one a row, there is always room)
     if (batch > 1 && slots < 5LL * batch) {
         const int64_t shares = std::min(c.resident, 4 * c.n_cu) / c.n_kv_heads;
-        if (shares < 1 || (rows >= 2LL * c.n_cu && tiles <= 32)) return {1, 4, 0};
-        return {1, 4, (int)shares};
+        return {1, 4, (int)shares};                   // (0: a workgroup a row)
     }
-    const int64_t balanced = (int64_t)std::sqrt((c.group > 4 ? 16.0 : 8.0) * (double)tiles / c.group);
-    const int64_t most = std::min<int64_t>({slots, c.max_splits, 1024 / c.group, tiles});
-    return {(int)clampi(balanced, 1, std::max<int64_t>(most, 1)), 8, batch > 1 ? (int)slots : 0};
+    const int64_t wide = (int64_t)(c.group > 4 ? balanced * std::sqrt(2.0) : balanced), most = std::min<int64_t>({slots, limit, tiles});
+    return {(int)clampi(wide, 1, std::max<int64_t>(most, 1)), 8, batch > 1 ? (int)slots : 0};
 }
 
 }  // namespace chess

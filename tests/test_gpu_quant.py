@@ -221,6 +221,15 @@ def test_every_page_of_short_and_odd_lengths(B, Hq, H):
 
 
 @pytest.mark.parametrize("B", [16, 32])
+@pytest.mark.parametrize("Hq,H", [(1, 1), (8, 2), (14, 2), (16, 1)])
+def test_short_and_odd_lengths_where_long_ones_could_be(B, Hq, H):
+    """The same and fewer of them in rows of a configuration for longer ones: in a line, and dealt by length."""
+    check_attention(np.random.default_rng(B + Hq), LENGTHS, Hq, H, B, pages=6000 // B)
+    check_attention(np.random.default_rng(B + Hq), LENGTHS[::2], Hq, H, B, pages=6000 // B)
+    check_attention(np.random.default_rng(B + Hq), [700, 700, 700], Hq, H, B, pages=6000 // B)
+
+
+@pytest.mark.parametrize("B", [16, 32])
 @pytest.mark.parametrize("n", [1, 40, 64, 700, 3001])
 def test_one_sequence(B, n):
     check_attention(np.random.default_rng(n), [n], 8, 2, B)
