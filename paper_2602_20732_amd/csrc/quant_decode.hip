@@ -133,13 +133,14 @@ struct QuantAcc {
                 s[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(operand_of(w.z, w.w, 1.f), qop[2 * half + 1], s[c], 0, 0, 0);
             }
         }
-        const float by = tl.scale.x * scale_log2, v_scale = tl.scale.y * kSumUnit;
+        // (above zero: a product with a masked token's score stays -inf)
+        const float by = fmaxf(tl.scale.x * scale_log2, 1e-37f), v_scale = tl.scale.y * kSumUnit;
         float x[16];
 #pragma unroll
-        for (int e = 0; e < 16; ++e) x[e] = e < tl.nt ? s[e >> 2][e & 3] * by : -INFINITY;
-        float tmax = x[0];
+        for (int e = 0; e < 16; ++e) x[e] = e < tl.nt ? s[e >> 2][e & 3] : -INFINITY;
+        float tmax = x[0] * by;
 #pragma unroll
-        for (int e = 1; e < 16; ++e) tmax = fmaxf(tmax, x[e]);
+        for (int e = 1; e < 16; ++e) tmax = fmaxf(tmax, x[e] * by);
         tmax = fmaxf(tmax, __shfl_xor(tmax, 16));
         tmax = fmaxf(tmax, __shfl_xor(tmax, 32));
         const float m_new = fmaxf(m_run, tmax);
@@ -149,7 +150,8 @@ struct QuantAcc {
         bf16x8 p[2][3];
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
-            const float w = __builtin_amdgcn_exp2f(x[e] - m_new);
+            // (score times scale less maximum, rounded once: what weighs most is next to the maximum, where that rounding is small)
+            const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(x[e], by, -m_new));
             psum += w;
             const __bf16 hi = (__bf16)w;
             const float rest = w - (float)hi;
