@@ -92,6 +92,15 @@ __device__ __forceinline__ void quant_rows(QuantTile<B>& tl, const QuantRef& r, 
     tl.nt = at.v < n_pages ? (r.lv == P - 1 ? L - r.lv * B : B) - 16 * grp % B : 0;
 }
 
+// 2^(score - largest), at most 1.  The score is the rounded product that the largest was chosen by, never one rounded together with the difference: a
+// score of 1e9 is rounded by 64 and more, and the largest one's weight would be 2 to the power of its rounding, 0 or infinite instead of 1.
+// (Rounded together, errors against 64 bits are a tenth smaller at ordinary scores: 16 sequences of 8-64K 6.7-7.4e-7 where 7.9-8.4e-7.)
+__device__ __forceinline__ float weight_of(float score, float largest)
+{
+#pragma clang fp contract(off)
+    return __builtin_amdgcn_exp2f(score - largest);
+}
+
 // Online-softmax state of one wave: all G heads of one KV head.
 struct QuantAcc {
     bf16x8 qop[4];      // head m16: d = 64 j + 16 grp + 8 i .. + 7 is step 2 j + i; heads >= G are zero columns
@@ -133,14 +142,13 @@ struct QuantAcc {
                 s[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(operand_of(w.z, w.w, 1.f), qop[2 * half + 1], s[c], 0, 0, 0);
             }
         }
-        // (above zero: a product with a masked token's score stays -inf)
-        const float by = fmaxf(tl.scale.x * scale_log2, 1e-37f), v_scale = tl.scale.y * kSumUnit;
+        const float by = tl.scale.x * scale_log2, v_scale = tl.scale.y * kSumUnit;
         float x[16];
 #pragma unroll
-        for (int e = 0; e < 16; ++e) x[e] = e < tl.nt ? s[e >> 2][e & 3] : -INFINITY;
-        float tmax = x[0] * by;
+        for (int e = 0; e < 16; ++e) x[e] = e < tl.nt ? s[e >> 2][e & 3] * by : -INFINITY;
+        float tmax = x[0];
 #pragma unroll
-        for (int e = 1; e < 16; ++e) tmax = fmaxf(tmax, x[e] * by);
+        for (int e = 1; e < 16; ++e) tmax = fmaxf(tmax, x[e]);
         tmax = fmaxf(tmax, __shfl_xor(tmax, 16));
         tmax = fmaxf(tmax, __shfl_xor(tmax, 32));
         const float m_new = fmaxf(m_run, tmax);
@@ -150,8 +158,7 @@ struct QuantAcc {
         bf16x8 p[2][3];
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
-            // (score times scale less maximum, rounded once: what weighs most is next to the maximum, where that rounding is small)
-            const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(x[e], by, -m_new));
+            const float w = weight_of(x[e], m_new);
             psum += w;
             const __bf16 hi = (__bf16)w;
             const float rest = w - (float)hi;
