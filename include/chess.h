@@ -285,6 +285,7 @@ int chess_monitor_step(chess_ctx* ctx, const void* logits, int32_t batch, int32_
  * decode kernel over page indices; App. B).  Per q head: softmax(sm_scale * q . K_t) weighted sum
  * of V_t over the valid tokens of the listed pages.  bf16 inputs, fp32 accumulation, fp32 out.
  * page_ids entries must be distinct valid logical pages of the sequence.
+ * Scores may have any size that fp32 holds, with sm_scale and log2(e) multiplied in; every call that attends is meant.
  */
 int chess_sparse_decode(chess_ctx* ctx, const void* q, const void* k_pool, const void* v_pool,
                         const int32_t* block_table, const int32_t* seq_lens, const int32_t* page_ids,

@@ -26,7 +26,9 @@ namespace chess {
 typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
 typedef __attribute__((ext_vector_type(4))) float f32x4;
 
-constexpr float kNegBig = -1.0e30f;     // "no token yet" running maximum (log2 domain), finite on purpose
+// "No token yet" running maximum (log2 domain): no finite score is below it (one that were would weigh 0 with all of its row), and being finite itself it
+// never makes a difference of two infinities.
+constexpr float kNegBig = -0x1.fffffep127f;
 
 __device__ __forceinline__ bf16x8 as_bf16x8(const uint4& v) { return __builtin_bit_cast(bf16x8, v); }
 

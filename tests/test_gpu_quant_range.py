@@ -89,3 +89,11 @@ def test_the_largest_score_weighs_one_in_other_groups(B, Hq, H):
     for e, sign in ((30, 1), (60, -1)):
         for _, way in EVERY_WAY:
             call(Hq + B, way, Hq, H, B, e, sign)
+
+
+@pytest.mark.parametrize("way", [w for _, w in EVERY_WAY], ids=[n.replace(" ", "_") for n, _ in EVERY_WAY])
+@pytest.mark.parametrize("B", [16, 32])
+@pytest.mark.parametrize("e", [94, 96, 100, 119])
+def test_rows_whose_every_score_is_far_below_zero(way, B, e):
+    """Scores from -1e30 down to -2e37 (the largest key scale) are scores all the same: the least of them in size weighs one."""
+    call(e + B, way, 8, 2, B, e, -1)
