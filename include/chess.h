@@ -7,7 +7,7 @@
  *
  * C ABI.  Every data pointer is a DEVICE pointer owned by the caller unless it says "host".
  * The library never allocates or frees device memory; only chess_append_kv and chess_reuse_step write the K/V
- * pools (the appended token's rows, nothing else), and only chess_quant_store 8-bit pools.  Every call is
+ * pools (the appended token's rows, nothing else), and only chess_quant_store and its bounded form 8-bit pools.  Every call is
  * asynchronous on `stream` (a hipStream_t passed as void*, NULL = the default stream), does no
  * host synchronisation, and can be captured in a HIP graph.  A context caches launch shapes: calls on one
  * context must not run concurrently from several host threads (use one context per thread).
@@ -400,10 +400,15 @@ int chess_map_tokens(chess_ctx* ctx, const int32_t* seq_lens, const int32_t* new
  * the page's own scale if it held tokens before (an offset above 0) and its scale is larger.  A byte is x / 2^e rounded to nearest even,
  * saturated at 448; a value that is not finite is stored as NaN and left out of the maximum.  When a page's scale grows, the tokens it held are
  * moved to it (exact but where they become subnormal: below 2^-6 of the scale).  Bytes behind the new tokens are left as they are.
- * No two entries may name the same page.
+ * No two entries may name the same page.  What the entries name is trusted here: k_new and v_new have the rows (at least counts[0] of them, as
+ * chess_map_tokens leaves it), the pools the pages.  chess_quant_store_bounded is told how many there are, n_rows and n_pages, and looks: an entry with
+ * a row or a page that is not there stores nothing, and the others what they store otherwise.  CHESS_EINVAL also for n_rows or n_pages below 1.
  */
 int chess_quant_store(chess_ctx* ctx, const void* k_new, int64_t k_stride, const void* v_new, int64_t v_stride, const int32_t* writes,
                       const int32_t* counts, int32_t max_writes, void* k_pool, void* v_pool, float* scales, void* stream);
+int chess_quant_store_bounded(chess_ctx* ctx, const void* k_new, int64_t k_stride, const void* v_new, int64_t v_stride, int32_t n_rows,
+                              const int32_t* writes, const int32_t* counts, int32_t max_writes, void* k_pool, void* v_pool, float* scales,
+                              int32_t n_pages, void* stream);
 
 /* chess_summarize (recent_pages = 0; from_page as there, or NULL) or chess_summarize_recent (recent_pages >= 1, from_page NULL; 1 is the refresh of
  * a decode step) on the values that 8-bit pages stand for; the summaries are what chess_select and chess_select_shared read. */

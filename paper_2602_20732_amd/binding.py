@@ -22,7 +22,7 @@ _lib = None
 
 EXPORTS = ["chess_create", "chess_destroy", "chess_summary_bytes", "chess_summary_layout", "chess_workspace_bytes", "chess_workspace_init",
            "chess_summarize", "chess_summarize_tail", "chess_summarize_recent", "chess_append_kv", "chess_select", "chess_anchor", "chess_select_shared", "chess_entropy", "chess_trigger_update", "chess_monitor_step", "chess_extend_window", "chess_reuse_step", "chess_sparse_decode", "chess_sparse_decode_static", "chess_dense_decode", "chess_decode_step",
-           "chess_write_rows", "chess_release_pages", "chess_map_tokens", "chess_quant_store", "chess_quant_summarize",
+           "chess_write_rows", "chess_release_pages", "chess_map_tokens", "chess_quant_store", "chess_quant_store_bounded", "chess_quant_summarize",
            "chess_quant_sparse_decode", "chess_quant_dense_decode",
            "chess_debug_force_splits", "chess_debug_force_cluster", "chess_debug_force_schedule", "chess_debug_force_general_cut", "chess_debug_set_poll_limit", "chess_workspace_error", "chess_strerror", "chess_version"]
 
@@ -125,6 +125,8 @@ def load_library() -> ctypes.CDLL:
         lib.chess_release_pages.argtypes = [vp, i32p, i32p, ctypes.c_int32, i32p, i32p, ctypes.c_int32, i32p, i32p, i32p, vp, vp]
         lib.chess_map_tokens.argtypes = [vp, i32p, i32p, ctypes.c_int32, ctypes.c_int32] + [vp] * 11
         lib.chess_quant_store.argtypes = [vp, vp, ctypes.c_int64, vp, ctypes.c_int64, i32p, i32p, ctypes.c_int32, vp, vp, vp, vp]
+        lib.chess_quant_store_bounded.argtypes = [vp, vp, ctypes.c_int64, vp, ctypes.c_int64, ctypes.c_int32, i32p, i32p, ctypes.c_int32, vp, vp, vp,
+                                                  ctypes.c_int32, vp]
         lib.chess_quant_summarize.argtypes = [vp, vp, vp, i32p, i32p, ctypes.c_int32, i32p, ctypes.c_int32, vp, vp]
         lib.chess_quant_sparse_decode.argtypes = [vp, vp, vp, vp, vp, i32p, i32p, i32p, i32p, ctypes.c_int32, vp, vp, vp]
         lib.chess_quant_dense_decode.argtypes = [vp, vp, vp, vp, vp, i32p, i32p, ctypes.c_int32, vp, vp, vp]
@@ -371,7 +373,7 @@ class Chess:
 
     def quant_store(self, k_new, v_new, writes, counts, k_pool, v_pool, scales):
         """k_new / v_new: bf16 [tokens, H_kv, 128], the rows of a token contiguous (slices of a wider projection will do); no tokens, nothing
-        stored."""
+        stored.  An entry that names a token or a page beyond these tensors stores nothing."""
         cfg, dev = self.cfg, self.device
         n, H, d = k_new.size(0), cfg.n_kv_heads, cfg.head_dim
         for t, name in ((k_new, "k_new"), (v_new, "v_new")):
@@ -386,9 +388,9 @@ class Chess:
         self._need_pool(v_pool, scales, "v_pool", dev)
         if n == 0:
             return
-        self._check(self.lib.chess_quant_store(self._h, k_new.data_ptr(), k_new.stride(0), v_new.data_ptr(), v_new.stride(0), writes.data_ptr(),
-                                               counts.data_ptr(), writes.numel() // 4, k_pool.data_ptr(), v_pool.data_ptr(), scales.data_ptr(),
-                                               torch._C._cuda_getCurrentRawStream(dev)))
+        self._check(self.lib.chess_quant_store_bounded(self._h, k_new.data_ptr(), k_new.stride(0), v_new.data_ptr(), v_new.stride(0), n,
+                                                       writes.data_ptr(), counts.data_ptr(), writes.numel() // 4, k_pool.data_ptr(), v_pool.data_ptr(),
+                                                       scales.data_ptr(), scales.numel() // (2 * H), torch._C._cuda_getCurrentRawStream(dev)))
 
     def quant_summarize(self, k_pool, scales, block_table, seq_lens, summaries, from_page=None, recent_pages: int = 0):
         batch, dev = seq_lens.numel(), self.device

@@ -779,18 +779,26 @@ int chess_map_tokens(chess_ctx* ctx, const int32_t* seq_lens, const int32_t* new
     return chess::launch_map(ctx, a, static_cast<hipStream_t>(stream)) == hipSuccess ? CHESS_OK : CHESS_EHIP;
 }
 
-int chess_quant_store(chess_ctx* ctx, const void* k_new, int64_t k_stride, const void* v_new, int64_t v_stride, const int32_t* writes,
-                      const int32_t* counts, int32_t max_writes, void* k_pool, void* v_pool, float* scales, void* stream)
+int chess_quant_store_bounded(chess_ctx* ctx, const void* k_new, int64_t k_stride, const void* v_new, int64_t v_stride, int32_t n_rows,
+                              const int32_t* writes, const int32_t* counts, int32_t max_writes, void* k_pool, void* v_pool, float* scales,
+                              int32_t n_pages, void* stream)
 {
-    if (!ctx || !k_new || !v_new || !writes || !counts || !k_pool || !v_pool || !scales || max_writes < 1) return CHESS_EINVAL;
+    if (!ctx || !k_new || !v_new || !writes || !counts || !k_pool || !v_pool || !scales || max_writes < 1 || n_rows < 1 || n_pages < 1) return CHESS_EINVAL;
     const int64_t row = (int64_t)ctx->geom.n_kv_heads * kHeadDim;
     if (k_stride < row || v_stride < row || ((k_stride | v_stride) & 7)) return CHESS_EINVAL;
     if (misaligned({k_new, v_new, writes, k_pool, v_pool}, 15) || misaligned({scales}, 7) || !on_device(ctx)) return CHESS_EINVAL;
     if ((int64_t)max_writes * ctx->geom.n_kv_heads > (int64_t)1 << 29) return CHESS_ENOTSUP;      // waves, in 32 bits
     const chess::StoreArgs a{static_cast<const uint16_t*>(k_new), static_cast<const uint16_t*>(v_new), k_stride, v_stride,
                              reinterpret_cast<const int4*>(writes), counts, static_cast<uint8_t*>(k_pool), static_cast<uint8_t*>(v_pool), scales,
-                             ctx->geom.n_kv_heads, max_writes};
+                             ctx->geom.n_kv_heads, max_writes, n_rows, n_pages};
     return chess::launch_quant_store(ctx, a, static_cast<hipStream_t>(stream)) == hipSuccess ? CHESS_OK : CHESS_EHIP;
+}
+
+int chess_quant_store(chess_ctx* ctx, const void* k_new, int64_t k_stride, const void* v_new, int64_t v_stride, const int32_t* writes,
+                      const int32_t* counts, int32_t max_writes, void* k_pool, void* v_pool, float* scales, void* stream)
+{
+    return chess_quant_store_bounded(ctx, k_new, k_stride, v_new, v_stride, INT32_MAX, writes, counts, max_writes, k_pool, v_pool, scales, INT32_MAX,
+                                     stream);
 }
 
 int chess_quant_summarize(chess_ctx* ctx, const void* k_pool, const float* scales, const int32_t* block_table, const int32_t* seq_lens,

@@ -402,6 +402,7 @@ struct StoreArgs {
     uint8_t* v_pool;
     float* scales;
     int heads, max_writes;
+    int n_rows, n_pages;             // of k_new and v_new, of the pools
 };
 hipError_t launch_quant_store(chess_ctx* ctx, const StoreArgs& a, hipStream_t stream);
 hipError_t launch_quant_summarize(chess_ctx* ctx, const uint8_t* k_pool, const float* scales, const int32_t* block_table,

@@ -80,11 +80,14 @@ __global__ __launch_bounds__(256) void quant_store_kernel(StoreArgs a)
 {
     const int lane = threadIdx.x & 63, unit = __builtin_amdgcn_readfirstlane((int)(blockIdx.x * 4 + (threadIdx.x >> 6)));
     const int H = a.heads, per = 2 * H, w = unit / per, part = unit - w * per, h = part >= H ? part - H : part;
-    if (w >= min(a.counts[1], a.max_writes)) return;
+    // (all three counts here: those that an entry is looked at with would be fetched behind counts[1] otherwise)
+    if (((min(a.counts[1], a.max_writes) - 1 - w) | (a.n_rows - 1) | (a.n_pages - 1)) < 0) return;
     const int4 entry = a.writes[w];
     const int phys = __builtin_amdgcn_readfirstlane(entry.x), row0 = __builtin_amdgcn_readfirstlane(entry.y);
     const int first = min(max(__builtin_amdgcn_readfirstlane(entry.z), 0), B - 1), count = min(__builtin_amdgcn_readfirstlane(entry.w), B - first);
-    if (count <= 0) return;
+    // nothing new, or a row or page that is not there: one of these is negative (the differences wrap for negative rows and pages only, which say so themselves)
+    const int rows_left = max((int)((unsigned)a.n_rows - (unsigned)row0), 0) - count, pages_left = (int)((unsigned)a.n_pages - 1u - (unsigned)phys);
+    if (((count - 1) | row0 | rows_left | phys | pages_left) < 0) return;
     const size_t ph = (size_t)phys * H + h;
     float* scale_at = a.scales + 2 * ph + (part >= H ? 1 : 0);
     const float scale = first > 0 ? *scale_at : 0.f;
