@@ -10,9 +10,8 @@
 //   256 threads, 16 rows in flight   182 / 56 / 14.9      512 threads, 8 / 16 rows   180 / 53 / 10.1    182 / 56 / 9.9
 //   1024 threads, 8 rows             197 / 61 / 9.9       512, 8, rows as a stream   180 / 49 / 11.1 (hence kOnce: see launch_all)
 // The first is 4.8 to 5.2 TB/s, read and written, from card to card (a copy of 2 GiB: 4.8).  Vectors stored as a stream: 240 where 169 without.
-#include <algorithm>
-
 #include "quant_device.h"
+#include "split_rule.h"
 #include "summary_device.h"
 
 namespace chess {
@@ -141,7 +140,7 @@ static hipError_t launch_all(chess_ctx* ctx, const uint8_t* k_pool, const float*
                       ctx->cfg.max_batch * g.n_kv_heads, g.max_chunks, g.inv_nc, g.inv_ng, g.max_grids, (uint64_t)scales);
     const int ppg = g.n_c * g.n_g;
     const size_t lds = (size_t)(ppg + g.n_g) * kHeadDim * sizeof(T);
-    const int span = recent > 0 ? std::min(g.max_grids, (recent + ppg - 2) / ppg + 1) : g.max_grids;   // grids `recent` pages can touch
+    const int span = recent > 0 ? (int)recent_grids(recent, ppg, g.max_grids) : g.max_grids;
     // rows as a stream once they are more than the L2s hold (8 x 4 MB); fewer may still be there from the store that wrote them
     const bool once = (int64_t)batch * g.max_pages * g.n_kv_heads * B * kHeadDim > 32LL << 20;
     const auto kern = once ? quant_summarize_kernel<B, T, true> : quant_summarize_kernel<B, T, false>;

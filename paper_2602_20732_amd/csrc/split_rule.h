@@ -25,6 +25,9 @@ constexpr int kDealMost = 4096;   // most sequences whose every-page attention i
 inline int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
 inline int64_t clampi(int64_t x, int64_t lo, int64_t hi) { return x < lo ? lo : (x > hi ? hi : x); }
 
+// Grids of `ppg` pages that the last `recent` pages of a sequence can touch (any `recent` from 1 on: more than there are mean all).
+inline int64_t recent_grids(int64_t recent, int64_t ppg, int64_t max_grids) { return std::min(max_grids, (recent + ppg - 2) / ppg + 1); }
+
 // Rows of split partials a workspace for `rows` (sequence, KV head) pairs holds, in units of G vectors.
 inline int64_t partial_rows(int n_cu, int64_t rows) { return 4LL * n_cu + rows; }
 

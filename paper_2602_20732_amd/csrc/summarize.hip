@@ -6,8 +6,7 @@
 // 256-byte rows.  Each lane adds its 8 columns over the tokens in token order in fp64, so the sum
 // is the same number whatever the launch shape; the mean is rounded to fp32 once.  Page vectors of
 // the grid stay in LDS, chunk and grid means are formed from them without re-reading HBM.
-#include <algorithm>
-
+#include "split_rule.h"
 #include "summary_device.h"
 
 namespace chess {
@@ -146,7 +145,7 @@ hipError_t launch_summarize(chess_ctx* ctx, const uint16_t* k_pool, const int32_
     const bool bf16 = ctx->cfg.summary_dtype == CHESS_SUMMARY_BF16;
     const size_t lds = (size_t)(g.n_c * g.n_g + g.n_g) * kHeadDim * (bf16 ? sizeof(uint16_t) : sizeof(float));
     const int ppg = g.n_c * g.n_g;
-    const int span = recent > 0 ? std::min(g.max_grids, (recent + ppg - 2) / ppg + 1) : g.max_grids;   // grids `recent` pages can touch
+    const int span = recent > 0 ? (int)recent_grids(recent, ppg, g.max_grids) : g.max_grids;
     const dim3 grid(span, g.n_kv_heads, batch), block(256);
     const void* kern = bf16 ? (g.page_size == 16 ? reinterpret_cast<const void*>(summarize_kernel<16, uint16_t>)
                                                  : reinterpret_cast<const void*>(summarize_kernel<32, uint16_t>))
