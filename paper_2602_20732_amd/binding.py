@@ -388,7 +388,9 @@ class Chess:
         self._need_pool(v_pool, scales, "v_pool", dev)
         if n == 0:
             return
-        self._check(self.lib.chess_quant_store_bounded(self._h, k_new.data_ptr(), k_new.stride(0), v_new.data_ptr(), v_new.stride(0), n,
+        # (one token's stride leads nowhere and may be any number: of [H, 1, 128] transposed it is 128)
+        k_stride, v_stride = (k_new.stride(0), v_new.stride(0)) if n > 1 else (H * d, H * d)
+        self._check(self.lib.chess_quant_store_bounded(self._h, k_new.data_ptr(), k_stride, v_new.data_ptr(), v_stride, n,
                                                        writes.data_ptr(), counts.data_ptr(), writes.numel() // 4, k_pool.data_ptr(), v_pool.data_ptr(),
                                                        scales.data_ptr(), scales.numel() // (2 * H), torch._C._cuda_getCurrentRawStream(dev)))
 

@@ -58,3 +58,19 @@ def test_the_call_without_bounds_stores_the_same():
     for n_rows, n_pages in ((0, 5), (30, 0), (-1, 5)):
         assert lib.lib.chess_quant_store_bounded(lib._h, x[0].data_ptr(), H * D, x[1].data_ptr(), H * D, n_rows, writes.data_ptr(), counts.data_ptr(), 3,
                                                  k.data_ptr(), v.data_ptr(), scales.data_ptr(), n_pages, stream) == -1
+
+
+@pytest.mark.parametrize("B", [16, 32])
+def test_one_token_of_heads_laid_out_first(B):
+    """Keys [H, 1, 128] transposed: the token's stride is smaller than its row, and leads nowhere."""
+    rng = np.random.default_rng(B)
+    cache = Cache(rng, 2, H, B)
+    k, v, scales = cache.cuda()
+    rows = bf16(rng.normal(0, 1, (2, H, 1, D)))
+    x = [r.transpose(0, 1) for r in rows.cuda()]
+    assert x[0].stride(0) == D
+    pk.Chess(pk.Config(2 * H, H, B, 1, 4, 4)).quant_store(*x, ints([[1, 0, 5, 1]]), ints([1, 1, 0, 0]), k, v, scales)
+    torch.cuda.synchronize()
+    ref.store(cache.k, cache.v, cache.scales, *[r.transpose(0, 1).double().numpy() for r in rows], [[1, 0, 5, 1]])
+    assert np.array_equal(scales.cpu().double().numpy(), cache.scales)
+    assert ref.same_bytes(k.cpu().numpy(), cache.k) and ref.same_bytes(v.cpu().numpy(), cache.v)

@@ -46,3 +46,11 @@ def test_without_a_context_the_bounded_store_is_refused():
         build()
     lib = pk.load_library()
     assert lib.chess_quant_store_bounded(None, None, 1024, None, 1024, 5, None, None, 1, None, None, None, 7, None) == -1
+
+
+def test_the_stride_of_one_token_is_not_passed_on(chess):
+    """A dimension of size one may have any stride; the library wants one that a row fits in."""
+    one = torch.zeros((2, 1, 128), dtype=torch.bfloat16).transpose(0, 1)
+    assert one.stride(0) == 128
+    _, a = store(chess, one, torch.zeros(256, dtype=torch.bfloat16).as_strided((1, 2, 128), (1, 128, 1)))
+    assert (a["n_rows"], a["k_stride"], a["v_stride"]) == (1, 256, 256)
