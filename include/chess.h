@@ -394,7 +394,7 @@ int chess_map_tokens(chess_ctx* ctx, const int32_t* seq_lens, const int32_t* new
 
 /*
  * New tokens into the pages that chess_map_tokens dealt them (writes, counts: as it leaves them; only counts[1] is read; max_writes: the
- * entries `writes` has room for, which the launch is sized by).  k_new, v_new: bf16 [token][H][128], k_stride / v_stride elements from a token to
+ * entries `writes` has room for, which the launch is sized by; CHESS_ENOTSUP if that times H_kv is above 2^25 - 2).  k_new, v_new: bf16 [token][H][128], k_stride / v_stride elements from a token to
  * the next (>= H * 128, a multiple of 8: the keys and values may be slices of a wider projection), 16-byte aligned.
  * Per page and head, keys and values each: scale = 2^e, the smallest with max |x| <= 448 * 2^e over the page's new values (-64 <= e <= 119), or
  * the page's own scale if it held tokens before (an offset above 0) and its scale is larger.  A byte is x / 2^e rounded to nearest even,

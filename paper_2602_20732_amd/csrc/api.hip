@@ -787,7 +787,7 @@ int chess_quant_store_bounded(chess_ctx* ctx, const void* k_new, int64_t k_strid
     const int64_t row = (int64_t)ctx->geom.n_kv_heads * kHeadDim;
     if (k_stride < row || v_stride < row || ((k_stride | v_stride) & 7)) return CHESS_EINVAL;
     if (misaligned({k_new, v_new, writes, k_pool, v_pool}, 15) || misaligned({scales}, 7) || !on_device(ctx)) return CHESS_EINVAL;
-    if ((int64_t)max_writes * ctx->geom.n_kv_heads > (int64_t)1 << 29) return CHESS_ENOTSUP;      // waves, in 32 bits
+    if ((int64_t)max_writes * ctx->geom.n_kv_heads > ((int64_t)1 << 25) - 2) return CHESS_ENOTSUP;   // (a launch has fewer than 2^32 threads: 128 of these)
     const chess::StoreArgs a{static_cast<const uint16_t*>(k_new), static_cast<const uint16_t*>(v_new), k_stride, v_stride,
                              reinterpret_cast<const int4*>(writes), counts, static_cast<uint8_t*>(k_pool), static_cast<uint8_t*>(v_pool), scales,
                              ctx->geom.n_kv_heads, max_writes, n_rows, n_pages};

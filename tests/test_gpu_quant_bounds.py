@@ -74,3 +74,17 @@ def test_one_token_of_heads_laid_out_first(B):
     ref.store(cache.k, cache.v, cache.scales, *[r.transpose(0, 1).double().numpy() for r in rows], [[1, 0, 5, 1]])
     assert np.array_equal(scales.cpu().double().numpy(), cache.scales)
     assert ref.same_bytes(k.cpu().numpy(), cache.k) and ref.same_bytes(v.cpu().numpy(), cache.v)
+
+
+def test_more_entries_than_a_launch_has_threads_for():
+    """128 threads an entry and KV head, fewer than 2^32: the largest list is launched (and has no entry here), one more is refused."""
+    lib = pk.Chess(pk.Config(2, 2, 16, 1, 4, 4))
+    x, pool, scales, counts = bf16(np.zeros((1, 2, D))).cuda(), torch.zeros((1, 2, 16, D), dtype=torch.uint8, device="cuda"), torch.ones((1, 2, 2), device="cuda"), ints([0] * 4)
+    most = 2 ** 24 - 1
+    writes = torch.zeros((most + 1, 4), dtype=torch.int32, device="cuda")
+    call = lambda n: lib.lib.chess_quant_store_bounded(lib._h, x.data_ptr(), 2 * D, x.data_ptr(), 2 * D, 1, writes.data_ptr(), counts.data_ptr(), n,  # noqa: E731
+                                                       pool.data_ptr(), pool.data_ptr(), scales.data_ptr(), 1, ctypes.c_void_p(torch.cuda.current_stream().cuda_stream))
+    assert call(most) == 0
+    assert call(most + 1) == call(2 ** 27) == call(2 ** 31 - 1) == -2                # CHESS_ENOTSUP
+    torch.cuda.synchronize()
+    assert not pool.any()
