@@ -144,7 +144,7 @@ inline SplitShape choose_quant_splits(const SplitLimits& c, int batch, int64_t m
     const int64_t slots = c.n_cu / c.n_kv_heads;      // (with the partials' rows, four a compute unit and one a row, there is always room)
     if (batch > 1 && slots < 5LL * batch) {
         const int64_t shares = std::min(c.resident, 4 * c.n_cu) / c.n_kv_heads;
-        return {1, 4, (int)shares};                   // (0: a workgroup a row)
+        return {1, 4, batch * tiles > INT32_MAX ? 0 : (int)shares};   // (0: a workgroup a row; a line's tiles are counted in 32 bits)
     }
     const int64_t wide = (int64_t)(c.group > 4 ? balanced * std::sqrt(2.0) : balanced), most = std::min<int64_t>({slots, limit, tiles});
     return {(int)clampi(wide, 1, std::max<int64_t>(most, 1)), 8, batch > 1 ? (int)slots : 0};
