@@ -380,11 +380,12 @@ __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2))) vo
             line.upto = total + lanes_upto(line.tiles);
             total = lane_of(line.upto, 63);
             if (total > at) break;
+            if (line.b0 + 64 >= batch) return;        // (lengths that changed since they were summed end the walk, here and below)
         }
-    } else line.b0 = 0;
+    }
     lines.hold();
     int i = __builtin_ctzll(__ballot(line.upto > at));
-    for (;;) {
+    while (line.b0 + i < batch) {
         const int b = line.b0 + i, L = lane_of(line.len, i), tiles = lane_of(line.tiles, i), upto = lane_of(line.upto, i), begin = upto - tiles;
         const int t0 = at - begin, t_end = min(end, upto) - begin;
         const int first = t0 == 0 && t_end == tiles ? slot : line.slot_of(begin), n_splits = t0 == 0 && t_end == tiles ? 1 : line.slot_of(upto - 1) - first + 1;
