@@ -90,7 +90,7 @@ typedef struct {
     int32_t pages_per_chunk;    /* N_c (Sec. 3.1)                                            */
     int32_t chunks_per_grid;    /* N_g (Sec. 3.1); N_c * N_g <= 256                          */
     int32_t max_batch;
-    int32_t max_pages_per_seq;  /* row stride of the block table and of the page summaries   */
+    int32_t max_pages_per_seq;  /* row stride of the block table and of the page summaries; times page_size below 2^31 */
     int32_t max_selected_pages; /* row stride of page_ids                                    */
     float   sm_scale;           /* softmax scale; 0 means 1 / sqrt(head_dim)                 */
     int32_t summary_dtype;      /* CHESS_SUMMARY_*                                           */

@@ -176,6 +176,7 @@ int chess_create(const chess_config* cfg, chess_ctx** out)
         (int64_t)cfg->pages_per_chunk * cfg->chunks_per_grid > 256) return CHESS_EINVAL;
     if (cfg->max_batch < 1 || cfg->max_pages_per_seq < 1 || cfg->max_selected_pages < 1) return CHESS_EINVAL;
     if (cfg->max_selected_pages > cfg->max_pages_per_seq) return CHESS_EINVAL;
+    if ((int64_t)cfg->max_pages_per_seq * cfg->page_size > INT32_MAX) return CHESS_EINVAL;        // (the kernels cap lengths by this product)
     if (!(cfg->sm_scale >= 0.f) || !std::isfinite(cfg->sm_scale)) return CHESS_EINVAL;
     if (cfg->summary_dtype != CHESS_SUMMARY_F32 && cfg->summary_dtype != CHESS_SUMMARY_BF16) return CHESS_EINVAL;
 
