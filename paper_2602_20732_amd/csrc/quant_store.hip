@@ -7,8 +7,8 @@
 // Values are token-minor in a page: a lane reads the same two (pages of 32: four) dims of 16 tokens and so has 16 bytes of each of the rows
 // [dim][token] that it writes, without an exchange.
 // Bound: HBM (2 bytes read, 1 written an element); for single tokens the chain entry -> rows -> store and the length of the code that runs once.
-// us: 24K tokens, 8 KV heads, pages of 16 31.8 (4.8 TB/s, what a copy of 2 GiB reaches), 64K, 4 heads, of 32 45.4 (4.4); a token of 32 sequences,
-// 8 heads, 4.3.  Rows not read as a stream: 36.3 and 50.8.  The values' conversion unrolled over dims: the tokens 4.7.
+// us in a graph: 24K tokens, 8 KV heads, pages of 16 32.3 (4.75 TB/s; a copy of 2 GiB reaches 4.8 to 5.0), 64K, 4 heads, of 32 45.3 (4.45); a token of 32
+// sequences, 8 heads, 4.4.  Rows not read as a stream: 36.3 and 50.8.  The values' conversion unrolled over dims: the tokens 4.7.
 #include "chess_internal.h"
 #include "quant_device.h"
 #include "split_rule.h"

@@ -111,8 +111,8 @@ inline SplitShape choose_splits(const SplitLimits& c, int batch, int64_t max_lis
 }
 
 // The same for 8-bit pages (tiles of 64 tokens, c.tile_pages pages each; c.resident: four-wave workgroups of attention over every page that
-// fit at once).  Lists and batches go by the rules above, which their own sweeps bear out: lists within 3 % of the best of 2 .. 64 splits of four or
-// eight waves, within 6 % of it for 24 rows of 500 pages.  Every page of one sequence: eight waves, at most one workgroup to a compute unit, since each
+// fit at once).  Lists go by the rules above, which their own sweeps bear out: within 3 % of the best of 2 .. 64 splits of four or
+// eight waves, within 6 % of it for 24 rows of 500 pages.  Every page has rules of its own.  One sequence: eight waves, at most one workgroup to a compute unit, since each
 // reads as fast alone as two do (us, 262139 tokens, 4 KV heads, G = 7: 64 splits, 256 workgroups, 58; 68, which is 272, 80; 128 76); fewer where the
 // partials outweigh the tiles, in which the merge by twice the threads counts when they have outputs (more than four heads).  us, eight waves:
 //   2048 tokens, 8 KV heads, G = 4       8 splits  6.9   16  7.3   24  8.3   32  8.7         32768   16 splits 19.0   24 17.6   32 17.3
