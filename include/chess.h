@@ -368,7 +368,7 @@ int chess_release_pages(chess_ctx* ctx, const int32_t* seq_lens, const int32_t* 
  * new_lens: device int32 [batch], the tokens each sequence wants behind the seq_lens[b] it holds (<= 0: none).  A sequence whose row has no room
  * (length + tokens above max_pages_per_seq * page_size, or a negative length) gets nothing; otherwise sequences are served in order
  * as long as their tokens add up to at most max_tokens and the new pages to at most *n_free: the first that does not fit and all behind it get
- * nothing.  Pages are taken from the end of free_pages.  Written:
+ * nothing.  Pages are taken from the end of free_pages, which holds at least the *n_free entries that are said to be in use.  Written:
  *   block_table  the entries of the new pages (nothing else of it)
  *   lens_after   int32 [batch]       seq_lens plus the tokens that a sequence got
  *   n_left       int32               *n_free minus the pages taken (free_pages itself is not changed)
