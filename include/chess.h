@@ -6,8 +6,8 @@
  * in place (no KV copy, only page indices change: Sec. 1, Sec. 4.1, App. B "Zero-Copy Logic").
  *
  * C ABI.  Every data pointer is a DEVICE pointer owned by the caller unless it says "host".
- * The library never allocates or frees device memory; only chess_append_kv and chess_reuse_step write the K/V
- * pools (the appended token's rows, nothing else), and only chess_quant_store and its bounded form 8-bit pools.  Every call is
+ * The library never allocates or frees device memory; only chess_append_kv, chess_reuse_step and chess_rotate_store write the K/V
+ * pools (the new tokens' rows, nothing else), and only chess_quant_store and its bounded form 8-bit pools.  Every call is
  * asynchronous on `stream` (a hipStream_t passed as void*, NULL = the default stream), does no
  * host synchronisation, and can be captured in a HIP graph.  A context caches launch shapes: calls on one
  * context must not run concurrently from several host threads (use one context per thread).
@@ -157,7 +157,7 @@ int chess_summarize(chess_ctx* ctx, const void* k_pool, const int32_t* block_tab
  * position seq_lens[b] of sequence b -- K row-major in its page, V token-minor -- through the block table, which
  * must already map that page.  seq_lens holds the lengths BEFORE the append and is not changed (the caller adds
  * one); a sequence with no room left (seq_lens[b] >= max_pages_per_seq * page_size) or a negative length is
- * skipped.  The only call that writes the pools.  Follow it with chess_summarize_tail (or chess_decode_step
+ * skipped.  (Many tokens at once: chess_rotate_store.)  Follow it with chess_summarize_tail (or chess_decode_step
  * with refresh_tail) on the new lengths to bring the summaries up to date.
  * page_ids / n_selected (both or neither; may be NULL): the lists that are being reused are extended in the same
  * launch as chess_extend_window would for the lengths after the append.
@@ -424,6 +424,111 @@ int chess_quant_sparse_decode(chess_ctx* ctx, const void* q, const void* k_pool,
                               int32_t batch, float* out, void* workspace, void* stream);
 int chess_quant_dense_decode(chess_ctx* ctx, const void* q, const void* k_pool, const void* v_pool, const float* scales,
                              const int32_t* block_table, const int32_t* seq_lens, int32_t batch, float* out, void* workspace, void* stream);
+
+/*
+ * ---- Several tokens of a sequence in a step ------------------------------------------------------------------------
+ * Prompts, and drafted tokens that the model is to verify: chess_map_tokens deals their pages, chess_rotate_store makes their queries and fills the
+ * pages, chess_dense_attend / chess_sparse_attend attend with every new token as a query of its own, chess_verify says how many drafts stand and
+ * chess_trim_pages takes back the pages of the others.  token_start: int32 [batch + 1] as chess_map_tokens writes it; the rows of sequence b are
+ * token_start[b] .. token_start[b + 1] - 1, in the order of their positions.  A sequence for which it names rows that are not there has none.
+ * All these calls: CHESS_EINVAL on null or misaligned pointers (16 bytes for rows, pools and workspaces), sizes outside the configuration, or when
+ * the context's device is not the current one; CHESS_ENOTSUP for more work than one launch holds.
+ */
+
+/* How queries and keys are normed and turned.  A host struct; the pointers are device pointers. */
+typedef struct {
+    const float* inv_freq;   /* fp32 [rotary_dim / 2]: radians a position, of each pair of dims                               */
+    const float* q_norm;     /* fp32 weights of the queries' norm, or NULL: queries are not normed                            */
+    const float* k_norm;     /* ... of the keys'                                                                             */
+    int32_t rotary_dim;      /* dims of a head that turn: the first ones; a multiple of 16 from 16 to 128                     */
+    int32_t interleaved;     /* pair i is 0: dims i and i + rotary_dim / 2; 1: dims 2 i and 2 i + 1                          */
+    int32_t norm_per_head;   /* weights are 0: [128], the same for every head; 1: [heads][128]                               */
+    int32_t n_axes;          /* rows of `positions`, 1 to 4                                                                  */
+    uint8_t axis[64];        /* which of them turns pair i (text: 0; time, height, width of a patch: 0, 1, 2)                */
+    float   eps;             /* of the norms                                                                                  */
+    float   scale;           /* factor on sine and cosine; 0 means 1                                                         */
+} chess_rotary;
+
+/*
+ * q: bf16 [n_rows][n_q_heads][128], k: bf16 [n_rows][H_kv][128], q_stride / k_stride elements from a row to the next (>= the row, multiples of 8:
+ * slices of a wider projection will do).  Per head y = x / sqrt(mean x^2 + eps) * weight, then each pair (a, b) of y at the angle
+ * t = positions[axis of the pair][row] * inv_freq becomes (a cos t - b sin t, a sin t + b cos t) * scale; dims behind rotary_dim stay y.  fp32
+ * from the inputs to the one rounding to bf16 (a norm's sum of squares too), angles in fp64.  positions: int32 [n_axes][n_rows].
+ * q_out: bf16 [n_rows][n_q_heads][128], k_out: bf16 [n_rows][H_kv][128].  q may be NULL (keys only) and k may be (queries only).  counts (or NULL): as
+ * chess_map_tokens leaves it; rows from counts[0] on are left as they are.  An output may be its own input where that is contiguous; no other overlap.
+ */
+int chess_rotate(chess_ctx* ctx, const chess_rotary* rotary, const void* q, int64_t q_stride, const void* k, int64_t k_stride,
+                 const int32_t* positions, int32_t n_rows, const int32_t* counts, void* q_out, void* k_out, void* stream);
+
+/*
+ * The same for rows that chess_map_tokens dealt pages to (writes, counts: as it leaves them; only counts[1] is read; max_writes: the entries `writes` has
+ * room for), with the keys and the values (bf16 [n_rows][H_kv][128], v_stride as k_stride; values are neither normed nor turned) stored in the
+ * bf16 pools of n_pages pages.  Only rows that an entry names are written, in q_out too.  An entry with a row or a page that is not there does nothing.
+ * No two entries may name the same page.  q may be NULL.
+ */
+int chess_rotate_store(chess_ctx* ctx, const chess_rotary* rotary, const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v,
+                       int64_t v_stride, const int32_t* positions, int32_t n_rows, const int32_t* writes, const int32_t* counts, int32_t max_writes,
+                       void* q_out, void* k_pool, void* v_pool, int32_t n_pages, void* stream);
+
+/* What a query sees and how a score is formed.  A host struct (NULL: causal order and nothing else); the pointers are device pointers. */
+typedef struct {
+    float   cap;                  /* > 0: a score s = sm_scale q . k becomes cap tanh(s / cap); 0: it stays               */
+    int32_t window;               /* > 0: a token at position p sees no key before p - window + 1                         */
+    const float*   slopes;        /* fp32 [n_q_heads]: slope |p - t| is taken from the (capped) score of key t; or NULL   */
+    const int32_t* prefix_lens;   /* int32 [batch]: the first prefix_lens[b] keys are seen by every row; or NULL          */
+    const int32_t* first_keys;    /* int32 [n_rows]: the first key that a row sees (where its document starts); or NULL   */
+} chess_scores;
+
+/* Bytes of the scratch that the two calls below need for up to so many rows, new tokens of one sequence and sequences.  Nothing has to be in it, and
+ * nothing is left in it; calls that share one must not overlap in time. */
+int chess_attend_scratch_bytes(const chess_ctx* ctx, int32_t n_rows, int32_t max_new, int32_t batch, size_t* bytes);
+
+/*
+ * seq_lens: the lengths WITH the new tokens, which are a sequence's last (chess_map_tokens' lens_after); max_new: no sequence has more of them (host
+ * value; rows beyond are not attended).  q, out: bf16 [n_rows][n_q_heads][128].  The row of the token at position p attends to the keys t of its
+ * sequence with t <= p or t < prefix_lens[b], t >= first_keys[row], t > p - window; a row that sees no key is 0.  Keys that a row does not see do not
+ * touch it, whatever they or their values are.  bf16 in and out; scores, softmax and sums in fp32 (weights are rounded to bf16 where the
+ * keys are shared by more rows than a few: see attend.hip), distances p - t in fp32.  Scores may have any size that fp32 holds.
+ * workspace: as elsewhere (arrival counters); scratch: chess_attend_scratch_bytes at least, 256-byte aligned.  The same batch gives the same bits on every call.
+ */
+int chess_dense_attend(chess_ctx* ctx, const chess_scores* scores, const void* q, int32_t n_rows, const int32_t* token_start, int32_t max_new,
+                       const void* k_pool, const void* v_pool, const int32_t* block_table, const int32_t* seq_lens, int32_t batch, void* out,
+                       void* workspace, void* scratch, size_t scratch_bytes, void* stream);
+
+/* The same over the keys of the listed pages only (page_ids, n_selected as for chess_sparse_decode; entries that are no page of the sequence count for
+ * nothing).  Lists for drafted tokens hold the pages of the new tokens: chess_extend_window on the lengths with them adds these. */
+int chess_sparse_attend(chess_ctx* ctx, const chess_scores* scores, const void* q, int32_t n_rows, const int32_t* token_start, int32_t max_new,
+                        const void* k_pool, const void* v_pool, const int32_t* block_table, const int32_t* seq_lens, const int32_t* page_ids,
+                        const int32_t* n_selected, int32_t batch, void* out, void* workspace, void* scratch, size_t scratch_bytes, void* stream);
+
+/*
+ * Drafted tokens against the target's probabilities, with given random numbers.  A sequence's first new token is one that stands already, those
+ * behind it are its drafts 0, 1, ...: tokens int32 [n_rows].  target: fp32 [n_rows][vocab], target_stride elements from a row to the
+ * next; row i of a sequence is the distribution of the token behind its i-th new one.  draft: fp32, the distribution that draft j of sequence b was
+ * drawn from at draft + b draft_seq + j draft_row; NULL: drafts came without probabilities (as if each had been certain).  uniforms: fp32
+ * [batch][max_drafts + 1] in [0, 1).  Only the first max_drafts drafts of a sequence are looked at; those behind count as refused.
+ *   draft j = x stands while  uniforms[b][j] q_j(x) < p_j(x)  (an x outside [0, vocab) does not);
+ *   the token behind the last that stands is the first v with w(0) + ... + w(v) > uniforms[b][max_drafts] W, W the sum of w, where
+ *   w(v) = max(p(v) - q(v), 0) if a draft was refused (p(v) without the draft itself where draft is NULL), p(v) if none was;
+ *   if a draft was refused and nothing is left over (W = 0), w = p; -1 if p too has no sum above 0, or W or it is infinite.  What is NaN or negative weighs nothing.
+ * Products and sums in fp64; the same row and numbers give the same token in every batch.  Written:
+ *   n_accepted int32 [batch]                drafts that stand
+ *   out_tokens int32 [batch][max_drafts+1]  those, the token drawn, -1 behind it (a sequence without new tokens: -1 only)
+ *   lens_after int32 [batch]                seq_lens (with all new tokens) less the refused drafts; may be seq_lens
+ */
+int chess_verify(chess_ctx* ctx, const float* target, int64_t target_stride, const float* draft, int64_t draft_seq, int64_t draft_row, int32_t vocab,
+                 const int32_t* tokens, int32_t n_rows, const int32_t* token_start, const float* uniforms, int32_t max_drafts,
+                 const int32_t* seq_lens, int32_t batch, int32_t* n_accepted, int32_t* out_tokens, int32_t* lens_after, void* workspace,
+                 void* stream);
+
+/*
+ * The pages that sequences of seq_lens tokens hold behind the first keep_lens of them go back to the free list, in sequence and logical order, as
+ * chess_release_pages does with ended sequences; the block table is not changed.  Without this call the pages of refused drafts would be lost: the
+ * next chess_map_tokens maps new ones in their place.  keep_lens[b] >= seq_lens[b]: nothing of that sequence.  Should the list be too short for a
+ * sequence's pages, they and those of the sequences behind it are left out of it (a list with room for every page never is).  n_left may be n_free.
+ */
+int chess_trim_pages(chess_ctx* ctx, const int32_t* seq_lens, const int32_t* keep_lens, int32_t batch, const int32_t* block_table, int32_t* free_pages,
+                     int32_t capacity, const int32_t* n_free, int32_t* n_left, void* workspace, void* stream);
 
 const char* chess_strerror(int code);
 int chess_version(void);

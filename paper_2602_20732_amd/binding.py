@@ -24,6 +24,8 @@ EXPORTS = ["chess_create", "chess_destroy", "chess_summary_bytes", "chess_summar
            "chess_summarize", "chess_summarize_tail", "chess_summarize_recent", "chess_append_kv", "chess_select", "chess_anchor", "chess_select_shared", "chess_entropy", "chess_trigger_update", "chess_monitor_step", "chess_extend_window", "chess_reuse_step", "chess_sparse_decode", "chess_sparse_decode_static", "chess_dense_decode", "chess_decode_step",
            "chess_write_rows", "chess_release_pages", "chess_map_tokens", "chess_quant_store", "chess_quant_store_bounded", "chess_quant_summarize",
            "chess_quant_sparse_decode", "chess_quant_dense_decode",
+           "chess_rotate", "chess_rotate_store", "chess_attend_scratch_bytes", "chess_dense_attend", "chess_sparse_attend", "chess_verify",
+           "chess_trim_pages",
            "chess_debug_force_splits", "chess_debug_force_cluster", "chess_debug_force_schedule", "chess_debug_force_general_cut", "chess_debug_set_poll_limit", "chess_workspace_error", "chess_strerror", "chess_version"]
 
 
@@ -43,6 +45,16 @@ class _CPlan(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in
                 ("plan", "sink_pages", "window_pages", "budget_pages", "budget_bp", "over_chunk", "over_grid",
                  "rho_g_bp", "rho_c_bp", "rho_p_bp", "probe", "cut_rule")] + [("budget_per_seq", ctypes.c_void_p)]
+
+
+class _CRotary(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("inv_freq", "q_norm", "k_norm")] + [
+        (n, ctypes.c_int32) for n in ("rotary_dim", "interleaved", "norm_per_head", "n_axes")] + [
+        ("axis", ctypes.c_uint8 * 64), ("eps", ctypes.c_float), ("scale", ctypes.c_float)]
+
+
+class _CScores(ctypes.Structure):
+    _fields_ = [("cap", ctypes.c_float), ("window", ctypes.c_int32)] + [(n, ctypes.c_void_p) for n in ("slopes", "prefix_lens", "first_keys")]
 
 
 @dataclass(frozen=True)
@@ -82,6 +94,40 @@ class SelectPlan:
         return _CPlan(self.plan, self.sink_pages, self.window_pages, self.budget_pages, self.budget_bp,
                       self.over_chunk, self.over_grid, self.rho_g_bp, self.rho_c_bp, self.rho_p_bp, self.probe,
                       self.cut_rule, per)
+
+
+class Rotary:
+    """How queries and keys are normed and turned (``chess_rotary``); holds its tensors.
+
+    inv_freq: device fp32 [rotary_dim / 2]; axis: for each pair the row of ``positions`` that turns it (None: row 0); q_norm, k_norm: device fp32
+    [128], or [heads, 128] both, or None; interleaved: pairs are neighbours."""
+
+    def __init__(self, inv_freq, axis=None, interleaved: bool = False, q_norm=None, k_norm=None, eps: float = 1e-6, scale: float = 1.0):
+        pairs = inv_freq.numel()
+        axis = [0] * pairs if axis is None else [int(i) for i in axis]
+        if len(axis) != pairs or pairs > 64 or min(axis, default=0) < 0 or max(axis, default=0) > 3:
+            raise ChessError(f"axis: one of 0 to 3 for each of at most 64 pairs is wanted, got {axis} for {pairs}")
+        if q_norm is not None and k_norm is not None and q_norm.dim() != k_norm.dim():
+            raise ChessError(f"q_norm, k_norm: weights a head, or for all heads, in both, got {tuple(q_norm.shape)} and {tuple(k_norm.shape)}")
+        if scale == 0:
+            raise ChessError("scale: not 0")
+        self.inv_freq, self.q_norm, self.k_norm = inv_freq, q_norm, k_norm
+        self.n_axes = max(axis, default=0) + 1
+        self.per_head = any(t is not None and t.dim() == 2 for t in (q_norm, k_norm))
+        self._c = _CRotary(inv_freq.data_ptr(), _ptr(q_norm), _ptr(k_norm), 2 * pairs, int(bool(interleaved)), int(self.per_head), self.n_axes,
+                           (ctypes.c_uint8 * 64)(*axis), eps, scale)
+        self._ref = ctypes.byref(self._c)
+
+
+class Scores:
+    """What a query sees and how a score is formed (``chess_scores``); holds its tensors.
+
+    slopes: device fp32 [n_q_heads]; prefix_lens: device int32 [batch]; first_keys: device int32 [rows]; each or None."""
+
+    def __init__(self, cap: float = 0.0, slopes=None, window: int = 0, prefix_lens=None, first_keys=None):
+        self.slopes, self.prefix_lens, self.first_keys = slopes, prefix_lens, first_keys
+        self._c = _CScores(cap, window, _ptr(slopes), _ptr(prefix_lens), _ptr(first_keys))
+        self._ref = ctypes.byref(self._c)
 
 
 def library_path() -> str:
@@ -130,6 +176,14 @@ def load_library() -> ctypes.CDLL:
         lib.chess_quant_summarize.argtypes = [vp, vp, vp, i32p, i32p, ctypes.c_int32, i32p, ctypes.c_int32, vp, vp]
         lib.chess_quant_sparse_decode.argtypes = [vp, vp, vp, vp, vp, i32p, i32p, i32p, i32p, ctypes.c_int32, vp, vp, vp]
         lib.chess_quant_dense_decode.argtypes = [vp, vp, vp, vp, vp, i32p, i32p, ctypes.c_int32, vp, vp, vp]
+        i32, i64 = ctypes.c_int32, ctypes.c_int64
+        lib.chess_rotate.argtypes = [vp, vp, vp, i64, vp, i64, i32p, i32, i32p, vp, vp, vp]
+        lib.chess_rotate_store.argtypes = [vp, vp, vp, i64, vp, i64, vp, i64, i32p, i32, i32p, i32p, i32, vp, vp, vp, i32, vp]
+        lib.chess_attend_scratch_bytes.argtypes = [vp, i32, i32, i32, ctypes.POINTER(ctypes.c_size_t)]
+        lib.chess_dense_attend.argtypes = [vp, vp, vp, i32, i32p, i32, vp, vp, i32p, i32p, i32, vp, vp, vp, ctypes.c_size_t, vp]
+        lib.chess_sparse_attend.argtypes = [vp, vp, vp, i32, i32p, i32, vp, vp, i32p, i32p, i32p, i32p, i32, vp, vp, vp, ctypes.c_size_t, vp]
+        lib.chess_verify.argtypes = [vp, vp, i64, vp, i64, i64, i32, i32p, i32, i32p, vp, i32, i32p, i32, i32p, i32p, i32p, vp, vp]
+        lib.chess_trim_pages.argtypes = [vp, i32p, i32p, i32, i32p, i32p, i32, i32p, i32p, vp, vp]
         lib.chess_debug_force_splits.argtypes = [vp, ctypes.c_int32, ctypes.c_int32]
         lib.chess_debug_force_cluster.argtypes = [vp, ctypes.c_int32]
         lib.chess_debug_force_general_cut.argtypes = [vp, ctypes.c_int32]
@@ -433,6 +487,177 @@ class Chess:
         self._check(self.lib.chess_quant_dense_decode(self._h, q.data_ptr(), k_pool.data_ptr(), v_pool.data_ptr(), scales.data_ptr(),
                                                       block_table.data_ptr(), seq_lens.data_ptr(), batch, out.data_ptr(), workspace.data_ptr(),
                                                       torch._C._cuda_getCurrentRawStream(dev)))
+
+    # ---- several tokens of a sequence in a step
+    def _need_rows(self, t, name, heads, n, dev):
+        """bf16 [n, heads, 128] whose token rows are contiguous; the stride from one to the next."""
+        d = self.cfg.head_dim
+        if (t.dtype is not torch.bfloat16 or t.dim() != 3 or t.size(0) != n or t.size(1) != heads or t.size(2) != d or t.stride(2) != 1 or
+                (t.stride(1) != d and heads > 1) or t.get_device() != dev):
+            raise ChessError(f"{name}: a bf16 tensor [{n}, {heads}, {d}] on the context's device with contiguous token rows is wanted, "
+                             f"got {t.dtype} {tuple(t.shape)} of strides {t.stride()} on {t.device}")
+        return t.stride(0) if n > 1 else heads * d    # (one token's stride leads nowhere)
+
+    def _need_rotary(self, rotary, positions, n, dev):
+        c = self.cfg
+        _need(rotary.inv_freq, "inv_freq", _FLOAT, 1, dev)
+        for t, name, heads in ((rotary.q_norm, "q_norm", c.n_q_heads), (rotary.k_norm, "k_norm", c.n_kv_heads)):
+            if t is not None:
+                _need(t, name, _FLOAT, c.head_dim * (heads if rotary.per_head else 1), dev)
+        _need(positions, "positions", _INT, rotary.n_axes * n, dev)
+
+    def rotate(self, rotary: Rotary, q, k, positions, q_out=None, k_out=None, counts=None):
+        """q: bf16 [rows, n_q_heads, 128] or None, k: bf16 [rows, H_kv, 128] or None (slices of a wider projection will do); positions: int32
+        [axes, rows] (or [rows] for one axis); no rows, nothing done."""
+        c, dev = self.cfg, self.device
+        if q is None and k is None:
+            raise ChessError("rotate: q or k is wanted")
+        n = (k if q is None else q).size(0)
+        q_stride = k_stride = 0
+        if q is not None:
+            q_stride = self._need_rows(q, "q", c.n_q_heads, n, dev)
+            _need(q_out, "q_out", _BF16, n * c.n_q_heads * c.head_dim, dev)
+        if k is not None:
+            k_stride = self._need_rows(k, "k", c.n_kv_heads, n, dev)
+            _need(k_out, "k_out", _BF16, n * c.n_kv_heads * c.head_dim, dev)
+        self._need_rotary(rotary, positions, n, dev)
+        if counts is not None:
+            _need(counts, "counts", _INT, 1, dev)
+        if n == 0:
+            return
+        if positions.numel() != rotary.n_axes * n:
+            raise ChessError(f"positions: [{rotary.n_axes}, {n}] is wanted, got {tuple(positions.shape)}")
+        self._check(self.lib.chess_rotate(self._h, rotary._ref, _ptr(q), q_stride, _ptr(k), k_stride, positions.data_ptr(), n, _ptr(counts),
+                                          None if q is None else q_out.data_ptr(), None if k is None else k_out.data_ptr(),
+                                          torch._C._cuda_getCurrentRawStream(dev)))
+
+    def rotate_store(self, rotary: Rotary, q, k_new, v_new, positions, writes, counts, q_out, k_pool, v_pool):
+        """q: bf16 [rows, n_q_heads, 128] or None (with q_out), k_new / v_new: bf16 [rows, H_kv, 128] (slices of a wider projection will do); no
+        rows, nothing stored.  An entry that names a row or a page beyond these tensors does nothing."""
+        c, dev = self.cfg, self.device
+        n, H, d, B = k_new.size(0), c.n_kv_heads, c.head_dim, c.page_size
+        k_stride, v_stride, q_stride = self._need_rows(k_new, "k_new", H, n, dev), self._need_rows(v_new, "v_new", H, n, dev), 0
+        if q is not None:
+            q_stride = self._need_rows(q, "q", c.n_q_heads, n, dev)
+            _need(q_out, "q_out", _BF16, n * c.n_q_heads * d, dev)
+        self._need_rotary(rotary, positions, n, dev)
+        _need(writes, "writes", _INT, 4, dev)
+        _need(counts, "counts", _INT, 2, dev)
+        _need(k_pool, "k_pool", _BF16, H * B * d, dev)
+        _need(v_pool, "v_pool", _BF16, H * B * d, dev)
+        if k_pool.numel() != v_pool.numel():
+            raise ChessError(f"k_pool, v_pool: {k_pool.numel()} and {v_pool.numel()} values are not of the same pages")
+        if n == 0:
+            return
+        if positions.numel() != rotary.n_axes * n:
+            raise ChessError(f"positions: [{rotary.n_axes}, {n}] is wanted, got {tuple(positions.shape)}")
+        self._check(self.lib.chess_rotate_store(self._h, rotary._ref, _ptr(q), q_stride, k_new.data_ptr(), k_stride, v_new.data_ptr(), v_stride,
+                                                positions.data_ptr(), n, writes.data_ptr(), counts.data_ptr(), writes.numel() // 4,
+                                                None if q is None else q_out.data_ptr(), k_pool.data_ptr(), v_pool.data_ptr(),
+                                                k_pool.numel() // (H * B * d), torch._C._cuda_getCurrentRawStream(dev)))
+
+    def attend_scratch_bytes(self, n_rows: int, max_new: int, batch: int) -> int:
+        n = ctypes.c_size_t()
+        self._check(self.lib.chess_attend_scratch_bytes(self._h, n_rows, max_new, batch, ctypes.byref(n)))
+        return n.value
+
+    def new_attend_scratch(self, n_rows: int, max_new: int, batch: int, device="cuda") -> torch.Tensor:
+        return torch.empty(self.attend_scratch_bytes(n_rows, max_new, batch), dtype=torch.uint8, device=device)
+
+    def _need_attend(self, q, token_start, k_pool, v_pool, block_table, seq_lens, out, workspace, scratch, scores, batch, dev):
+        c = self.cfg
+        n = q.size(0)
+        values = n * c.n_q_heads * c.head_dim
+        if q.dim() != 3:
+            raise ChessError(f"q: [rows, {c.n_q_heads}, {c.head_dim}] is wanted, got {tuple(q.shape)}")
+        _need(q, "q", _BF16, values, dev)
+        _need(out, "out", _BF16, values, dev)
+        _need(token_start, "token_start", _INT, batch + 1, dev)
+        page = c.n_kv_heads * c.page_size * c.head_dim
+        _need(k_pool, "k_pool", _BF16, page, dev)
+        _need(v_pool, "v_pool", _BF16, page, dev)
+        _need(block_table, "block_table", _INT, batch * c.max_pages_per_seq, dev)
+        _need(seq_lens, "seq_lens", _INT, batch, dev)
+        _need(workspace, "workspace", _BYTE, self.workspace_bytes, dev)
+        _need(scratch, "scratch", _BYTE, 1, dev)
+        if scores is not None:
+            if scores.slopes is not None:
+                _need(scores.slopes, "slopes", _FLOAT, c.n_q_heads, dev)
+            if scores.prefix_lens is not None:
+                _need(scores.prefix_lens, "prefix_lens", _INT, batch, dev)
+            if scores.first_keys is not None:
+                _need(scores.first_keys, "first_keys", _INT, n, dev)
+        if q.size(1) != c.n_q_heads or q.size(2) != c.head_dim:
+            raise ChessError(f"q: [rows, {c.n_q_heads}, {c.head_dim}] is wanted, got {tuple(q.shape)}")
+        return n
+
+    def dense_attend(self, q, token_start, max_new: int, k_pool, v_pool, block_table, seq_lens, out, workspace, scratch, scores: Scores = None):
+        """q, out: bf16 [rows, n_q_heads, 128]; scratch: of new_attend_scratch for as many rows, new tokens of a sequence and sequences; no rows, nothing done."""
+        batch, dev = seq_lens.numel(), self.device
+        n = self._need_attend(q, token_start, k_pool, v_pool, block_table, seq_lens, out, workspace, scratch, scores, batch, dev)
+        if n == 0:
+            return
+        self._check(self.lib.chess_dense_attend(self._h, None if scores is None else scores._ref, q.data_ptr(), n, token_start.data_ptr(), max_new,
+                                                k_pool.data_ptr(), v_pool.data_ptr(), block_table.data_ptr(), seq_lens.data_ptr(), batch,
+                                                out.data_ptr(), workspace.data_ptr(), scratch.data_ptr(), scratch.numel(),
+                                                torch._C._cuda_getCurrentRawStream(dev)))
+
+    def sparse_attend(self, q, token_start, max_new: int, k_pool, v_pool, block_table, seq_lens, page_ids, n_selected, out, workspace, scratch,
+                      scores: Scores = None):
+        batch, dev = seq_lens.numel(), self.device
+        n = self._need_attend(q, token_start, k_pool, v_pool, block_table, seq_lens, out, workspace, scratch, scores, batch, dev)
+        _need(page_ids, "page_ids", _INT, batch * self.cfg.n_kv_heads * self.cfg.max_selected_pages, dev)
+        _need(n_selected, "n_selected", _INT, batch * self.cfg.n_kv_heads, dev)
+        if n == 0:
+            return
+        self._check(self.lib.chess_sparse_attend(self._h, None if scores is None else scores._ref, q.data_ptr(), n, token_start.data_ptr(), max_new,
+                                                 k_pool.data_ptr(), v_pool.data_ptr(), block_table.data_ptr(), seq_lens.data_ptr(),
+                                                 page_ids.data_ptr(), n_selected.data_ptr(), batch, out.data_ptr(), workspace.data_ptr(),
+                                                 scratch.data_ptr(), scratch.numel(), torch._C._cuda_getCurrentRawStream(dev)))
+
+    def verify(self, target, draft, tokens, token_start, uniforms, seq_lens, n_accepted, out_tokens, lens_after, workspace):
+        """target: fp32 [rows, vocab]; draft: fp32 [batch, at least max_drafts, vocab] or None (words of a row next to one another in both; rows may be
+        slices of wider ones); tokens: int32 [rows]; uniforms: fp32 [batch, max_drafts + 1]."""
+        batch, dev = seq_lens.numel(), self.device
+        if uniforms.dim() != 2 or uniforms.size(0) != batch or uniforms.size(1) < 1:
+            raise ChessError(f"uniforms: [{batch}, max_drafts + 1] is wanted, got {tuple(uniforms.shape)}")
+        if target.dim() != 2 or target.dtype is not torch.float32 or target.stride(1) != 1 and target.size(1) > 1 or target.get_device() != dev or target.size(0) < 1:
+            raise ChessError(f"target: an fp32 tensor [rows, vocab] with contiguous rows on the context's device is wanted, got {target.dtype} "
+                             f"{tuple(target.shape)} of strides {target.stride()} on {target.device}")
+        n, vocab = target.shape
+        most = uniforms.size(1) - 1
+        draft_seq = draft_row = 0
+        if draft is not None:
+            if (draft.dim() != 3 or draft.dtype is not torch.float32 or draft.size(0) != batch or draft.size(1) < most or draft.size(2) != vocab or
+                    draft.stride(2) != 1 and vocab > 1 or draft.get_device() != dev):
+                raise ChessError(f"draft: an fp32 tensor [{batch}, {most}, {vocab}] with contiguous rows on the context's device is wanted, got {draft.dtype} "
+                                 f"{tuple(draft.shape)} of strides {draft.stride()} on {draft.device}")
+            draft_seq, draft_row = (draft.stride(0) if batch > 1 else max(vocab, draft.stride(0))), (draft.stride(1) if draft.size(1) > 1 else vocab)
+        _need(tokens, "tokens", _INT, n, dev)
+        _need(token_start, "token_start", _INT, batch + 1, dev)
+        _need(uniforms, "uniforms", _FLOAT, batch * (most + 1), dev)
+        _need(seq_lens, "seq_lens", _INT, batch, dev)
+        _need(n_accepted, "n_accepted", _INT, batch, dev)
+        _need(out_tokens, "out_tokens", _INT, batch * (most + 1), dev)
+        _need(lens_after, "lens_after", _INT, batch, dev)
+        _need(workspace, "workspace", _BYTE, self.workspace_bytes, dev)
+        self._check(self.lib.chess_verify(self._h, target.data_ptr(), target.stride(0) if n > 1 else vocab, _ptr(draft), draft_seq, draft_row, vocab,
+                                          tokens.data_ptr(), n, token_start.data_ptr(), uniforms.data_ptr(), most, seq_lens.data_ptr(), batch,
+                                          n_accepted.data_ptr(), out_tokens.data_ptr(), lens_after.data_ptr(), workspace.data_ptr(),
+                                          torch._C._cuda_getCurrentRawStream(dev)))
+
+    def trim_pages(self, seq_lens, keep_lens, block_table, free_pages, n_free, n_left, workspace):
+        batch, dev = seq_lens.numel(), self.device
+        _need(seq_lens, "seq_lens", _INT, batch, dev)
+        _need(keep_lens, "keep_lens", _INT, batch, dev)
+        _need(block_table, "block_table", _INT, batch * self.cfg.max_pages_per_seq, dev)
+        _need(free_pages, "free_pages", _INT, 1, dev)
+        _need(n_free, "n_free", _INT, 1, dev)
+        _need(n_left, "n_left", _INT, 1, dev)
+        _need(workspace, "workspace", _BYTE, self.workspace_bytes, dev)
+        self._check(self.lib.chess_trim_pages(self._h, seq_lens.data_ptr(), keep_lens.data_ptr(), batch, block_table.data_ptr(), free_pages.data_ptr(),
+                                              free_pages.numel(), n_free.data_ptr(), n_left.data_ptr(), workspace.data_ptr(),
+                                              torch._C._cuda_getCurrentRawStream(dev)))
 
     def workspace_error(self, workspace) -> int:
         flag = ctypes.c_int32()

@@ -8,7 +8,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libchess.so")
 SOURCES = ["api.hip", "summarize.hip", "select.hip", "decode.hip", "step.hip", "shared.hip", "trigger.hip", "pages.hip",
-           "quant_store.hip", "quant_summarize.hip", "quant_decode.hip"]
+           "quant_store.hip", "quant_summarize.hip", "quant_decode.hip", "rotate.hip", "attend.hip", "verify.hip"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared", "-fno-gpu-rdc",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
          # the first arguments of a kernel (as far as they are pointers and numbers, not structs) are in registers when it starts:

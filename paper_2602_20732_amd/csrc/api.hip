@@ -220,7 +220,8 @@ int chess_create(const chess_config* cfg, chess_ctx** out)
     c->ws_err_off = align_up(c->ws_cnt_off + rows * chess::kArrivalStride * sizeof(int32_t), 256);
     c->ws_ent_off = align_up(c->ws_err_off + 256, 256);
     c->ws_entcnt_off = align_up(c->ws_ent_off + (size_t)cfg->max_batch * chess::kEntMaxSplits * 4 * sizeof(float), 256);
-    c->workspace_bytes = align_up(c->ws_entcnt_off + (size_t)cfg->max_batch * chess::kArrivalStride * sizeof(int32_t), 256);
+    c->ws_ver_off = align_up(c->ws_entcnt_off + (size_t)cfg->max_batch * chess::kArrivalStride * sizeof(int32_t), 256);
+    c->workspace_bytes = align_up(c->ws_ver_off + (size_t)cfg->max_batch * chess::kVerPieces * sizeof(double), 256);
     c->dense_blocks = 2;
     if (chess::dense_occupancy(g.page_size, g.group, &v) == hipSuccess && v > 0) c->dense_blocks = v;
     c->quant_blocks = 2;
@@ -843,6 +844,170 @@ int chess_quant_dense_decode(chess_ctx* ctx, const void* q, const void* k_pool, 
                              const int32_t* block_table, const int32_t* seq_lens, int32_t batch, float* out, void* workspace, void* stream)
 {
     return quant_decode_common(ctx, q, k_pool, v_pool, scales, block_table, seq_lens, nullptr, nullptr, batch, out, workspace, stream);
+}
+
+static int rotate_common(chess_ctx* ctx, const chess_rotary* rot, chess::RotateArgs a, bool paged, void* stream)
+{
+    if (!rot || !rot->inv_freq || !a.positions || a.n_rows < 1 || a.n_rows > CHESS_MAX_TOKENS) return CHESS_EINVAL;
+    if ((a.q != nullptr) != (a.q_out != nullptr) || (a.k != nullptr) != (a.k_out != nullptr) || (!a.q && !a.k)) return CHESS_EINVAL;
+    const int64_t q_row = (int64_t)ctx->geom.n_q_heads * kHeadDim, kv_row = (int64_t)ctx->geom.n_kv_heads * kHeadDim;
+    if (a.q && (a.q_stride < q_row || (a.q_stride & 7))) return CHESS_EINVAL;
+    if (a.k && (a.k_stride < kv_row || (a.k_stride & 7))) return CHESS_EINVAL;
+    if (rot->rotary_dim < 16 || rot->rotary_dim > kHeadDim || rot->rotary_dim % 16 != 0 || rot->n_axes < 1 || rot->n_axes > 4) return CHESS_EINVAL;
+    if (!(rot->eps >= 0.f) || !std::isfinite(rot->eps) || !std::isfinite(rot->scale)) return CHESS_EINVAL;
+    if (misaligned({a.q, a.k, a.v, a.q_out, a.k_out, a.v_pool, a.writes}, 15) || misaligned({rot->inv_freq, rot->q_norm, rot->k_norm, a.positions, a.counts}, 3) ||
+        !on_device(ctx))
+        return CHESS_EINVAL;
+    a.pairs = rot->rotary_dim / 2;
+    for (int i = 0; i < a.pairs; ++i) {
+        if (rot->axis[i] >= rot->n_axes) return CHESS_EINVAL;
+        (i < 32 ? a.axis_lo : a.axis_hi) |= (uint64_t)rot->axis[i] << (2 * (i & 31));
+    }
+    a.inv_freq = rot->inv_freq;
+    a.q_norm = rot->q_norm;
+    a.k_norm = rot->k_norm;
+    a.norm_stride = rot->norm_per_head ? kHeadDim : 0;
+    a.eps = rot->eps;
+    a.scale = rot->scale == 0.f ? 1.f : rot->scale;
+    a.position_stride = a.n_rows;
+    a.q_heads = ctx->geom.n_q_heads;
+    a.kv_heads = ctx->geom.n_kv_heads;
+    const chess::RotateShape s = chess::rotate_shape(ctx, a, paged);
+    if (s.units * s.parts > (1 << 24) - 1) return CHESS_ENOTSUP;            // (a launch has fewer than 2^32 threads: 256 of these)
+    return chess::launch_rotate(ctx, a, paged, rot->interleaved != 0, static_cast<hipStream_t>(stream)) == hipSuccess ? CHESS_OK : CHESS_EHIP;
+}
+
+int chess_rotate(chess_ctx* ctx, const chess_rotary* rotary, const void* q, int64_t q_stride, const void* k, int64_t k_stride,
+                 const int32_t* positions, int32_t n_rows, const int32_t* counts, void* q_out, void* k_out, void* stream)
+{
+    if (!ctx) return CHESS_EINVAL;
+    chess::RotateArgs a{};
+    a.q = static_cast<const uint16_t*>(q); a.q_stride = q_stride; a.q_out = static_cast<uint16_t*>(q_out);
+    a.k = static_cast<const uint16_t*>(k); a.k_stride = k_stride; a.k_out = static_cast<uint16_t*>(k_out);
+    a.positions = positions; a.n_rows = n_rows; a.counts = counts;
+    return rotate_common(ctx, rotary, a, false, stream);
+}
+
+int chess_rotate_store(chess_ctx* ctx, const chess_rotary* rotary, const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v,
+                       int64_t v_stride, const int32_t* positions, int32_t n_rows, const int32_t* writes, const int32_t* counts, int32_t max_writes,
+                       void* q_out, void* k_pool, void* v_pool, int32_t n_pages, void* stream)
+{
+    if (!ctx || !k || !v || !writes || !counts || !k_pool || !v_pool || max_writes < 1 || n_pages < 1) return CHESS_EINVAL;
+    if (v_stride < (int64_t)ctx->geom.n_kv_heads * kHeadDim || (v_stride & 7)) return CHESS_EINVAL;
+    chess::RotateArgs a{};
+    a.q = static_cast<const uint16_t*>(q); a.q_stride = q_stride; a.q_out = static_cast<uint16_t*>(q_out);
+    a.k = static_cast<const uint16_t*>(k); a.k_stride = k_stride; a.k_out = static_cast<uint16_t*>(k_pool);
+    a.v = static_cast<const uint16_t*>(v); a.v_stride = v_stride; a.v_pool = static_cast<uint16_t*>(v_pool);
+    a.positions = positions; a.n_rows = n_rows;
+    a.writes = reinterpret_cast<const int4*>(writes); a.counts = counts; a.max_writes = max_writes; a.n_pages = n_pages;
+    return rotate_common(ctx, rotary, a, true, stream);
+}
+
+// Where the parts of the scratch lie; the bytes of all.
+static size_t attend_layout(const chess::AttendShape& s, size_t* ml_off)
+{
+    const size_t rows = (size_t)s.parts * s.rows;
+    *ml_off = align_up(rows * kHeadDim * sizeof(float), 256);
+    return align_up(*ml_off + rows * 2 * sizeof(float), 256);
+}
+
+int chess_attend_scratch_bytes(const chess_ctx* ctx, int32_t n_rows, int32_t max_new, int32_t batch, size_t* bytes)
+{
+    if (!ctx || !bytes || n_rows < 1 || n_rows > CHESS_MAX_TOKENS || max_new < 1 || batch < 1 || batch > ctx->cfg.max_batch) return CHESS_EINVAL;
+    // no shape has more than two partials of 64 rows a compute unit
+    chess::AttendShape most{};
+    most.rows = 64;
+    most.parts = 2 * (int64_t)ctx->n_cu;
+    size_t ml;
+    *bytes = attend_layout(most, &ml);
+    return CHESS_OK;
+}
+
+static int attend_common(chess_ctx* ctx, const chess_scores* scores, const void* q, int32_t n_rows, const int32_t* token_start, int32_t max_new,
+                         const void* k_pool, const void* v_pool, const int32_t* block_table, const int32_t* seq_lens, const int32_t* page_ids,
+                         const int32_t* n_selected, int32_t batch, void* out, void* workspace, void* scratch, size_t scratch_bytes, void* stream)
+{
+    if (!ctx || !q || !token_start || !k_pool || !v_pool || !block_table || !seq_lens || !out || !workspace || !scratch) return CHESS_EINVAL;
+    if (batch < 1 || batch > ctx->cfg.max_batch || n_rows < 1 || n_rows > CHESS_MAX_TOKENS || max_new < 1) return CHESS_EINVAL;
+    if (misaligned({q, k_pool, v_pool, out, workspace}, 15) || misaligned({scratch}, 255) || !on_device(ctx)) return CHESS_EINVAL;
+    chess::AttendArgs a{};
+    a.scale_log2 = ctx->sm_scale * 1.44269504088896340736f;
+    if (scores) {
+        if (!(scores->cap >= 0.f) || !std::isfinite(scores->cap) || scores->window < 0) return CHESS_EINVAL;
+        if (misaligned({scores->slopes, scores->prefix_lens, scores->first_keys}, 3)) return CHESS_EINVAL;
+        if (scores->cap > 0.f) {
+            a.cap_in = ctx->sm_scale / scores->cap;
+            a.cap_out = scores->cap * 1.44269504088896340736f;
+            // (a cap so small or so large that these leave the normal numbers is no cap)
+            if (!std::isnormal(a.cap_in) || !std::isfinite(a.cap_out)) return CHESS_EINVAL;
+        }
+        a.window = scores->window;
+        a.slopes = scores->slopes; a.prefix_lens = scores->prefix_lens; a.first_keys = scores->first_keys;
+    }
+    max_new = std::min(max_new, n_rows);
+    const chess::Geom& g = ctx->geom;
+    const chess::AttendShape s = chess::attend_shape(ctx, max_new, batch, page_ids != nullptr);
+    size_t ml_off;
+    if (scratch_bytes < attend_layout(s, &ml_off)) return CHESS_EINVAL;
+    if (s.blocks > 65535 || (int64_t)batch * g.n_kv_heads * s.n_splits > (1 << 24) - 1) return CHESS_ENOTSUP;
+    a.q = static_cast<const uint16_t*>(q);
+    a.k_pool = static_cast<const uint16_t*>(k_pool);
+    a.v_pool = static_cast<const uint16_t*>(v_pool);
+    a.block_table = block_table; a.seq_lens = seq_lens; a.token_start = token_start; a.page_ids = page_ids; a.n_selected = n_selected;
+    a.out = static_cast<uint16_t*>(out);
+    a.part_acc = static_cast<float*>(scratch);
+    a.part_ml = reinterpret_cast<float*>(static_cast<char*>(scratch) + ml_off);
+    a.arrivals = reinterpret_cast<int32_t*>(static_cast<char*>(workspace) + ctx->ws_cnt_off);
+    a.n_rows = n_rows; a.max_new = max_new; a.rows_most = (int)std::min<int64_t>((int64_t)max_new * g.group, 1 << 20);
+    a.batch = batch; a.max_pages = g.max_pages; a.max_sel = g.max_sel; a.n_kv_heads = g.n_kv_heads; a.group = g.group;
+    return chess::launch_attend(ctx, a, s, static_cast<hipStream_t>(stream)) == hipSuccess ? CHESS_OK : CHESS_EHIP;
+}
+
+int chess_dense_attend(chess_ctx* ctx, const chess_scores* scores, const void* q, int32_t n_rows, const int32_t* token_start, int32_t max_new,
+                       const void* k_pool, const void* v_pool, const int32_t* block_table, const int32_t* seq_lens, int32_t batch, void* out,
+                       void* workspace, void* scratch, size_t scratch_bytes, void* stream)
+{
+    return attend_common(ctx, scores, q, n_rows, token_start, max_new, k_pool, v_pool, block_table, seq_lens, nullptr, nullptr, batch, out, workspace,
+                         scratch, scratch_bytes, stream);
+}
+
+int chess_sparse_attend(chess_ctx* ctx, const chess_scores* scores, const void* q, int32_t n_rows, const int32_t* token_start, int32_t max_new,
+                        const void* k_pool, const void* v_pool, const int32_t* block_table, const int32_t* seq_lens, const int32_t* page_ids,
+                        const int32_t* n_selected, int32_t batch, void* out, void* workspace, void* scratch, size_t scratch_bytes, void* stream)
+{
+    if (!page_ids || !n_selected) return CHESS_EINVAL;
+    return attend_common(ctx, scores, q, n_rows, token_start, max_new, k_pool, v_pool, block_table, seq_lens, page_ids, n_selected, batch, out, workspace,
+                         scratch, scratch_bytes, stream);
+}
+
+int chess_verify(chess_ctx* ctx, const float* target, int64_t target_stride, const float* draft, int64_t draft_seq, int64_t draft_row, int32_t vocab,
+                 const int32_t* tokens, int32_t n_rows, const int32_t* token_start, const float* uniforms, int32_t max_drafts,
+                 const int32_t* seq_lens, int32_t batch, int32_t* n_accepted, int32_t* out_tokens, int32_t* lens_after, void* workspace,
+                 void* stream)
+{
+    if (!ctx || !target || !tokens || !token_start || !uniforms || !seq_lens || !n_accepted || !out_tokens || !lens_after || !workspace) return CHESS_EINVAL;
+    if (batch < 1 || batch > ctx->cfg.max_batch || vocab < 1 || vocab > INT32_MAX - 1023 || n_rows < 1 || max_drafts < 0 || max_drafts > CHESS_MAX_TOKENS) return CHESS_EINVAL;
+    if (target_stride < vocab || (draft && max_drafts > 0 && (draft_row < vocab || draft_seq < vocab))) return CHESS_EINVAL;
+    if (misaligned({target, draft, tokens, token_start, uniforms, seq_lens, n_accepted, out_tokens, lens_after}, 3) || misaligned({workspace}, 15) ||
+        !on_device(ctx))
+        return CHESS_EINVAL;
+    if (batch > 65535) return CHESS_ENOTSUP;
+    char* wb = static_cast<char*>(workspace);
+    const chess::VerifyArgs a{target, target_stride, draft, draft_seq, draft_row, tokens, token_start, uniforms, seq_lens, n_accepted, out_tokens, lens_after,
+                              reinterpret_cast<double*>(wb + ctx->ws_ver_off), reinterpret_cast<int32_t*>(wb + ctx->ws_entcnt_off), vocab, n_rows,
+                              max_drafts, batch, 0, 0, 0};
+    return chess::launch_verify(ctx, a, static_cast<hipStream_t>(stream)) == hipSuccess ? CHESS_OK : CHESS_EHIP;
+}
+
+int chess_trim_pages(chess_ctx* ctx, const int32_t* seq_lens, const int32_t* keep_lens, int32_t batch, const int32_t* block_table, int32_t* free_pages,
+                     int32_t capacity, const int32_t* n_free, int32_t* n_left, void* workspace, void* stream)
+{
+    if (!ctx || !seq_lens || !keep_lens || !block_table || !free_pages || !n_free || !n_left || !workspace) return CHESS_EINVAL;
+    if (batch < 1 || batch > ctx->cfg.max_batch || capacity < 1 || capacity > CHESS_MAX_TOKENS || misaligned({workspace}, 15) || !on_device(ctx)) return CHESS_EINVAL;
+    if (batch > chess::kPageMost) return CHESS_ENOTSUP;
+    const chess::TrimArgs a{seq_lens, keep_lens, block_table, free_pages, n_free, n_left,
+                            reinterpret_cast<int32_t*>(static_cast<char*>(workspace) + ctx->ws_cnt_off), batch, capacity, ctx->geom.max_pages, n_left == n_free};
+    return chess::launch_trim(ctx, a, static_cast<hipStream_t>(stream)) == hipSuccess ? CHESS_OK : CHESS_EHIP;
 }
 
 int chess_debug_force_splits(chess_ctx* ctx, int32_t n_splits, int32_t waves)

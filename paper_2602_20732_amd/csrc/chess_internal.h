@@ -246,6 +246,7 @@ struct chess_ctx {
     int force_splits, force_waves;                         // 0 = automatic
     size_t ws_acc_off, ws_ml_off, workspace_bytes;
     size_t ws_ent_off, ws_entcnt_off;                      // entropy partials, their arrival counters
+    size_t ws_ver_off;                                     // sums of a verified row's pieces (their counters: the entropy's)
     size_t ws_keys_off, ws_tail_off, ws_meta_off, ws_cnt_off, ws_err_off, ws_prof_off;   // select scratch, decode arrival counters, error word
     int64_t key_stride;
     int force_cluster;                                     // 0 = automatic
@@ -382,6 +383,16 @@ struct ReleaseArgs {
     int32_t* arrivals;
     int batch, capacity, max_pages, in_place;
 };
+struct TrimArgs {
+    const int32_t* seq_lens;
+    const int32_t* keep_lens;
+    const int32_t* block_table;
+    int32_t* free_pages;
+    const int32_t* n_free;
+    int32_t* n_left;
+    int32_t* arrivals;
+    int batch, capacity, max_pages, in_place;
+};
 // Pages that so many new tokens of `batch` sequences can lie in.
 inline int64_t most_writes(int64_t tokens, int64_t batch, int page_size)
 {
@@ -390,6 +401,88 @@ inline int64_t most_writes(int64_t tokens, int64_t batch, int page_size)
 }
 hipError_t launch_map(chess_ctx* ctx, const MapArgs& a, hipStream_t stream);
 hipError_t launch_release(chess_ctx* ctx, const ReleaseArgs& a, hipStream_t stream);
+hipError_t launch_trim(chess_ctx* ctx, const TrimArgs& a, hipStream_t stream);
+
+// Norms and rotation (rotate.hip).
+struct RotateArgs {
+    const uint16_t* q;               // null: keys only
+    const uint16_t* k;               // null: queries only
+    const uint16_t* v;
+    int64_t q_stride, k_stride, v_stride;   // elements from a token to the next
+    const int32_t* positions;        // [axes][position_stride]
+    int64_t position_stride;
+    const float* inv_freq;
+    const float* q_norm;             // [128] or [heads][128], or null
+    const float* k_norm;
+    uint64_t axis_lo, axis_hi;       // two bits a pair: which row of positions turns it
+    const int4* writes;
+    const int32_t* counts;
+    uint16_t* q_out;
+    uint16_t* k_out;                 // rows, or the K pool
+    uint16_t* v_pool;
+    int q_heads, kv_heads, pairs, norm_stride, max_writes, n_rows, n_pages;
+    float eps, scale;
+    int q_parts, k_parts, parts;     // runs of heads, workgroups a unit (rotate_shape)
+};
+// Heads / 4 that a wave turns at a time, and how many units (an entry of the write list, or 16 rows) of how many workgroups there are.
+struct RotateShape {
+    int quads, q_parts, k_parts, parts;
+    int64_t units;
+};
+RotateShape rotate_shape(const chess_ctx* ctx, const RotateArgs& a, bool paged);
+hipError_t launch_rotate(chess_ctx* ctx, RotateArgs a, bool paged, bool beside, hipStream_t stream);
+
+// Attention of several new tokens of a sequence (attend.hip).
+struct AttendArgs {
+    const uint16_t* q;
+    const uint16_t* k_pool;
+    const uint16_t* v_pool;
+    const int32_t* block_table;
+    const int32_t* seq_lens;
+    const int32_t* token_start;
+    const int32_t* page_ids;         // null: every page
+    const int32_t* n_selected;
+    uint16_t* out;
+    const float* slopes;             // or null, as the next two
+    const int32_t* prefix_lens;
+    const int32_t* first_keys;
+    float* part_acc;                 // partials: [part][rows][128], (m, l) [part][rows]
+    float* part_ml;
+    int32_t* arrivals;               // [batch][H_kv][kArrivalStride], zero between launches
+    float scale_log2;                // sm_scale log2(e)
+    float cap_in, cap_out;           // sm_scale / cap, cap log2(e); 0: no cap
+    int window, n_rows, max_new, rows_most;
+    int batch, max_pages, max_sel, n_kv_heads, group;
+    int n_slots, n_splits;           // (of the shape)
+};
+// How a call is cut: rows of a workgroup, blocks of them a sequence, splits of the keys (n_slots > 0: dealt by length, at most n_splits to one sequence).
+struct AttendShape {
+    int rows, blocks, n_splits, n_slots;
+    int64_t parts;                   // partials of `rows` rows
+};
+AttendShape attend_shape(const chess_ctx* ctx, int64_t max_new, int batch, bool list);
+hipError_t launch_attend(chess_ctx* ctx, AttendArgs a, const AttendShape& s, hipStream_t stream);
+
+// Drafted tokens verified (verify.hip).
+constexpr int kVerPieces = 256;      // most pieces of a vocabulary
+struct VerifyArgs {
+    const float* target;
+    int64_t target_stride;
+    const float* draft;              // or null
+    int64_t draft_seq, draft_row;
+    const int32_t* tokens;
+    const int32_t* token_start;
+    const float* uniforms;           // [batch][most + 1]
+    const int32_t* seq_lens;
+    int32_t* n_accepted;
+    int32_t* out_tokens;             // [batch][most + 1]
+    int32_t* lens_after;
+    double* parts;                   // [batch][kVerPieces]
+    int32_t* arrivals;               // [batch][kArrivalStride], zero between launches
+    int vocab, n_rows, most, batch;
+    int piece, n_pieces, per_split;  // (of launch_verify)
+};
+hipError_t launch_verify(chess_ctx* ctx, VerifyArgs a, hipStream_t stream);
 
 // 8-bit pages (quant_store.hip, quant_summarize.hip, quant_decode.hip).  scales: fp32 [physical page][H_kv][2] (keys, values).
 struct StoreArgs {

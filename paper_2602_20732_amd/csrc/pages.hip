@@ -193,6 +193,29 @@ __global__ __launch_bounds__(kPageThreads) void release_kernel(ReleaseArgs a)
     if (threadIdx.x == 0) *a.n_left = n_free + total;
 }
 
+// The pages behind what a sequence keeps of its tokens, as release_kernel.
+template <int B>
+__global__ __launch_bounds__(kPageThreads) void trim_kernel(TrimArgs a)
+{
+    extern __shared__ int upto[];                     // [batch]: pages pushed; then [batch] pages kept
+    const int batch = a.batch, n_free = max(*a.n_free, 0);
+    int* kept = upto + batch;
+    const auto pages = [&](int len) { return (int)min(((int64_t)max(len, 0) + B - 1) / B, (int64_t)a.max_pages); };
+    sums_upto<1>(batch, upto, [&](int b, int (&v)[1]) {
+        kept[b] = pages(a.keep_lens[b]);
+        v[0] = max(pages(a.seq_lens[b]) - kept[b], 0);
+    });
+    const int cut = served(batch, [&](int b) { return upto[b] <= a.capacity - n_free; });
+    const int total = cut > 0 ? upto[cut - 1] : 0;
+    for (int i = blockIdx.x * kPageThreads + threadIdx.x; i < total; i += gridDim.x * kPageThreads) {
+        int b[1];
+        first_above(b, upto, cut, {i});
+        a.free_pages[n_free + i] = a.block_table[(size_t)b[0] * a.max_pages + kept[b[0]] + i - (b[0] > 0 ? upto[b[0] - 1] : 0)];
+    }
+    if (!writes_rows(a.in_place, a.arrivals)) return;
+    if (threadIdx.x == 0) *a.n_left = n_free + total;
+}
+
 hipError_t launch_map(chess_ctx* ctx, const MapArgs& a, hipStream_t stream)
 {
     const int B = ctx->geom.page_size;
@@ -212,6 +235,15 @@ hipError_t launch_release(chess_ctx* ctx, const ReleaseArgs& a, hipStream_t stre
     const unsigned n = (unsigned)clampi(cdiv((int64_t)a.batch * a.max_pages, 16 * kPageThreads), 1, 64);
     const size_t lds = (size_t)a.batch * sizeof(int);
     return launch(B == 16 ? release_kernel<16> : release_kernel<32>, dim3(n), dim3(kPageThreads), lds, stream, a);
+}
+
+hipError_t launch_trim(chess_ctx* ctx, const TrimArgs& a, hipStream_t stream)
+{
+    const int B = ctx->geom.page_size;
+    // (a step's refused tokens leave a page or so a sequence: one workgroup a 256 sequences, more only where rows are long)
+    const unsigned n = (unsigned)clampi(cdiv((int64_t)a.batch * a.max_pages, 64 * kPageThreads), 1, 16);
+    const size_t lds = (size_t)a.batch * 2 * sizeof(int);
+    return launch(B == 16 ? trim_kernel<16> : trim_kernel<32>, dim3(n), dim3(kPageThreads), lds, stream, a);
 }
 
 }  // namespace chess

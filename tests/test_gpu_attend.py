@@ -1,0 +1,243 @@
+"""Attention of several new tokens of a sequence over the bf16 pages, against 64 bits: few rows (the keys are split) and many."""
+from __future__ import annotations
+
+import ctypes
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2602_20732_amd as pk
+from attend_common import Batch, bf16, ints
+
+pytestmark = pytest.mark.gpu
+SUMMARY_DTYPE_SWEEP = False
+
+HEADS = [(8, 2), (4, 4), (7, 1), (32, 2)]
+RULES = [dict(), dict(cap=5.0), dict(window=37), dict(slopes=8.0), dict(cap=30.0, slopes=4.0, window=100)]
+rule_name = lambda r: "-".join(r) or "causal"  # noqa: E731
+
+
+@pytest.mark.parametrize("rule", RULES, ids=rule_name)
+@pytest.mark.parametrize("B", [16, 32])
+@pytest.mark.parametrize("heads", HEADS, ids=str)
+@pytest.mark.parametrize("new", [1, 2, 5, 8, 19])
+def test_one_sequence(new, heads, B, rule):
+    for held in (0, 1, 30, 15 + new, 700):
+        Batch(new + held, [held], [new], *heads, B=B, **rule).check()
+
+
+@pytest.mark.parametrize("rule", RULES[:3], ids=rule_name)
+@pytest.mark.parametrize("B", [16, 32])
+def test_ragged_batch_dealt_by_length(B, rule):
+    Batch(3, [1500, 0, 3, 900, 64, 31, 2000], [5, 1, 0, 8, 2, 3, 4], 8, 2, B=B, **rule).check()
+    Batch(4, [0] * 70 + [600], [2] * 70 + [3], 4, 1, B=B, **rule).check()
+
+
+@pytest.mark.parametrize("B", [16, 32])
+@pytest.mark.parametrize("new", [3, 8, 40])
+def test_lists(new, B):
+    Batch(new, [777, 40, 0, 333], [new, new - 1, 1, 2], 8, 2, B=B, listed=9).check()
+    Batch(new, [777, 40, 0, 333], [new, new - 1, 1, 2], 8, 2, B=B, listed=9, cap=7.0, window=200, slopes=3.0).check()
+
+
+def test_lists_with_entries_that_are_no_pages():
+    b = Batch(1, [200, 90], [3, 2], 8, 2, listed=8)
+    want = b.want()
+    pages = [[int(b.ids[s, h, b.n[s, h] - 1]) for h in range(2)] for s in range(2)]
+    b.n -= 1
+    for s in range(2):
+        for h in range(2):
+            assert pages[s][h] >= 0
+    want = b.want()
+    # entries behind the last page of the sequence, negative ones, and a count above the row
+    for s in range(2):
+        for h in range(2):
+            b.ids[s, h, b.n[s, h]:] = [b.pages[s], -1, 2 ** 31 - 1, -2 ** 31, 10 ** 6, -7, b.pages[s] + 1, -1][: 8 - b.n[s, h]]
+    b.n[:] = 1000
+    got = b.run().double().cpu().numpy()
+    assert (np.abs(got - want[0]) <= want[1]).all()
+
+
+@pytest.mark.parametrize("new", [6, 200])
+@pytest.mark.parametrize("rule", [dict(), dict(cap=20.0)], ids=rule_name)
+def test_prefixes(new, rule):
+    Batch(2, [0, 50, 300, 0], [new, new, 5, new - 1], 8, 2, prefix=[4, 500, 302, 0], **rule).check()
+
+
+@pytest.mark.parametrize("listed", [None, 6])
+@pytest.mark.parametrize("new", [8, 150])
+def test_documents_and_rows_that_see_nothing(new, listed):
+    """Starts of documents, some behind the token itself: those rows are 0; a negative one is the beginning."""
+    held = [90, 0, 400]
+    first = np.concatenate([[(h + i) // 33 * 33 for i in range(new)] for h in held])
+    first[::5] = [(h + i) + 1 for h in held for i in range(new)][::5]
+    first[1] = -5
+    b = Batch(5, held, [new] * 3, 8, 2, first=first, slopes=2.0, listed=listed)
+    got = b.run()
+    b.check(got)
+    assert (got[::5] == 0).all()
+
+
+@pytest.mark.parametrize("heads", HEADS, ids=str)
+@pytest.mark.parametrize("B", [16, 32])
+@pytest.mark.parametrize("rule", RULES, ids=rule_name)
+def test_prompts(rule, B, heads):
+    Batch(6, [0, 100, 7, 0], [129, 70, 1, 333], *heads, B=B, **rule).check(weight_step=2.0 ** -8)
+
+
+@pytest.mark.parametrize("new", [4, 130])
+def test_a_longer_context_with_peaks(new):
+    Batch(7, [3000, 5], [new, new], 4, 2, sharp=3.0).check(weight_step=2.0 ** -8)
+
+
+def poisoned(new, value, listed=None, **rule):
+    """Sequences whose last tokens' keys and values are not finite: the rows before do not see them."""
+    b = Batch(8, [60, 210], [new, new], 8, 2, listed=listed, **rule)
+    for s in range(2):
+        k, v = b.seqs[s]
+        v[-1, 0, 3], v[-1, 1, 64:], v[-2, 1, 127] = value, value, -value
+        k[-1, 0, 5] = value
+        v[11, 0, 40] = value
+        for p in range(b.pages[s]):
+            b.put(s, p)
+    return b
+
+
+@pytest.mark.parametrize("value", [np.inf, -np.inf, np.nan])
+@pytest.mark.parametrize("new", [5, 150])
+@pytest.mark.parametrize("rule", [dict(), dict(window=20), dict(first=True)], ids=["causal", "window", "documents"])
+def test_what_a_row_does_not_see_does_not_touch_it(rule, new, value):
+    if "first" in rule:
+        rule = dict(first=np.concatenate([np.arange(h, h + new) - 15 for h in (60, 210)]))
+    b = poisoned(new, value, **rule)
+    got = b.run()
+    y, off = b.want(2.0 ** -8)
+    got = got.double().cpu().numpy()
+    fine = np.isfinite(y)
+    assert fine[:-1].any() and not fine.all()
+    assert np.isfinite(got[fine]).all() and (np.abs(got - y) <= off)[fine].all()
+    assert (np.isnan(got) == np.isnan(y)).all()
+    assert (got[np.isinf(y)] == y[np.isinf(y)]).all()
+
+
+def test_scores_of_any_size():
+    """Keys so large that scores reach 1e30: the largest weighs 1."""
+    for new in (3, 140):
+        for size in (1e4, 1e12, 1e28):
+            b = Batch(9, [40], [new], 4, 2)
+            k, _ = b.seqs[0]
+            k *= np.float32(size)
+            k[:] = bf16(k).float().numpy()
+            for p in range(b.pages[0]):
+                b.put(0, p)
+            got = b.run().double().cpu().numpy()
+            # (one key outweighs all others unless two are within rounding: those rows say nothing)
+            for r in range(new):
+                for h in range(4):
+                    s = b.sm * (k[: 41 + r, h // 2].astype(np.float64) @ b.q[r, h].double().numpy())
+                    order = np.argsort(s)
+                    if s[order[-1]] - s[order[-2]] > 1e-4 * abs(s[order[-1]]) + 40:
+                        v = b.seqs[0][1][order[-1], h // 2]
+                        assert (np.abs(got[r, h] - v) <= 2.0 ** -8 * np.abs(v) + 1e-6).all(), (size, r, h)
+            assert np.isfinite(got).all()
+
+
+def test_sequences_without_tokens_and_rows_behind():
+    b = Batch(10, [0, 40, 0], [0, 3, 0], 8, 2)
+    b.check()
+    args = b.cuda()
+    args["token_start"] = ints([0, 0, 2, 2])                      # the last row is nobody's
+    out = b.launch(args)
+    torch.cuda.synchronize()
+    assert (out[2:] == 5).all() and (out[:2] != 5).any()
+    args = b.cuda()
+    args["token_start"] = ints([0, 0, 4, 4])                      # rows that are not there
+    assert (b.launch(args) == 5).all()
+    args = b.cuda()
+    args["max_new"] = 2                                           # rows beyond max_new are left
+    out = b.launch(args)
+    torch.cuda.synchronize()
+    assert (out[2:] == 5).all()
+
+
+def test_lengths_shorter_than_the_new_tokens_say():
+    """A row whose position would be negative sees nothing."""
+    b = Batch(11, [0], [6], 4, 2)
+    args = b.cuda()
+    args["seq_lens"] = ints([2])
+    out = b.launch(args)
+    torch.cuda.synchronize()
+    assert (out[:4] == 0).all() and (out[4:6] != 0).any()
+
+
+@pytest.mark.parametrize("new", [5, 90])
+def test_replayed_with_other_lengths_between_eager_work(new):
+    """The launch reads lengths and starts on the device: a captured one follows them."""
+    full = Batch(12, [500, 33, 250], [new, new, new - 2], 8, 2)
+    args = full.cuda()
+    side, g = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(g, stream=side):
+        full.launch(args)
+    want = full.run()
+    for step in range(3):
+        args["out"].fill_(5.0)
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(args["out"][: full.rows], want)
+    shorter = ints([full.lens[0] - 3, full.lens[1] - 1, full.lens[2] - 7])
+    args["seq_lens"].copy_(shorter)
+    eager = {**full.cuda(), "seq_lens": shorter}
+    out = full.launch(eager)
+    g.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(args["out"], out)
+
+
+@pytest.mark.parametrize("new", [2, 60])
+def test_many_sequences(new):
+    rng = np.random.default_rng(0)
+    Batch(13, rng.integers(0, 90, 150), rng.integers(0, new + 1, 150), 4, 1).check(weight_step=2.0 ** -8)
+
+
+def test_far_pages_of_a_large_pool():
+    """Offsets beyond 2^32 bytes into the pools."""
+    H, B = 8, 32
+    page = H * B * 128
+    n_phys = (1 << 32) // (2 * page) + 3
+    b = Batch(14, [70], [3], 16, H, B=B)
+    args = b.cuda()
+    k, v = (torch.empty((n_phys, *x.shape[1:]), dtype=torch.bfloat16, device="cuda") for x in (args["k_pool"], args["v_pool"]))
+    far = [n_phys - 1, 0, n_phys - 2]
+    for p in range(b.pages[0]):
+        k[far[p]], v[far[p]] = args["k_pool"][b.table[0, p]], args["v_pool"][b.table[0, p]]
+    table = args["block_table"].clone()
+    table[0, : b.pages[0]] = ints(far[: b.pages[0]])
+    out = b.launch({**args, "k_pool": k, "v_pool": v, "block_table": table})
+    torch.cuda.synchronize()
+    b.check(out[: b.rows])
+
+
+def test_refusals():
+    b = Batch(15, [30], [4], 8, 2, listed=2)
+    args = b.cuda()
+    args["out"] = args["out"][:4]
+    dense = b.lib.dense_attend
+    dense(**args)
+    s = pk.Scores
+    for name, bad in (("q", args["q"].float()), ("q", args["q"][:, :4]), ("q", args["q"].reshape(4, -1)), ("out", args["out"].float()), ("out", args["out"][:3]),
+                      ("token_start", args["token_start"][:1]), ("block_table", args["block_table"][:, :1]), ("workspace", args["workspace"][:64]),
+                      ("scratch", args["scratch"][1:]), ("scratch", args["scratch"][:0]), ("max_new", 0), ("scores", s(cap=-1.0)), ("scores", s(cap=float("nan"))),
+                      ("scores", s(cap=float("inf"))), ("scores", s(cap=1e-42)), ("scores", s(window=-1)),
+                      ("scores", s(slopes=torch.ones(7, device="cuda"))), ("scores", s(slopes=torch.ones(8))), ("scores", s(first_keys=ints([0] * 3))),
+                      ("scores", s(prefix_lens=torch.zeros(1, device="cuda")))):
+        with pytest.raises(pk.ChessError):
+            dense(**{**args, name: bad})
+    with pytest.raises(pk.ChessError):
+        b.lib.sparse_attend(**args, page_ids=ints([0]), n_selected=ints([1]))
+    n = ctypes.c_size_t()
+    for bad in ((0, 1, 1), (1, 0, 1), (1, 1, 0), (1, 1, 2)):
+        assert b.lib.lib.chess_attend_scratch_bytes(b.lib._h, *bad, ctypes.byref(n)) == -1
+    torch.cuda.synchronize()
