@@ -904,22 +904,25 @@ int chess_rotate_store(chess_ctx* ctx, const chess_rotary* rotary, const void* q
 }
 
 // Where the parts of the scratch lie; the bytes of all.
-static size_t attend_layout(const chess::AttendShape& s, size_t* ml_off)
+struct AttendLayout { size_t ml, blocks, units, n_units, counters, bytes; };
+static AttendLayout attend_layout(const chess_ctx* ctx, const chess::AttendShape& s)
 {
-    const size_t rows = (size_t)s.parts * s.rows;
-    *ml_off = align_up(rows * kHeadDim * sizeof(float), 256);
-    return align_up(*ml_off + rows * 2 * sizeof(float), 256);
+    AttendLayout l;
+    const size_t rows = (size_t)(s.parts * s.rows);
+    l.ml = align_up(rows * kHeadDim * sizeof(float), 256);
+    l.blocks = align_up(l.ml + rows * 2 * sizeof(float), 256);
+    l.units = align_up(l.blocks + (size_t)s.blocks * sizeof(int4), 256);
+    l.n_units = align_up(l.units + (size_t)(s.blocks + s.extra) * sizeof(chess::AttendUnit), 256);
+    l.counters = l.n_units + 256;
+    l.bytes = align_up(l.counters + (size_t)s.blocks * ctx->geom.n_kv_heads * sizeof(int32_t), 256);
+    return l;
 }
 
 int chess_attend_scratch_bytes(const chess_ctx* ctx, int32_t n_rows, int32_t max_new, int32_t batch, size_t* bytes)
 {
     if (!ctx || !bytes || n_rows < 1 || n_rows > CHESS_MAX_TOKENS || max_new < 1 || batch < 1 || batch > ctx->cfg.max_batch) return CHESS_EINVAL;
-    // no shape has more than two partials of 64 rows a compute unit
-    chess::AttendShape most{};
-    most.rows = 64;
-    most.parts = 2 * (int64_t)ctx->n_cu;
-    size_t ml;
-    *bytes = attend_layout(most, &ml);
+    // (a call with fewer new tokens of a sequence may be one of few rows)
+    *bytes = std::max(attend_layout(ctx, chess::attend_shape(ctx, n_rows, max_new, batch)).bytes, attend_layout(ctx, chess::attend_shape(ctx, 64, 64 / ctx->geom.group, 1)).bytes);
     return CHESS_OK;
 }
 
@@ -946,19 +949,24 @@ static int attend_common(chess_ctx* ctx, const chess_scores* scores, const void*
     }
     max_new = std::min(max_new, n_rows);
     const chess::Geom& g = ctx->geom;
-    const chess::AttendShape s = chess::attend_shape(ctx, max_new, batch, page_ids != nullptr);
-    size_t ml_off;
-    if (scratch_bytes < attend_layout(s, &ml_off)) return CHESS_EINVAL;
-    if (s.blocks > 65535 || (int64_t)batch * g.n_kv_heads * s.n_splits > (1 << 24) - 1) return CHESS_ENOTSUP;
+    const chess::AttendShape s = chess::attend_shape(ctx, n_rows, max_new, batch);
+    const AttendLayout lay = attend_layout(ctx, s);
+    if (scratch_bytes < lay.bytes) return CHESS_EINVAL;
+    if (batch > chess::kDealMost || (int64_t)n_rows * g.group > (1 << 30) || (s.blocks + s.extra) * g.n_kv_heads > (1 << 24) - 1) return CHESS_ENOTSUP;
     a.q = static_cast<const uint16_t*>(q);
     a.k_pool = static_cast<const uint16_t*>(k_pool);
     a.v_pool = static_cast<const uint16_t*>(v_pool);
     a.block_table = block_table; a.seq_lens = seq_lens; a.token_start = token_start; a.page_ids = page_ids; a.n_selected = n_selected;
     a.out = static_cast<uint16_t*>(out);
     a.part_acc = static_cast<float*>(scratch);
-    a.part_ml = reinterpret_cast<float*>(static_cast<char*>(scratch) + ml_off);
+    char* sb = static_cast<char*>(scratch);
+    a.part_ml = reinterpret_cast<float*>(sb + lay.ml);
+    a.blocks = reinterpret_cast<int4*>(sb + lay.blocks);
+    a.units = reinterpret_cast<chess::AttendUnit*>(sb + lay.units);
+    a.n_units = reinterpret_cast<int32_t*>(sb + lay.n_units);
+    a.counters = reinterpret_cast<int32_t*>(sb + lay.counters);
     a.arrivals = reinterpret_cast<int32_t*>(static_cast<char*>(workspace) + ctx->ws_cnt_off);
-    a.n_rows = n_rows; a.max_new = max_new; a.rows_most = (int)std::min<int64_t>((int64_t)max_new * g.group, 1 << 20);
+    a.n_rows = n_rows; a.max_new = max_new;
     a.batch = batch; a.max_pages = g.max_pages; a.max_sel = g.max_sel; a.n_kv_heads = g.n_kv_heads; a.group = g.group;
     return chess::launch_attend(ctx, a, s, static_cast<hipStream_t>(stream)) == hipSuccess ? CHESS_OK : CHESS_EHIP;
 }

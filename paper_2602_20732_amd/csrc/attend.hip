@@ -12,353 +12,849 @@
 namespace chess {
 
 // ---- few rows a sequence and KV head (drafted tokens): the keys are split ------------------------------------------------------
-// A workgroup has up to 32 kRows query rows (token, head of the group) and every n-th tile of 32 keys, a wave every fourth of those; a wave
-// reads K and V from the pages into the operands of 32 x 32 x 16 products:
-//   S^T[key][row] = K[key][dim] Q^T[dim][row]             8 products a tile and 32 rows
+// A tile is 32 keys (16 KB).  The tiles of all sequences of a KV head lie in a line, in sequence order, and each of the head's workgroups (one a
+// compute unit) takes an equal share of it: the segments of one or several sequences.  Within a segment a wave takes every fourth tile, all
+// (token, head of the group) rows at once, up to 32 kRows of them:
+//   S^T[key][row] = K[key][dim] Q^T[dim][row]             8 products of 32 x 32 x 16 a tile and 32 rows
 //   O^T[dim][row] += V^T[dim][key] P^T[key][row]          8, twice: P as a bf16 number and a bf16 remainder (2^-17 of a weight)
-// The key rows of the first are dealt so that the 16 weights a lane ends up with are the 2 x 8 that it has to supply to the second.
-// The rows of the next tile are asked for as soon as the registers of this one's are free.
-// Bound: HBM, for as long as a tile's products (1.3 us a wave of 64 rows) take less than its 16 KB do.
-template <int B, int kRows, bool kList, bool kDealt, bool kCap>
-__global__ __launch_bounds__(256, kRows == 1 ? 2 : 1) void attend_few_kernel(AttendArgs a)
+// Each wave has two tiles of LDS of its own: one is worked on, the next is on its way (loads that write LDS, no barrier).  A sequence that lies in one share
+// is written at once; partials of the others are merged by the last workgroup of the sequence to arrive.
+// Bound: HBM, for as long as a tile's arithmetic (about 1 us a wave and 32 rows) takes less than the four waves' 64 KB do (2.7 us).
+
+// Keys of a sequence that its rows can see at all, in tiles, for those that deal: [first, end) of the pages' tiles, one at least.
+struct Tiles { int first, count; };
+
+template <int B, bool kList>
+__device__ __forceinline__ Tiles tiles_of(const AttendArgs& a, int b, int h, int n_new, int len)
 {
     constexpr int PPT = 32 / B;
-    __shared__ float comb[2][4][16][64];
+    if (n_new <= 0) return {0, 0};
+    if constexpr (kList) {
+        const int n = min(max(a.n_selected[(int64_t)b * a.n_kv_heads + h], 0), a.max_sel);
+        return {0, max((n + PPT - 1) / PPT, 1)};
+    } else {
+        const int first = a.window > 0 ? max(len - n_new - a.window + 1, 0) / 32 : 0;
+        return {first, max((len + 31) / 32 - first, 1)};
+    }
+}
+
+constexpr int kFewRing = 4 * 2 * 1024;                // 16-byte pieces: two tiles a wave
+constexpr size_t few_lds(int rows) { return (kFewRing + rows * 16) * 16; }
+
+template <int B, int kRows, bool kList, bool kCap>
+__global__ __launch_bounds__(256, 1) void attend_few_kernel(AttendArgs a)
+{
+    constexpr int PPT = 32 / B;
+    extern __shared__ uint4 ring[];                   // [wave][stage][1024]: 512 pieces of keys, 512 of values; afterwards the waves' sums.  Then [row][16] the queries
     __shared__ float wave_m[4][32 * kRows], wave_l[4][32 * kRows];
+    __shared__ int block_tiles[kDealMost / 64];
+    __shared__ Odd odd[kRows][256];
     __shared__ int flag;
-    __shared__ DealLds<4> deal;
-    __shared__ uint4 queries[32 * kRows][16];         // 16-byte pieces of a row, piece i of row r at i ^ (r % 16): no two rows' on the same banks
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     const int col = lane & 31, half = lane >> 5;
-    const int H = a.n_kv_heads, G = a.group;
+    const int H = a.n_kv_heads, G = a.group, h = blockIdx.x % H, slot = blockIdx.x / H;
 
-    int b, h, split, n_splits;
-    int64_t part0;
-    if constexpr (kDealt) {
-        h = blockIdx.x % H;
-        const int slot = blockIdx.x / H;
-        const SlotShare s = share_slots<B, 4, 32>(slot, a.n_slots, a.batch, a.n_splits, a.rows_most, a.seq_lens, a.max_pages, lane, wave, deal);
-        if (s.b < 0) return;
-        b = __builtin_amdgcn_readfirstlane(s.b);
-        split = __builtin_amdgcn_readfirstlane(s.split);
-        n_splits = __builtin_amdgcn_readfirstlane(s.n_splits);
-        part0 = (int64_t)h * a.n_slots + __builtin_amdgcn_readfirstlane(s.first);
-    } else {
-        h = blockIdx.x % H;
-        const int x = blockIdx.x / H;
-        b = x % a.batch;
-        split = x / a.batch;
-        n_splits = a.n_splits;
-        part0 = ((int64_t)blockIdx.y * a.batch * H + (int64_t)b * H + h) * n_splits;
-    }
-    const Span span = span_of(a, b, B);
-    const int n_rows = span.n_new * G, row0 = blockIdx.y * (32 * kRows);
-    if (row0 >= n_rows) return;
-
-    // the rows: what each sees; their queries into LDS
-    RowView row[kRows];
-    int see_lo = INT32_MAX, see_hi = -1, all_lo = 0, all_hi = INT32_MAX;
-#pragma unroll
-    for (int y = 0; y < kRows; ++y) {
-        row[y] = view_of(a, span, b, h, row0 + 32 * y + col);
-        const uint4* src = reinterpret_cast<const uint4*>(a.q + row[y].at * kHeadDim) + 4 * wave + 2 * half;
-#pragma unroll
-        for (int s = 0; s < 2; ++s) queries[32 * y + col][(4 * wave + 2 * half + s) ^ (col & 15)] = src[s];
-        if (row[y].there) {
-            if (row[y].hi >= row[y].lo) {
-                see_lo = min(see_lo, row[y].lo);
-                see_hi = max(see_hi, row[y].hi);
-            }
-            all_lo = max(all_lo, row[y].lo);
-            all_hi = min(all_hi, row[y].hi);
+    // the line: its length, this workgroup's share, the sequence that it begins in
+    const auto tiles_at = [&](int b) {
+        if (b >= a.batch) return Tiles{0, 0};
+        const Span s = span_by_lane(a, b, B);
+        return tiles_of<B, kList>(a, b, h, s.n_new, s.len);
+    };
+    int before = 0, total = 0, block = 0;
+    if (a.batch > 64) {
+        for (int i = wave; i * 64 < a.batch; i += 4) {
+            const int n = lane_of(lanes_upto(tiles_at(i * 64 + lane).count), 63);
+            if (lane == 0) block_tiles[i] = n;
         }
+        __syncthreads();
     }
-    see_lo = lanes_min(see_lo); see_hi = lanes_max(see_hi); all_lo = lanes_max(all_lo); all_hi = lanes_min(all_hi);
-
-    __syncthreads();
-
-    // its tiles
-    const int P = span.pages;
-    const int32_t* table = a.block_table + (int64_t)b * a.max_pages;
-    const int32_t* ids = kList ? a.page_ids + ((int64_t)b * H + h) * a.max_sel : nullptr;
-    const int n_list = kList ? min(max(a.n_selected[(int64_t)b * H + h], 0), a.max_sel) : P;
-    int t_first = 0, t_end = P > 0 && see_hi >= see_lo ? (n_list + PPT - 1) / PPT : 0;
-    if constexpr (!kList) {
-        t_first = see_hi >= see_lo ? see_lo / 32 : 0;
-        t_end = min(t_end, see_hi / 32 + 1);
+    int mine = tiles_at(lane).count, upto = lanes_upto(mine);
+    total = lane_of(upto, 63);
+    int of_block = 0, upto_block = 0;
+    if (a.batch > 64) {
+        of_block = lane * 64 < a.batch ? block_tiles[lane] : 0;
+        upto_block = lanes_upto(of_block);
+        total = lane_of(upto_block, 63);
     }
-    const int stride = 4 * n_splits;
-    int t = t_first + split * 4 + wave;
-
-    float m[kRows], l[kRows];
-    f32x16 o[kRows][4];
-#pragma unroll
-    for (int y = 0; y < kRows; ++y) {
-        m[y] = kNegBig;
-        l[y] = 0.f;
-#pragma unroll
-        for (int d = 0; d < 4; ++d)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) o[y][d][i] = 0.f;
+    // (a tile a wave at least)
+    const int share = max((int)(((int64_t)total + a.n_slots - 1) / a.n_slots), 4);
+    const int begin = slot * share, end = min(begin + share, total);
+    if (begin >= end) return;
+    if (a.batch > 64) {
+        block = __builtin_ctzll(__ballot(upto_block > begin));
+        before = lane_of(upto_block, block) - lane_of(of_block, block);
+        mine = tiles_at(block * 64 + lane).count;
+        upto = lanes_upto(mine);
     }
+    const int at = __builtin_ctzll(__ballot(before + upto > begin));
+    int b = __builtin_amdgcn_readfirstlane(block * 64 + at);
+    int line = __builtin_amdgcn_readfirstlane(before + lane_of(upto, at) - lane_of(mine, at));     // where the sequence begins in the line
 
-    int lp[PPT], lp_next[PPT], phys_next[PPT];
-    uint4 k[8], v[4][2];
-    const auto pages_of = [&](int tile, int (&page)[PPT]) {         // logical pages of a tile; a slot without one: -1
-#pragma unroll
-        for (int s = 0; s < PPT; ++s) {
-            const int i = tile * PPT + s;
-            int p = i;
-            if constexpr (kList) p = ids[min(i, a.max_sel - 1)];
-            page[s] = i < n_list && p >= 0 && p < P ? p : -1;
-        }
-    };
-    const auto look_up = [&](const int (&page)[PPT], int (&phys)[PPT]) {
-#pragma unroll
-        for (int s = 0; s < PPT; ++s) phys[s] = table[max(page[s], 0)];
-    };
-    const auto load_k = [&](const int (&phys)[PPT]) {
-        // row `col` of the product is key 16 (col / 16) + 8 (bit 2) + 4 (bit 3) + (col % 4) of the tile
-        const int key = (col & 16) + ((col & 4) << 1) + ((col & 8) >> 1) + (col & 3);
-        const int64_t pg = PPT == 1 || key < B ? phys[0] : phys[PPT - 1];
-        const uint4* src = reinterpret_cast<const uint4*>(a.k_pool + ((pg * H + h) * B + key % B) * kHeadDim) + half;
-#pragma unroll
-        for (int s = 0; s < 8; ++s) k[s] = src[2 * s];
-    };
-    const auto load_v = [&](const int (&phys)[PPT]) {
-#pragma unroll
-        for (int s = 0; s < 2; ++s) {
-            const int64_t pg = phys[(16 * s) / B];
-            const uint16_t* src = a.v_pool + ((pg * H + h) * kHeadDim + col) * B + (16 * s) % B + 8 * half;
-#pragma unroll
-            for (int d = 0; d < 4; ++d) v[d][s] = *reinterpret_cast<const uint4*>(src + d * 32 * B);
-        }
-    };
-    const auto first_key = [&](const int (&page)[PPT], int s) {     // of the eight keys that a lane has of step s
-        return page[(16 * s) / B] < 0 ? INT32_MIN / 2 : page[(16 * s) / B] * B + (16 * s) % B + 8 * half;
-    };
-    const auto scalar = [&](int (&x)[PPT]) {
-#pragma unroll
-        for (int s = 0; s < PPT; ++s) x[s] = __builtin_amdgcn_readfirstlane(x[s]);
-    };
+    const PageLanes from(lane, B);
+    const uint32_t ring_lds = lds_at(ring) + (uint32_t)wave * (2 * 16384);
+    const uint4* ring_own = ring + wave * 2048;
+    uint4* queries = ring + kFewRing;
 
-    if (t < t_end) {
-        int phys[PPT];
-        pages_of(t, lp);
-        look_up(lp, phys);
-        scalar(phys);
-        load_k(phys);
-        load_v(phys);
-        pages_of(min(t + stride, t_end - 1), lp_next);
-        look_up(lp_next, phys_next);
-    }
-    for (; t < t_end; t += stride) {
-        // whether a row may see less than all of the tile
-        bool part = false;
-#pragma unroll
-        for (int s = 0; s < PPT; ++s) part = part || lp[s] < 0 || lp[s] * B < all_lo || lp[s] * B + B - 1 > all_hi;
-        part = __builtin_amdgcn_readfirstlane(part);
-        f32x16 z[kRows];
+    for (; line < end; ++b) {
+        const Span span = span_of(a, b, B);
+        const Tiles all = tiles_of<B, kList>(a, b, h, span.n_new, span.len);
+        const int count = __builtin_amdgcn_readfirstlane(all.count), first = __builtin_amdgcn_readfirstlane(all.first);
+        if (count == 0) continue;
+        const int line_end = line + count;
+        // this segment, in tiles of the sequence
+        int t = max(begin - line, 0) + first + wave;
+        int t_end = min(end - line, count) + first;
+        const int P = span.pages;
+        const int32_t* table = a.block_table + (int64_t)b * a.max_pages;
+        const int32_t* ids = kList ? a.page_ids + ((int64_t)b * H + h) * a.max_sel : nullptr;
+        const int n_list = kList ? min(max(load_same(a.n_selected, (int64_t)b * H + h), 0), a.max_sel) : P;
+        if (P == 0 || n_list == 0) t_end = 0;         // (a tile was dealt all the same, so that the rows are written)
+
+        // the rows: their queries (Q^T operands), what each sees
+        const int n_rows = span.n_new * G;
+        RowView row[kRows];
+        int see_lo = INT32_MAX, see_hi = -1, all_lo = 0, all_hi = INT32_MAX;
 #pragma unroll
         for (int y = 0; y < kRows; ++y) {
+            row[y] = view_of(a, span, b, h, 32 * y + col);
+            // (piece i of row r at i ^ (r % 16): no two rows' on the same banks)
+            const uint4* src = reinterpret_cast<const uint4*>(a.q + row[y].at * kHeadDim) + 4 * wave + 2 * half;
 #pragma unroll
-            for (int i = 0; i < 16; ++i) z[y][i] = 0.f;
-#pragma unroll
-            for (int s = 0; s < 8; ++s) z[y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(k[s]), as_bf16x8(queries[32 * y + col][(2 * s + half) ^ (col & 15)]), z[y], 0, 0, 0);
+            for (int s = 0; s < 2; ++s) queries[(32 * y + col) * 16 + ((4 * wave + 2 * half + s) ^ (col & 15))] = src[s];
+            if (row[y].there) {
+                if (row[y].hi >= row[y].lo) {
+                    see_lo = min(see_lo, row[y].lo);
+                    see_hi = max(see_hi, row[y].hi);
+                }
+                all_lo = max(all_lo, row[y].lo);
+                all_hi = min(all_hi, row[y].hi);
+            }
         }
-        scalar(phys_next);
-        int phys[PPT];
-#pragma unroll
-        for (int s = 0; s < PPT; ++s) phys[s] = phys_next[s];
-        load_k(phys);                                 // (behind the last tile: that one's again)
-        int lp_now[PPT];
-#pragma unroll
-        for (int s = 0; s < PPT; ++s) {
-            lp_now[s] = lp[s];
-            lp[s] = lp_next[s];
+        see_lo = lanes_min(see_lo); see_hi = lanes_max(see_hi); all_lo = lanes_max(all_lo); all_hi = lanes_min(all_hi);
+        if (see_hi < see_lo) t_end = 0;
+        if constexpr (!kList) {                       // tiles that no row sees (this wave's others stay its own)
+            t_end = min(t_end, see_hi / 32 + 1);
+            while (t < t_end && t * 32 + 31 < see_lo) t += 4;
         }
-        pages_of(min(t + 2 * stride, t_end - 1), lp_next);
-        look_up(lp_next, phys_next);
 
-        bf16x8 hi_part[kRows][2], lo_part[kRows][2];
+        float m[kRows], l[kRows];
+        f32x16 o[kRows][4];
+        bool any_odd = false;
+#pragma unroll
+        for (int y = 0; y < kRows; ++y) odd[y][threadIdx.x] = Odd{0, 0};
 #pragma unroll
         for (int y = 0; y < kRows; ++y) {
-            // z[8 s + e] is key 16 s + 8 half + e of the tile
-            float largest = kNegBig;
-#pragma unroll
-            for (int s = 0; s < 2; ++s) {
-                const int key0 = first_key(lp_now, s);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    float x = score_of<kCap>(a, z[y][8 * s + e]);
-                    x = fmaf(-row[y].slope, fabsf((float)(row[y].p - key0 - e)), x);
-                    const bool see = key0 + e >= row[y].lo && key0 + e <= row[y].hi;
-                    if (part) x = see ? x : -INFINITY;
-                    z[y][8 * s + e] = x;
-                    largest = fmaxf(largest, x);
-                }
-            }
-            largest = fmaxf(largest, __shfl_xor(largest, 32));
-            const float m_new = fmaxf(m[y], largest);
-            if (__any(m_new > m[y])) {
-                const float alpha = __builtin_amdgcn_exp2f(m[y] - m_new);
-                l[y] *= alpha;
-#pragma unroll
-                for (int d = 0; d < 4; ++d)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) o[y][d][i] *= alpha;
-                m[y] = m_new;
-            }
-            float sum = 0.f;
-#pragma unroll
-            for (int s = 0; s < 2; ++s)
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const float w = __builtin_amdgcn_exp2f(z[y][8 * s + e] - m[y]);
-                    sum += w;
-                    const __bf16 top = (__bf16)w;
-                    hi_part[y][s][e] = top;
-                    lo_part[y][s][e] = (__bf16)(w - (float)top);
-                }
-            l[y] += sum;
-        }
-        // keys that a row does not see weigh nothing, but nothing times a value that is not finite is NaN, and a remainder may be nothing or
-        // negative: such values are taken out of the product, and what they do to the rows that see them is added by itself
-        if (__builtin_expect(not_finite(v), 0)) {
-            __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-            for (int y = 0; y < kRows; ++y) {
-                bf16x8 seen[2], lowest[2];            // (a score of -infinity weighs nothing: that times an infinity is NaN, both of them here)
-#pragma unroll
-                for (int s = 0; s < 2; ++s) {
-                    const int key0 = first_key(lp_now, s);
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        const bool see = key0 + e >= row[y].lo && key0 + e <= row[y].hi;
-                        seen[s][e] = (__bf16)(see ? 1.f : 0.f);
-                        lowest[s][e] = (__bf16)(see && z[y][8 * s + e] == -INFINITY ? 1.f : 0.f);
-                    }
-                }
-#pragma unroll
-                for (int d = 0; d < 4; ++d)
-#pragma unroll
-                    for (int sign = 0; sign < 2; ++sign) {
-                        f32x16 n;
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) n[i] = 0.f;
-#pragma unroll
-                        for (int s = 0; s < 2; ++s) {
-                            n = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(not_finite_of(v[d][s], sign)), seen[s], n, 0, 0, 0);
-                            n = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(not_finite_of(v[d][s], !sign)), lowest[s], n, 0, 0, 0);
-                        }
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) o[y][d][i] += n[i] > 0.f ? (sign ? -INFINITY : INFINITY) : 0.f;
-                        __builtin_amdgcn_sched_barrier(0);          // (one after the other: this is rare, and registers are not)
-                    }
-            }
+            m[y] = kNegBig;
+            l[y] = 0.f;
 #pragma unroll
             for (int d = 0; d < 4; ++d)
 #pragma unroll
-                for (int s = 0; s < 2; ++s) v[d][s] = finite_of(v[d][s]);
+                for (int i = 0; i < 16; ++i) o[y][d][i] = 0.f;
         }
+
+        // logical pages of a tile (one that is none of the sequence's: -1), and their physical ones
+        const auto pages_of = [&](int tile, int (&page)[PPT], int (&phys)[PPT]) {
 #pragma unroll
-        for (int d = 0; d < 4; ++d)
+            for (int s = 0; s < PPT; ++s) {
+                const int i = tile * PPT + s;
+                int p = i;
+                if constexpr (kList) p = load_same(ids, min(i, a.max_sel - 1));
+                page[s] = i < n_list && p >= 0 && p < P ? p : -1;
+                phys[s] = load_same(table, max(page[s], 0));
+            }
+        };
+        const auto fetch = [&](const int (&phys)[PPT], int stage) {
+            const uint32_t to = ring_lds + (uint32_t)stage * 16384;
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                const int64_t at = ((int64_t)phys[s * PPT / 2] * H + h) * (B * kHeadDim) + (PPT == 1 ? s * 2048 : 0);
+                load_4k(to + s * 4096, a.k_pool + at, from.key[0], from.key[1], from.key[2], from.key[3]);
+                load_4k(to + 8192 + s * 4096, a.v_pool + at, from.value, from.value, from.value, from.value);
+            }
+        };
+
+        int lp[PPT], lp_next[PPT], lp_last[PPT], phys[PPT];
+        if (t < t_end) {
+            pages_of(t, lp, phys);
+            fetch(phys, 0);
+            if (t + 4 < t_end) {
+                pages_of(t + 4, lp_next, phys);
+                fetch(phys, 1);
+            }
+            pages_of(min(t + 8, t_end - 1), lp_last, phys);
+        }
+        __syncthreads();                              // the queries
+        for (int stage = 0; t < t_end; t += 4, stage ^= 1) {
+            const uint4* keys = ring_own + stage * 1024;
+            const uint4* values = keys + 512;
+            if (t + 4 < t_end) loads_left<16>();
+            else loads_left<0>();
+            // whether a row may see less than all of the tile
+            int less = 0;
+#pragma unroll
+            for (int s = 0; s < PPT; ++s) less |= lp[s] | (lp[s] * B - all_lo) | (all_hi - lp[s] * B - B + 1);
+            const bool part = __builtin_amdgcn_readfirstlane(less) < 0;
+            f32x16 z[kRows];
 #pragma unroll
             for (int y = 0; y < kRows; ++y)
 #pragma unroll
-                for (int s = 0; s < 2; ++s) {
-                    o[y][d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(v[d][s]), hi_part[y][s], o[y][d], 0, 0, 0);
-                    o[y][d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(v[d][s]), lo_part[y][s], o[y][d], 0, 0, 0);
-                }
-        load_v(phys);
-    }
+                for (int i = 0; i < 16; ++i) z[y][i] = 0.f;
+#pragma unroll
+            for (int s = 0; s < 8; ++s) {
+                const bf16x8 k = as_bf16x8(keys[key_piece(key_of_col(col), half, s)]);
+#pragma unroll
+                for (int y = 0; y < kRows; ++y) z[y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, as_bf16x8(queries[(32 * y + col) * 16 + ((2 * s + half) ^ (col & 15))]), z[y], 0, 0, 0);
+            }
+            uint4 v[4][2];
+#pragma unroll
+            for (int d = 0; d < 4; ++d)
+#pragma unroll
+                for (int s = 0; s < 2; ++s) v[d][s] = values[value_piece<B>(32 * d + col, half, s)];
 
-    // the workgroup's waves: O^T[dim 32 d + 8 (i / 4) + 4 half + i % 4][row col]
+            const auto first_key = [&](int s) {       // of the eight keys that a lane has of step s
+                const int page = lp[s * PPT / 2];
+                return page < 0 ? INT32_MIN / 2 : page * B + (16 * s) % B + 8 * half;
+            };
+            bf16x8 hi_part[kRows][2], lo_part[kRows][2];
+            Seen seen[kRows];
 #pragma unroll
-    for (int y = 0; y < kRows; ++y) {
-        l[y] += __shfl_xor(l[y], 32);
-        if (half == 0) {
-            wave_m[wave][32 * y + col] = m[y];
-            wave_l[wave][32 * y + col] = l[y];
+            for (int y = 0; y < kRows; ++y) {
+                // z[8 s + e] is key 16 s + 8 half + e of the tile
+                float largest = kNegBig;
+                seen[y].any = part ? 0u : 0xffffu;
+                seen[y].lowest = 0;
+#pragma unroll
+                for (int s = 0; s < 2; ++s) {
+                    const int key0 = first_key(s);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        float x = score_of<kCap>(a, z[y][8 * s + e]);
+                        x = fmaf(-row[y].slope, fabsf((float)(row[y].p - key0 - e)), x);
+                        if (part) {
+                            const bool see = key0 + e >= row[y].lo && key0 + e <= row[y].hi;
+                            seen[y].any |= see ? 1u << (8 * s + e) : 0u;
+                            x = see ? x : -INFINITY;
+                        }
+                        seen[y].lowest |= x == -INFINITY ? 1u << (8 * s + e) : 0u;
+                        z[y][8 * s + e] = x;
+                        largest = fmaxf(largest, x);
+                    }
+                }
+                seen[y].lowest &= seen[y].any;
+                largest = fmaxf(largest, __shfl_xor(largest, 32));
+                const float m_new = fmaxf(m[y], largest);
+                if (__any(m_new > m[y])) {
+                    const float alpha = __builtin_amdgcn_exp2f(m[y] - m_new);
+                    l[y] *= alpha;
+#pragma unroll
+                    for (int d = 0; d < 4; ++d)
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) o[y][d][i] *= alpha;
+                    __builtin_amdgcn_sched_barrier(0);
+                    m[y] = m_new;
+                }
+                float sum = 0.f;
+#pragma unroll
+                for (int s = 0; s < 2; ++s)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const float w = __builtin_amdgcn_exp2f(z[y][8 * s + e] - m[y]);
+                        sum += w;
+                        const __bf16 top = (__bf16)w;
+                        hi_part[y][s][e] = top;
+                        lo_part[y][s][e] = (__bf16)(w - (float)top);
+                    }
+                l[y] += sum;
+            }
+            // keys that a row does not see weigh nothing, but nothing times a value that is not finite is NaN, and a remainder may be nothing or
+            // negative: such values are taken out of the product, and what they do to the rows that see them is noted by itself
+            Magnitudes most = {0, 0};
+#pragma unroll
+            for (int d = 0; d < 4; ++d) most = larger(larger(most, v[d][0]), v[d][1]);
+            if (__builtin_expect(not_finite(most), 0)) {
+#pragma unroll
+                for (int y = 0; y < kRows; ++y) note_not_finite<B>(&odd[y][threadIdx.x], values, 0, col, half, seen[y]);
+                any_odd = true;
+#pragma unroll
+                for (int d = 0; d < 4; ++d)
+#pragma unroll
+                    for (int s = 0; s < 2; ++s) v[d][s] = finite_of(v[d][s]);
+            }
+            // the tile's LDS is free: the one after the next into it
+            if (t + 8 < t_end) {
+                reads_done();
+                fetch(phys, stage);
+            }
+#pragma unroll
+            for (int s = 0; s < PPT; ++s) {
+                lp[s] = lp_next[s];
+                lp_next[s] = lp_last[s];
+            }
+            pages_of(min(t + 12, t_end - 1), lp_last, phys);
+#pragma unroll
+            for (int d = 0; d < 4; ++d)
+#pragma unroll
+                for (int y = 0; y < kRows; ++y)
+#pragma unroll
+                    for (int s = 0; s < 2; ++s) {
+                        o[y][d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(v[d][s]), hi_part[y][s], o[y][d], 0, 0, 0);
+                        o[y][d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(v[d][s]), lo_part[y][s], o[y][d], 0, 0, 0);
+                    }
         }
-    }
-    __syncthreads();
-    const bool whole = n_splits == 1;
+
+        if (any_odd)
 #pragma unroll
-    for (int y = 0; y < kRows; ++y) {
-        float top = kNegBig, sum = 0.f;
+            for (int y = 0; y < kRows; ++y) add_not_finite(o[y], odd[y][threadIdx.x]);
+
+        // the workgroup's waves: O^T[dim 32 d + 8 (i / 4) + 4 half + i % 4][row col]
 #pragma unroll
-        for (int w = 0; w < 4; ++w) top = fmaxf(top, wave_m[w][32 * y + col]);
-#pragma unroll
-        for (int w = 0; w < 4; ++w) sum += wave_l[w][32 * y + col] * __builtin_amdgcn_exp2f(wave_m[w][32 * y + col] - top);
-        const float by = __builtin_amdgcn_exp2f(m[y] - top), inv = sum == 0.f ? 0.f : 1.f / sum;
-        const int64_t part = (part0 + split) * (32 * kRows) + 32 * y + col;
-#pragma unroll
-        for (int d = 0; d < 4; ++d) {
-            float(&buf)[4][16][64] = comb[d & 1];
-#pragma unroll
-            for (int i = 0; i < 16; ++i) buf[wave][i][lane] = o[y][d][i] * by;
-            __syncthreads();
-            float x[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) x[i] = (buf[0][4 * wave + i][lane] + buf[1][4 * wave + i][lane]) + (buf[2][4 * wave + i][lane] + buf[3][4 * wave + i][lane]);
-            const int dim = 32 * d + 8 * wave + 4 * half;
-            if (whole) {
-                if (row[y].there)
-                    *reinterpret_cast<uint2*>(a.out + row[y].at * kHeadDim + dim) = make_uint2(two_bf16(x[0] * inv, x[1] * inv), two_bf16(x[2] * inv, x[3] * inv));
-            } else {
-                uint64_t* at = reinterpret_cast<uint64_t*>(a.part_acc + part * kHeadDim + dim);
-                publish_u64(at, __builtin_bit_cast(uint64_t, make_float2(x[0], x[1])));
-                publish_u64(at + 1, __builtin_bit_cast(uint64_t, make_float2(x[2], x[3])));
+        for (int y = 0; y < kRows; ++y) {
+            l[y] += __shfl_xor(l[y], 32);
+            if (half == 0) {
+                wave_m[wave][32 * y + col] = m[y];
+                wave_l[wave][32 * y + col] = l[y];
             }
         }
-        if (!whole && wave == 0 && half == 0) publish_u64(reinterpret_cast<uint64_t*>(a.part_ml) + part, __builtin_bit_cast(uint64_t, make_float2(top, sum)));
+        __syncthreads();                              // (and no wave's tiles are read or written any more)
+        float(*comb)[4][16][64] = reinterpret_cast<float(*)[4][16][64]>(ring);
+        const int w0 = line / share, n_parts = (line_end - 1) / share - w0 + 1;
+        const bool whole = n_parts == 1;
+        const int64_t part0 = 2 * ((int64_t)h * a.n_slots + w0);
+        const int64_t part_own = 2 * ((int64_t)h * a.n_slots + slot) + (slot == w0 ? 1 : 0);
+#pragma unroll
+        for (int y = 0; y < kRows; ++y) {
+            float top = kNegBig, sum = 0.f;
+#pragma unroll
+            for (int w = 0; w < 4; ++w) top = fmaxf(top, wave_m[w][32 * y + col]);
+#pragma unroll
+            for (int w = 0; w < 4; ++w) sum += wave_l[w][32 * y + col] * __builtin_amdgcn_exp2f(wave_m[w][32 * y + col] - top);
+            const float by = __builtin_amdgcn_exp2f(m[y] - top), inv = sum == 0.f ? 0.f : 1.f / sum;
+            const int64_t part = part_own * (32 * kRows) + 32 * y + col;
+#pragma unroll
+            for (int d = 0; d < 4; ++d) {
+                float(&buf)[4][16][64] = comb[d];
+#pragma unroll
+                for (int i = 0; i < 16; ++i) buf[wave][i][lane] = o[y][d][i] * by;
+            }
+            __syncthreads();
+#pragma unroll
+            for (int d = 0; d < 4; ++d) {
+                float(&buf)[4][16][64] = comb[d];
+                float x[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) x[i] = (buf[0][4 * wave + i][lane] + buf[1][4 * wave + i][lane]) + (buf[2][4 * wave + i][lane] + buf[3][4 * wave + i][lane]);
+                const int dim = 32 * d + 8 * wave + 4 * half;
+                if (whole) {
+                    if (row[y].there)
+                        *reinterpret_cast<uint2*>(a.out + row[y].at * kHeadDim + dim) = make_uint2(two_bf16(x[0] * inv, x[1] * inv), two_bf16(x[2] * inv, x[3] * inv));
+                } else {
+                    uint64_t* to = reinterpret_cast<uint64_t*>(a.part_acc + part * kHeadDim + dim);
+                    publish_u64(to, __builtin_bit_cast(uint64_t, make_float2(x[0], x[1])));
+                    publish_u64(to + 1, __builtin_bit_cast(uint64_t, make_float2(x[2], x[3])));
+                }
+            }
+            if (!whole && wave == 0 && half == 0) publish_u64(reinterpret_cast<uint64_t*>(a.part_ml) + part, __builtin_bit_cast(uint64_t, make_float2(top, sum)));
+            __syncthreads();
+        }
+        if (!whole && arrive_last(a.arrivals + ((int64_t)b * H + h) * kArrivalStride, n_parts, &flag))
+            merge_parts<32 * kRows, 256>(a, span, h, 0, n_rows, n_parts, [&](int s) { return part0 + 2 * s + (s == 0 ? 1 : 0); });
+        line = line_end;
     }
-    if (whole) return;
-    if (!arrive_last(a.arrivals + ((int64_t)b * H + h) * kArrivalStride + blockIdx.y, n_splits, &flag)) return;
-    merge_parts<32 * kRows, 256>(a, span, h, row0, n_rows, part0, n_splits);
+}
+
+// ---- many rows (prompts): the rows are split ----------------------------------------------------------------------------------------------
+// A unit is 128 rows (token, head of the group) of a sequence and KV head, 32 a wave, and a run of tiles of 64 keys (32 KB) that its workgroup brings to
+// LDS for all of them, the next while one is worked on.  The same products as above, twice as many keys at a time, but the weights are bf16: an output is
+// rounded to bf16 all the same, and its weights' roundings come to less than that (the sum of the weights is of the unrounded ones).
+// A plan says which units there are (plan_kernel): tiles that no row of a block sees are left out, and long blocks are cut where there are too
+// few to fill the card; partials are merged by the last unit of a block to arrive.
+// Bound: the matrix units and the exponentials beside them, 32 products of 32 cycles and 32 exponentials a lane for a tile and wave.
+
+constexpr int kBlockRows = 128;
+constexpr int kManyStage = 2048;                      // 16-byte pieces of a tile: 1024 of keys, 1024 of values
+constexpr int kPlanThreads = 1024;
+
+__device__ __forceinline__ int blocks_of(int n_new, int G) { return (int)(((int64_t)n_new * G + kBlockRows - 1) / kBlockRows); }
+
+// The keys that a block's rows see at all: first and last (last < first: none).
+struct Keys { int first, last; };
+__device__ __forceinline__ Keys keys_of_block(const AttendArgs& a, const Span& s, int b, int block)
+{
+    const int G = a.group, row_end = min((block + 1) * kBlockRows, s.n_new * G) - 1;
+    const int i0 = (int)((unsigned)(block * kBlockRows) / (unsigned)G), i1 = (int)((unsigned)row_end / (unsigned)G);
+    const int p0 = s.len - s.n_new + i0, p1 = s.len - s.n_new + i1;
+    Keys k{a.window > 0 ? max(p0 - a.window + 1, 0) : 0, min(a.prefix_lens != nullptr ? max(p1, a.prefix_lens[b] - 1) : p1, s.len - 1)};
+    if (a.first_keys != nullptr) {
+        int first = INT32_MAX;
+        for (int i = i0; i <= i1; ++i) first = min(first, a.first_keys[s.start + i]);
+        k.first = max(k.first, first);
+    }
+    if (p1 < 0) k.last = -1;
+    return k;
+}
+
+// One workgroup.  Blocks in sequence order: their tiles; how long a unit may be (by what the card would take for it, of sixteen lengths); the units, longest
+// first as far as it is known (whole lengths, then the rest), and which partials they leave.
+template <int B>
+__global__ __launch_bounds__(kPlanThreads) void plan_kernel(AttendArgs a)
+{
+    constexpr int kWaves = kPlanThreads / 64, kTry = 16;
+    extern __shared__ int upto[];                     // [batch]: blocks of the sequences up to this one
+    __shared__ int of_wave[kWaves], counts[kTry], n_tiles_most;
+    __shared__ int64_t n_tiles_all;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    // a running sum over all threads' numbers, chunk by chunk
+    const auto sum_before = [&](int v, int* all) {
+        const int own = lanes_upto(v);
+        __syncthreads();
+        if (lane == 63) of_wave[wave] = own;
+        __syncthreads();
+        int base = 0, sum = 0;
+        for (int w = 0; w < kWaves; ++w) {
+            if (w == wave) base = sum;
+            sum += of_wave[w];
+        }
+        *all = sum;
+        return base + own - v;
+    };
+    int n_blocks = 0;
+    for (int b0 = 0; b0 < a.batch; b0 += kPlanThreads) {
+        const int b = b0 + (int)threadIdx.x;
+        const int v = b < a.batch ? blocks_of(span_by_lane(a, b, B).n_new, a.group) : 0;
+        int all;
+        const int before = sum_before(v, &all);
+        if (b < a.batch) upto[b] = n_blocks + before + v;
+        n_blocks += all;
+    }
+    if (threadIdx.x < kTry) counts[threadIdx.x] = 0;
+    if (threadIdx.x == 0) {
+        n_tiles_most = 1;
+        n_tiles_all = 0;
+    }
+    __syncthreads();
+    n_blocks = min(n_blocks, a.blocks_most);
+    for (int i = threadIdx.x; i < n_blocks; i += kPlanThreads) {
+        int lo = 0, hi = a.batch - 1;                 // the first sequence whose blocks go beyond i
+        while (lo < hi) {
+            const int mid = (lo + hi) / 2;
+            if (upto[mid] > i) hi = mid;
+            else lo = mid + 1;
+        }
+        const int block = i - (lo > 0 ? upto[lo - 1] : 0);
+        const Span s = span_by_lane(a, lo, B);
+        const Keys k = keys_of_block(a, s, lo, block);
+        const bool any = k.last >= k.first;
+        const int first = any ? k.first / 64 : 0, n = a.page_ids != nullptr ? 1 : any ? k.last / 64 - first + 1 : 1;
+        a.blocks[i] = make_int4(lo, block, first, n);
+        atomicMax(&n_tiles_most, n);
+        atomicAdd(reinterpret_cast<unsigned long long*>(&n_tiles_all), (unsigned long long)n);
+        for (int h = 0; h < a.n_kv_heads; ++h) a.counters[(int64_t)i * a.n_kv_heads + h] = 0;
+    }
+    __syncthreads();
+    // units of each length tried
+    const int most = n_tiles_most;
+    const auto length = [&](int y) { return max((most + y) / (y + 1), 1); };
+    for (int i = threadIdx.x; i < n_blocks; i += kPlanThreads) {
+        const int n = a.blocks[i].w;
+        for (int y = 0; y < kTry; ++y) atomicAdd(&counts[y], (n + length(y) - 1) / length(y));
+    }
+    __syncthreads();
+    // what they would take, in tiles: a unit costs some of its own, and a cut one the partials'
+    const float slots = (float)a.n_slots, heads = (float)a.n_kv_heads, all_tiles = (float)n_tiles_all;
+    int best = 0;
+    float least = INFINITY;
+    for (int y = 0; y < kTry; ++y) {
+        const int len = length(y), units = counts[y], extra = units - n_blocks;
+        if (y > 0 && (len < 8 || extra > a.extra_most)) break;
+        const float own = 5.f, size = (float)len + own, work = heads * (all_tiles + own * (float)units + (extra > 0 ? 6.f * (float)units : 0.f));
+        const float rounds = work / (slots * size);
+        const float cost = rounds >= 4.f ? work / slots + 0.5f * size : ceilf(rounds) * size + (extra > 0 ? 6.f : 0.f);
+        if (cost < 0.97f * least) {
+            least = cost;
+            best = y;
+        }
+    }
+    const int len = length(best);
+    __syncthreads();
+    // whole lengths first, then what is left of the blocks
+    int n_whole_all = 0, units_before = 0, parts_before = 0;
+    for (int i0 = 0; i0 < n_blocks; i0 += kPlanThreads) {
+        const int i = i0 + (int)threadIdx.x;
+        int all;
+        const int v = i < n_blocks ? a.blocks[i].w / len : 0;
+        sum_before(v, &all);
+        n_whole_all += all;
+    }
+    int rest_before = n_whole_all;
+    for (int i0 = 0; i0 < n_blocks; i0 += kPlanThreads) {
+        const int i = i0 + (int)threadIdx.x;
+        const int4 blk = i < n_blocks ? a.blocks[i] : make_int4(0, 0, 0, 0);
+        const int whole = blk.w / len, rest = blk.w - whole * len, n = whole + (rest > 0 ? 1 : 0);
+        int all;
+        int at = units_before + sum_before(whole, &all);
+        units_before += all;
+        const int at_rest = rest_before + sum_before(rest > 0 ? 1 : 0, &all);
+        rest_before += all;
+        const int part0 = parts_before + sum_before(n > 1 ? n : 0, &all);
+        parts_before += all;
+        for (int s = 0; s < n; ++s) {
+            const int to = s < whole ? at + s : at_rest;
+            AttendUnit u;
+            u.b = blk.x; u.block = blk.y;
+            u.first = blk.z + s * len;
+            u.end = a.page_ids != nullptr ? INT32_MAX : blk.z + min((s + 1) * len, blk.w);
+            u.n_parts = n; u.part = part0 + s; u.part0 = part0; u.counter = i;
+            a.units[to] = u;
+        }
+    }
+    if (threadIdx.x == 0) *a.n_units = rest_before;
+}
+
+template <int B, bool kList, bool kGeneral>
+__global__ __launch_bounds__(256, 2) void attend_many_kernel(AttendArgs a)
+{
+    constexpr int PPT = 64 / B;
+    extern __shared__ uint4 stages[];                 // [2][kManyStage]
+    __shared__ Odd odd[256];
+    __shared__ int flag;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+    const int col = lane & 31, half = lane >> 5;
+    const int H = a.n_kv_heads, G = a.group, h = blockIdx.x % H, unit = blockIdx.x / H;
+    if (unit >= load_same(a.n_units, 0)) return;
+    const auto of_unit = [&](int i) { return load_same(reinterpret_cast<const int32_t*>(a.units + unit), i); };
+    const int b = of_unit(0), block = of_unit(1), n_parts = of_unit(4);
+    int t = of_unit(2), t_end = of_unit(3);
+    const Span span = span_of(a, b, B);
+    const int P = span.pages, n_rows = span.n_new * G, row0 = block * kBlockRows + 32 * wave;
+    const int32_t* table = a.block_table + (int64_t)b * a.max_pages;
+    const int32_t* ids = kList ? a.page_ids + ((int64_t)b * H + h) * a.max_sel : nullptr;
+    const int n_list = kList ? min(max(load_same(a.n_selected, (int64_t)b * H + h), 0), a.max_sel) : P;
+    if constexpr (kList) {
+        t = 0;
+        t_end = (n_list + PPT - 1) / PPT;
+    }
+    if (P == 0) t_end = 0;
+
+    // a wave brings 16 keys and their values
+    const PageLanes from(lane, B);
+    const uint32_t to = lds_at(stages) + (uint32_t)wave * 4096;
+    const auto page_at = [&](int i) {
+        int p = i;
+        if constexpr (kList) p = load_same(ids, min(i, a.max_sel - 1));
+        return i < n_list && p >= 0 && p < P ? p : -1;
+    };
+    const auto fetch = [&](int phys, int stage) {
+        const int64_t at = ((int64_t)phys * H + h) * (B * kHeadDim) + (B == 32 ? (wave & 1) * 2048 : 0);
+        load_4k(to + (uint32_t)stage * (kManyStage * 16), a.k_pool + at, from.key[0], from.key[1], from.key[2], from.key[3]);
+        load_4k(to + (uint32_t)stage * (kManyStage * 16) + 16384, a.v_pool + at, from.value, from.value, from.value, from.value);
+    };
+    const auto phys_of = [&](int tile) { return load_same(table, max(page_at(tile * PPT + (B == 32 ? wave >> 1 : wave)), 0)); };
+    int phys = 0;
+    if (t < t_end) {
+        fetch(phys_of(t), 0);
+        phys = phys_of(min(t + 1, t_end - 1));
+    }
+
+    RowView row = view_of(a, span, b, h, row0 + col);
+    const bool works = row0 < n_rows;                 // a wave without rows only brings its keys
+    uint4 q[8];
+    {
+        const uint4* src = reinterpret_cast<const uint4*>(a.q + row.at * kHeadDim) + half;
+#pragma unroll
+        for (int s = 0; s < 8; ++s) q[s] = src[2 * s];
+    }
+    const int all_lo = lanes_max(row.there ? row.lo : 0), all_hi = lanes_min(row.there ? row.hi : INT32_MAX);
+
+    float m = kNegBig, l = 0.f;
+    f32x16 o[4];
+    bool any_odd = false;
+    odd[threadIdx.x] = Odd{0, 0};
+#pragma unroll
+    for (int d = 0; d < 4; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
+
+    int stage = 0;
+    const uint4 *keys, *values;
+    // the next tile is there, and nobody reads the last one any more: the one behind it into that one's place
+    const auto begin_tile = [&] {
+        loads_left<0>();
+        __syncthreads();
+        if (t + 1 < t_end) {
+            fetch(phys, stage ^ 1);
+            phys = phys_of(min(t + 2, t_end - 1));
+        }
+        keys = stages + stage * kManyStage;
+        values = keys + 1024;
+    };
+    const auto end_tile = [&] {
+        ++t;
+        stage ^= 1;
+    };
+    // whether every row sees all of tile t (the same in every lane)
+    const auto is_whole = [&] {
+        if constexpr (!kList) return ((t * 64 - all_lo) | (all_hi - t * 64 - 63)) >= 0;
+        int less = 0;
+#pragma unroll
+        for (int s = 0; s < PPT; ++s) {
+            const int p = page_at(t * PPT + s);
+            less |= p | (p * B - all_lo) | (all_hi - p * B - B + 1);
+        }
+        return less >= 0;
+    };
+    const auto first_key = [&](int i) {               // of a lane's eight keys of step i
+        const int p = page_at(t * PPT + 16 * i / B);
+        return p < 0 ? INT32_MIN / 2 : p * B + (16 * i) % B + 8 * half;
+    };
+    // scores of 32 keys, from y on; z[8 s + e] is key 32 y + 16 s + 8 half + e of the tile
+    const auto scores = [&](f32x16& z, int y) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) z[i] = 0.f;
+#pragma unroll
+        for (int s = 0; s < 8; ++s)
+            z = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(keys[key_piece(32 * y + key_of_col(col), half, s)]), as_bf16x8(q[s]), z, 0, 0, 0);
+        if constexpr (kGeneral) {
+            if (a.cap_in != 0.f) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) z[i] = score_of<true>(a, z[i]);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) z[i] = score_of<false>(a, z[i]);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            if (a.slopes != nullptr)
+#pragma unroll
+                for (int s = 0; s < 2; ++s) {
+                    const float d = (float)(row.p - first_key(2 * y + s));
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) z[8 * s + e] = fmaf(-row.slope, fabsf(d - (float)e), z[8 * s + e]);
+                }
+        }
+    };
+    const float scale = kGeneral ? 1.f : a.scale_log2;
+    // the running maximum (of scores times `scale`), and what was summed, to a new one
+    const auto raise = [&](float largest) {
+        const float m_new = fmaxf(m, product(fmaxf(largest, __shfl_xor(largest, 32)), scale));
+        if (__any(m_new > m)) {
+            const float alpha = __builtin_amdgcn_exp2f(m - m_new);
+            l *= alpha;
+#pragma unroll
+            for (int d = 0; d < 4; ++d)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) o[d][i] *= alpha;
+            m = m_new;
+        }
+    };
+    // a score times `scale` this large is rounded before the difference, as the maximum was: what one rounding would keep could weigh more than 1
+    const auto is_large = [&] { return !kGeneral && __any(fabsf(m) > 0x1p24f && m != kNegBig); };
+    while (!works && t < t_end) {
+        begin_tile();
+        end_tile();
+    }
+    while (t < t_end) {
+        for (; t < t_end && is_whole(); end_tile()) {
+            begin_tile();
+            f32x16 z[2];
+            scores(z[0], 0);
+            scores(z[1], 1);
+            float largest = z[0][0];
+#pragma unroll
+            for (int y = 0; y < 2; ++y)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) largest = fmaxf(largest, z[y][i]);
+            raise(largest);
+            float by = scale, top = m;
+            if (__builtin_expect(is_large(), 0)) {
+#pragma unroll
+                for (int y = 0; y < 2; ++y)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) z[y][i] = product(z[y][i], scale) - m;
+                by = 1.f;
+                top = 0.f;
+            }
+            float sum = 0.f;
+            bf16x8 w[2][2];
+#pragma unroll
+            for (int y = 0; y < 2; ++y)
+#pragma unroll
+                for (int s = 0; s < 2; ++s)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const float x = __builtin_amdgcn_exp2f(kGeneral ? z[y][8 * s + e] - top : fmaf(z[y][8 * s + e], by, -top));
+                        sum += x;
+                        w[y][s][e] = (__bf16)x;
+                    }
+            l += sum;
+#pragma unroll
+            for (int d = 0; d < 4; ++d)
+#pragma unroll
+                for (int s = 0; s < 4; ++s)
+                    o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(values[value_piece<B>(32 * d + col, half, s)]), w[s >> 1][s & 1], o[d], 0, 0, 0);
+        }
+        // tiles that not every row sees whole: 32 keys at a time
+        for (; t < t_end && !is_whole(); end_tile()) {
+            begin_tile();
+#pragma nounroll
+            for (int y = 0; y < 2; ++y) {
+                f32x16 z;
+                scores(z, y);
+                Seen seen;
+                float largest = kNegBig;
+#pragma unroll
+                for (int s = 0; s < 2; ++s) {
+                    const int key0 = first_key(2 * y + s);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const bool see = key0 + e >= row.lo && key0 + e <= row.hi;
+                        seen.any |= see ? 1u << (8 * s + e) : 0u;
+                        seen.lowest |= see && z[8 * s + e] == -INFINITY ? 1u << (8 * s + e) : 0u;
+                        z[8 * s + e] = see ? z[8 * s + e] : -INFINITY;
+                        largest = fmaxf(largest, z[8 * s + e]);
+                    }
+                }
+                raise(largest);
+                float by = scale, top = m;
+                if (__builtin_expect(is_large(), 0)) {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) z[i] = product(z[i], scale) - m;
+                    by = 1.f;
+                    top = 0.f;
+                }
+                float sum = 0.f;
+                bf16x8 w[2];
+#pragma unroll
+                for (int s = 0; s < 2; ++s)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const float x = __builtin_amdgcn_exp2f(kGeneral ? z[8 * s + e] - top : fmaf(z[8 * s + e], by, -top));
+                        sum += x;
+                        w[s][e] = (__bf16)x;
+                    }
+                l += sum;
+                __builtin_amdgcn_sched_barrier(0);    // (the values are not asked for earlier: registers are not free)
+                uint4 v[4][2];
+                Magnitudes most = {0, 0};
+#pragma unroll
+                for (int d = 0; d < 4; ++d)
+#pragma unroll
+                    for (int s = 0; s < 2; ++s) {
+                        v[d][s] = values[value_piece<B>(32 * d + col, half, 2 * y + s)];
+                        most = larger(most, v[d][s]);
+                    }
+                // (values that are not finite, as above; where every row sees every key there is nothing to take out)
+                if (__builtin_expect(not_finite(most), 0)) {
+                    any_odd = true;
+                    note_not_finite<B>(odd + threadIdx.x, values, 2 * y, col, half, seen);
+                    asm volatile("" : : : "memory");  // (read again: registers are not free)
+#pragma unroll
+                    for (int d = 0; d < 4; ++d)
+#pragma unroll
+                        for (int s = 0; s < 2; ++s) v[d][s] = finite_of(values[value_piece<B>(32 * d + col, half, 2 * y + s)]);
+                }
+#pragma unroll
+                for (int d = 0; d < 4; ++d)
+#pragma unroll
+                    for (int s = 0; s < 2; ++s) o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(v[d][s]), w[s], o[d], 0, 0, 0);
+            }
+        }
+    }
+
+    if (any_odd) add_not_finite(o, odd[threadIdx.x]);
+    l += __shfl_xor(l, 32);
+    if (n_parts == 1) {
+        const float inv = l == 0.f ? 0.f : 1.f / l;
+        int r = row0 + col;
+        asm volatile("" : "+v"(r));                   // (worked out again, not kept: registers are not free)
+        const int64_t at = row_at(a, span, h, r);
+        if (r < n_rows)
+#pragma unroll
+            for (int d = 0; d < 4; ++d)
+#pragma unroll
+                for (int i = 0; i < 16; i += 4)
+                    *reinterpret_cast<uint2*>(a.out + at * kHeadDim + 32 * d + 2 * i + 4 * half) =
+                        make_uint2(two_bf16(o[d][i] * inv, o[d][i + 1] * inv), two_bf16(o[d][i + 2] * inv, o[d][i + 3] * inv));
+        return;
+    }
+    const int64_t part_rows = ((int64_t)of_unit(5) * H + h) * kBlockRows + 32 * wave + col;
+    if (works) {
+#pragma unroll
+        for (int d = 0; d < 4; ++d)
+#pragma unroll
+            for (int i = 0; i < 16; i += 4) {
+                uint64_t* at = reinterpret_cast<uint64_t*>(a.part_acc + part_rows * kHeadDim + 32 * d + 2 * i + 4 * half);
+                publish_u64(at, __builtin_bit_cast(uint64_t, make_float2(o[d][i], o[d][i + 1])));
+                publish_u64(at + 1, __builtin_bit_cast(uint64_t, make_float2(o[d][i + 2], o[d][i + 3])));
+            }
+        if (half == 0) publish_u64(reinterpret_cast<uint64_t*>(a.part_ml) + part_rows, __builtin_bit_cast(uint64_t, make_float2(m, l)));
+    }
+    if (!arrive_last(a.counters + (int64_t)of_unit(7) * H + h, n_parts, &flag)) return;
+    const int64_t part0 = (int64_t)of_unit(6) * H + h;
+    merge_parts<kBlockRows, 256>(a, span, h, block * kBlockRows, n_rows, n_parts, [&](int s) { return part0 + (int64_t)s * H; });
 }
 
 // ---- launch -----------------------------------------------------------------------------------------------------------------------------------
-template <int B, int kRows, bool kCap>
-static hipError_t launch_few(const AttendArgs& a, const AttendShape& s, bool list, hipStream_t stream)
+template <class Kernel>
+static hipError_t launch_lds(Kernel kernel, dim3 grid, int threads, size_t lds, hipStream_t stream, const AttendArgs& a)
 {
-    const dim3 grid((unsigned)(s.n_slots > 0 ? (int64_t)s.n_slots * a.n_kv_heads : (int64_t)a.batch * s.n_splits * a.n_kv_heads), (unsigned)s.blocks);
-    if (list) return launch(attend_few_kernel<B, kRows, true, false, kCap>, grid, dim3(256), 0, stream, a);
-    return s.n_slots > 0 ? launch(attend_few_kernel<B, kRows, false, true, kCap>, grid, dim3(256), 0, stream, a)
-                         : launch(attend_few_kernel<B, kRows, false, false, kCap>, grid, dim3(256), 0, stream, a);
+    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+    if (e != hipSuccess) return e;
+    return launch(kernel, grid, dim3(threads), lds, stream, a);
 }
 
-AttendShape attend_shape(const chess_ctx* ctx, int64_t max_new, int batch, bool list)
+template <int B, int kRows, bool kCap>
+static hipError_t launch_few(const AttendArgs& a, bool list, hipStream_t stream)
+{
+    const dim3 grid((unsigned)(a.n_slots * a.n_kv_heads));
+    return list ? launch_lds(attend_few_kernel<B, kRows, true, kCap>, grid, 256, few_lds(32 * kRows), stream, a)
+                : launch_lds(attend_few_kernel<B, kRows, false, kCap>, grid, 256, few_lds(32 * kRows), stream, a);
+}
+
+// Few rows: a line a KV head.  Many: units; `most` blocks and cut units that there can be, whatever the sequences are.
+AttendShape attend_shape(const chess_ctx* ctx, int64_t n_rows, int64_t max_new, int64_t batch)
 {
     const Geom& g = ctx->geom;
-    const int ppt = kTileTokens / g.page_size;
     AttendShape s{};
-    const int64_t rows = max_new * g.group, want = 2 * (int64_t)ctx->n_cu;
-    s.rows = rows <= 32 ? 32 : 64;
-    s.blocks = (int)cdiv(rows, s.rows);
-    const int64_t pairs = (int64_t)batch * g.n_kv_heads * s.blocks, waves = cdiv(list ? g.max_sel : g.max_pages, 4 * ppt);
-    // (an arrival counter for each block of a pair: 64)
-    s.n_splits = s.blocks > kArrivalStride ? 1 : (int)clampi(want / pairs, 1, std::min<int64_t>(waves, 64));
-    if (!list && s.blocks == 1 && batch > 1 && batch <= kDealMost && s.n_splits > 1) {
-        s.n_slots = (int)(want / g.n_kv_heads);
-        s.n_splits = (int)std::min<int64_t>(waves, 64);
+    max_new = std::min(max_new, n_rows);
+    const int64_t cu = std::max(ctx->n_cu / g.n_kv_heads, 1);
+    if (max_new * g.group <= 64) {
+        s.rows = max_new * g.group <= 32 ? 32 : 64;
+        s.n_slots = cu;
+        s.parts = 2 * cu * g.n_kv_heads;
+        return s;
     }
-    s.parts = s.n_slots > 0 ? (int64_t)s.n_slots * g.n_kv_heads : s.n_splits > 1 ? pairs * s.n_splits : 0;
+    s.rows = kBlockRows;
+    s.n_slots = 2 * (int64_t)ctx->n_cu;               // workgroups that are on the card at once
+    s.blocks = n_rows * g.group / kBlockRows + std::min(batch, n_rows);
+    s.extra = 4 * cu;
+    s.parts = 2 * s.extra * g.n_kv_heads;             // (a block of n units has n partials, and n - 1 units more than one)
     return s;
 }
 
 hipError_t launch_attend(chess_ctx* ctx, AttendArgs a, const AttendShape& s, hipStream_t stream)
 {
-    a.n_slots = s.n_slots;
-    a.n_splits = s.n_splits;
-    const bool list = a.page_ids != nullptr, cap = a.cap_in != 0.f;
-    if (ctx->geom.page_size == 16) {
-        if (s.rows == 32) return cap ? launch_few<16, 1, true>(a, s, list, stream) : launch_few<16, 1, false>(a, s, list, stream);
-        return cap ? launch_few<16, 2, true>(a, s, list, stream) : launch_few<16, 2, false>(a, s, list, stream);
+    a.n_slots = (int)s.n_slots;
+    const bool list = a.page_ids != nullptr, cap = a.cap_in != 0.f, b16 = ctx->geom.page_size == 16;
+    if (s.rows < kBlockRows) {
+        if (b16) {
+            if (s.rows == 32) return cap ? launch_few<16, 1, true>(a, list, stream) : launch_few<16, 1, false>(a, list, stream);
+            return cap ? launch_few<16, 2, true>(a, list, stream) : launch_few<16, 2, false>(a, list, stream);
+        }
+        if (s.rows == 32) return cap ? launch_few<32, 1, true>(a, list, stream) : launch_few<32, 1, false>(a, list, stream);
+        return cap ? launch_few<32, 2, true>(a, list, stream) : launch_few<32, 2, false>(a, list, stream);
     }
-    if (s.rows == 32) return cap ? launch_few<32, 1, true>(a, s, list, stream) : launch_few<32, 1, false>(a, s, list, stream);
-    return cap ? launch_few<32, 2, true>(a, s, list, stream) : launch_few<32, 2, false>(a, s, list, stream);
+    a.blocks_most = (int)s.blocks;
+    a.extra_most = (int)s.extra;
+    const hipError_t e = launch(b16 ? plan_kernel<16> : plan_kernel<32>, dim3(1), dim3(kPlanThreads), (size_t)a.batch * sizeof(int), stream, a);
+    if (e != hipSuccess) return e;
+    const dim3 grid((unsigned)((s.blocks + s.extra) * a.n_kv_heads));
+    constexpr size_t lds = 2 * kManyStage * 16;
+    const bool general = cap || a.slopes != nullptr;
+    if (b16) {
+        if (list) return general ? launch_lds(attend_many_kernel<16, true, true>, grid, 256, lds, stream, a) : launch_lds(attend_many_kernel<16, true, false>, grid, 256, lds, stream, a);
+        return general ? launch_lds(attend_many_kernel<16, false, true>, grid, 256, lds, stream, a) : launch_lds(attend_many_kernel<16, false, false>, grid, 256, lds, stream, a);
+    }
+    if (list) return general ? launch_lds(attend_many_kernel<32, true, true>, grid, 256, lds, stream, a) : launch_lds(attend_many_kernel<32, true, false>, grid, 256, lds, stream, a);
+    return general ? launch_lds(attend_many_kernel<32, false, true>, grid, 256, lds, stream, a) : launch_lds(attend_many_kernel<32, false, false>, grid, 256, lds, stream, a);
 }
 
 }  // namespace chess

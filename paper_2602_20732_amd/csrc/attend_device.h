@@ -45,6 +45,19 @@ __device__ __forceinline__ Span span_of(const AttendArgs& a, int b, int page_siz
     return s;
 }
 
+// The same where each lane asks for a sequence of its own.
+__device__ __forceinline__ Span span_by_lane(const AttendArgs& a, int b, int page_size)
+{
+    Span s;
+    s.start = a.token_start[b];
+    s.n_new = (int)((unsigned)a.token_start[b + 1] - (unsigned)s.start);
+    s.len = min(max(a.seq_lens[b], 0), a.max_pages * page_size);
+    s.pages = (s.len + page_size - 1) / page_size;
+    if (s.n_new < 0 || s.start < 0 || s.start > a.n_rows - s.n_new) s.n_new = 0;
+    s.n_new = min(s.n_new, a.max_new);
+    return s;
+}
+
 // Query row r of a sequence and KV head: head r % G of its new token r / G.  A row that is not there is the last one again, and sees nothing.
 struct RowView {
     int64_t at;              // row of q and out
@@ -52,6 +65,12 @@ struct RowView {
     float slope;             // in powers of two a position
     bool there;
 };
+
+__device__ __forceinline__ int64_t row_at(const AttendArgs& a, const Span& s, int h, int r)
+{
+    const int G = a.group, i = (int)((unsigned)r / (unsigned)G);
+    return (int64_t)(s.start + i) * (a.n_kv_heads * G) + h * G + (r - i * G);
+}
 
 __device__ __forceinline__ RowView view_of(const AttendArgs& a, const Span& s, int b, int h, int r)
 {
@@ -84,29 +103,31 @@ __device__ __forceinline__ float tanh_of(float x)
     return fabsf(x) < 0.3f ? near : far;
 }
 
+// A product that is rounded before anything is added to it.
+__device__ __forceinline__ float product(float x, float y)
+{
+#pragma clang fp contract(off)
+    return x * y;
+}
+
 // A product of query and key as a power of two.
 template <bool kCap>
 __device__ __forceinline__ float score_of(const AttendArgs& a, float qk)
 {
-    if constexpr (kCap) return a.cap_out * tanh_of(qk * a.cap_in);
-    return qk * a.scale_log2;
+    if constexpr (kCap) return product(a.cap_out, tanh_of(qk * a.cap_in));
+    return product(qk, a.scale_log2);
 }
 
-// Whether one of the wave's values is infinite or NaN: the largest of their magnitudes as bits, two at a time.
-__device__ __forceinline__ bool not_finite(const uint4 (&v)[4][2])
+// The larger magnitudes of two pairs of bf16 values and eight, as bits; whether one of them is infinite or NaN in any lane.
+typedef __attribute__((ext_vector_type(2))) unsigned short Magnitudes;
+__device__ __forceinline__ Magnitudes larger(Magnitudes most, const uint4& v)
 {
-    typedef __attribute__((ext_vector_type(2))) unsigned short pair;
-    pair most = {0, 0};
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-    for (int d = 0; d < 4; ++d)
-#pragma unroll
-        for (int s = 0; s < 2; ++s) {
-            const uint32_t w[4] = {v[d][s].x, v[d][s].y, v[d][s].z, v[d][s].w};
-#pragma unroll
-            for (int i = 0; i < 4; ++i) most = __builtin_elementwise_max(most, __builtin_bit_cast(pair, w[i] & 0x7fff7fffu));
-        }
-    return __any(most.x >= 0x7f80 || most.y >= 0x7f80);
+    for (int i = 0; i < 4; ++i) most = __builtin_elementwise_max(most, __builtin_bit_cast(Magnitudes, w[i] & 0x7fff7fffu));
+    return most;
 }
+__device__ __forceinline__ bool not_finite(Magnitudes most) { return __any(most.x >= 0x7f80 || most.y >= 0x7f80); }
 
 // Eight values: 1 (bf16) where one is +infinity (down: -infinity) or NaN, 0 elsewhere.
 __device__ __forceinline__ uint4 not_finite_of(const uint4& v, bool down)
@@ -130,22 +151,80 @@ __device__ __forceinline__ uint4 finite_of(const uint4& v)
     return make_uint4(of(v.x), of(v.y), of(v.z), of(v.w));
 }
 
-// What the last split of a block of kRowsOf rows to arrive does: out = sum_s acc_s 2^(m_s - M) / sum_s l_s 2^(m_s - M), always in split order.
-// A thread has four dims of a row; eight splits are asked for at a time.
-template <int kRowsOf, int kThreads>
-__device__ __forceinline__ void merge_parts(const AttendArgs& a, const Span& span, int h, int row0, int n_rows, int64_t part0, int n_splits)
+// Which of a lane's 64 outputs of 32 rows (bit 16 d + i: element i of the product of dims 32 d ...) get an infinity, by values that are not finite.  In LDS,
+// for each thread: this is rare, and registers are not free.
+struct Odd { uint64_t up, down; };
+
+template <int B>
+__device__ __forceinline__ int value_piece(int dim, int half, int s)
+{
+    return B == 16 ? s * 256 + dim * 2 + half : (s >> 1) * 512 + dim * 4 + ((2 * (s & 1) + half) ^ ((dim >> 2) & 3));
+}
+
+// Which of a lane's keys (bit 8 s + e of a 32 keys') its row sees, and which of those have a score of -infinity: these weigh nothing, and nothing times an
+// infinity is NaN, where a weight that is only small times an infinity is one.
+struct Seen { uint32_t any = 0, lowest = 0; };
+
+// Eight bits as bf16 numbers.
+__device__ __forceinline__ bf16x8 ones_of(uint32_t bits)
+{
+    const auto two = [&](int i) { return (bits >> i & 1u ? 0x3f80u : 0u) | (bits >> (i + 1) & 1u ? 0x3f800000u : 0u); };
+    return as_bf16x8(make_uint4(two(0), two(2), two(4), two(6)));
+}
+
+// What values that are not finite do: those of 32 keys, of steps step0 and step0 + 1.
+template <int B>
+__device__ __forceinline__ void note_not_finite(Odd* odd, const uint4* values, int step0, int col, int half, const Seen& seen)
+{
+#pragma nounroll
+    for (int i = 0; i < 8; ++i) {                     // (one at a time: this is rare, and registers are not free)
+        const int d = i & 3, down = i >> 2;
+        uint32_t any = seen.any, lowest = seen.lowest;
+        asm volatile("" : "+v"(any), "+v"(lowest));   // (what follows from them is worked out anew)
+        f32x16 n;
+#pragma unroll
+        for (int j = 0; j < 16; ++j) n[j] = 0.f;
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            const uint4 x = values[value_piece<B>(32 * d + col, half, step0 + s)];
+            n = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(not_finite_of(x, down)), ones_of(any >> (8 * s)), n, 0, 0, 0);
+            n = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(not_finite_of(x, !down)), ones_of(lowest >> (8 * s)), n, 0, 0, 0);
+        }
+        uint64_t bits = 0;
+#pragma unroll
+        for (int j = 0; j < 16; ++j) bits |= n[j] > 0.f ? 1u << j : 0u;
+        bits <<= 16 * d;
+        if (down) odd->down |= bits;
+        else odd->up |= bits;
+    }
+}
+
+__device__ __forceinline__ void add_not_finite(f32x16 (&o)[4], const Odd& odd)
+{
+#pragma unroll
+    for (int d = 0; d < 4; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            if (odd.up >> (16 * d + i) & 1) o[d][i] += INFINITY;
+            if (odd.down >> (16 * d + i) & 1) o[d][i] -= INFINITY;
+        }
+}
+
+// What the last of n_parts workgroups with partials of a block of kRowsOf rows to arrive does: out = sum_s acc_s 2^(m_s - M) / sum_s l_s 2^(m_s - M),
+// always in the same order; at(s): where partial s is.  A thread has four dims of a row; eight partials are asked for at a time.
+template <int kRowsOf, int kThreads, class At>
+__device__ __forceinline__ void merge_parts(const AttendArgs& a, const Span& span, int h, int row0, int n_rows, int n_parts, At part_at)
 {
     constexpr int kChunk = 8;
-    const int G = a.group;
     for (int i = threadIdx.x; i < kRowsOf * 32; i += kThreads) {
         const int r = i >> 5, dim = 4 * (i & 31);
         if (row0 + r >= n_rows) break;
         float M = kNegBig, l = 0.f, x[4] = {};
-        for (int s0 = 0; s0 < n_splits; s0 += kChunk) {
+        for (int s0 = 0; s0 < n_parts; s0 += kChunk) {
             uint64_t ml[kChunk], v[kChunk][2];
 #pragma unroll
             for (int s = 0; s < kChunk; ++s) {
-                const int64_t part = (part0 + min(s0 + s, n_splits - 1)) * kRowsOf + r;
+                const int64_t part = part_at(min(s0 + s, n_parts - 1)) * kRowsOf + r;
                 ml[s] = observe_u64(reinterpret_cast<const uint64_t*>(a.part_ml) + part);
                 const uint64_t* at = reinterpret_cast<const uint64_t*>(a.part_acc + part * kHeadDim + dim);
                 v[s][0] = observe_u64(at);
@@ -161,7 +240,7 @@ __device__ __forceinline__ void merge_parts(const AttendArgs& a, const Span& spa
             for (int d = 0; d < 4; ++d) x[d] *= keep;
 #pragma unroll
             for (int s = 0; s < kChunk; ++s)
-                if (s0 + s < n_splits) {
+                if (s0 + s < n_parts) {
                     const float2 one = __builtin_bit_cast(float2, ml[s]), lo = __builtin_bit_cast(float2, v[s][0]), hi = __builtin_bit_cast(float2, v[s][1]);
                     const float by = __builtin_amdgcn_exp2f(one.x - M);
                     l += one.y * by;
@@ -169,10 +248,57 @@ __device__ __forceinline__ void merge_parts(const AttendArgs& a, const Span& spa
                 }
         }
         const float inv = l == 0.f ? 0.f : 1.f / l;
-        const int rr = row0 + r, token = (int)((unsigned)rr / (unsigned)G), g = rr - token * G;
-        const int64_t at = (int64_t)(span.start + token) * (a.n_kv_heads * G) + h * G + g;
-        *reinterpret_cast<uint2*>(a.out + at * kHeadDim + dim) = make_uint2(two_bf16(x[0] * inv, x[1] * inv), two_bf16(x[2] * inv, x[3] * inv));
+        *reinterpret_cast<uint2*>(a.out + row_at(a, span, h, row0 + r) * kHeadDim + dim) = make_uint2(two_bf16(x[0] * inv, x[1] * inv), two_bf16(x[2] * inv, x[3] * inv));
     }
 }
 
+// ---- pages into LDS -------------------------------------------------------------------------------------------------------------------------
+// Loads that write LDS themselves: no registers hold what is on its way, so that tiles can be asked for far ahead.  One instruction moves 1 KB, a lane
+// 16 bytes to the lane's place behind a common base; what a lane reads is its own choice, and that is how rows are swizzled.  The compiler does not
+// know of these loads: whoever reads what they bring waits for them (loads_left) and whoever overwrites what was read waits for the reads (reads_done).
+// A quarter of 4 KB from `base` (the same in every lane) + `at` and 1 KB each further on, to LDS bytes [lds, lds + 4096).
+__device__ __forceinline__ void load_4k(uint32_t lds, const void* base, uint32_t at0, uint32_t at1, uint32_t at2, uint32_t at3)
+{
+    asm volatile("s_mov_b32 m0, %0\n\t"
+                 "s_nop 0\n\t"
+                 "global_load_lds_dwordx4 %2, %1\n\t"
+                 "global_load_lds_dwordx4 %3, %1 offset:1024\n\t"
+                 "global_load_lds_dwordx4 %4, %1 offset:2048\n\t"
+                 "global_load_lds_dwordx4 %5, %1 offset:3072"
+                 :
+                 : "s"(lds), "s"(base), "v"(at0), "v"(at1), "v"(at2), "v"(at3)
+                 : "memory");
+}
+template <int kLeft>
+__device__ __forceinline__ void loads_left()
+{
+    static_assert(kLeft == 0 || kLeft == 16);
+    if constexpr (kLeft == 0) asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
+    else asm volatile("s_waitcnt vmcnt(16)" : : : "memory");
+}
+__device__ __forceinline__ void reads_done() { asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory"); }
+
+template <class T>
+__device__ __forceinline__ uint32_t lds_at(T* p) { return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) T*)p; }
+
+// The same number in every lane, as a load of its own that does not count with the lanes' loads.
+__device__ __forceinline__ int load_same(const int32_t* p, int64_t i) { return ((const __attribute__((address_space(4))) int32_t*)p)[i]; }
+
+// What a lane reads of 16 keys (4 KB; of keys 16 .. 31 of a page the same) and of 4 KB of a page's values.
+// Keys: row r has its 16-byte piece c at c ^ (r % 16), so that the same piece of sixteen rows is on all banks.  Values of pages of 16: as they are, a lane
+// reads 16 bytes of 32 of a dim, 64 lanes a KB.  Of 32: a dim's four pieces at j ^ (dim / 4 % 4).
+struct PageLanes {
+    uint32_t key[4], value;
+    __device__ __forceinline__ PageLanes(int lane, int page_size)
+    {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) key[i] = (uint32_t)((lane >> 4) * 256 + (((lane & 15) ^ (4 * i + (lane >> 4))) & 15) * 16);
+        value = page_size == 16 ? (uint32_t)lane * 16 : (uint32_t)((lane >> 2) * 64 + ((lane & 3) ^ (lane >> 4)) * 16);
+    }
+};
+
+// Where 32 keys' operands lie in LDS, in 16-byte pieces from their page's (pages': of 16) beginning.  Row `col` of a product over keys is key
+// 16 (col / 16) + 8 (bit 2) + 4 (bit 3) + (col % 4), and with it the 16 weights of a lane are keys 8 half .. + 7 and 16 + 8 half .. + 7.
+__device__ __forceinline__ int key_of_col(int col) { return (col & 16) + ((col & 4) << 1) + ((col & 8) >> 1) + (col & 3); }
+__device__ __forceinline__ int key_piece(int key, int half, int step) { return key * 16 + ((2 * step + half) ^ (key & 15)); }
 }  // namespace chess

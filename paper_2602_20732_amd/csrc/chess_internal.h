@@ -433,6 +433,7 @@ RotateShape rotate_shape(const chess_ctx* ctx, const RotateArgs& a, bool paged);
 hipError_t launch_rotate(chess_ctx* ctx, RotateArgs a, bool paged, bool beside, hipStream_t stream);
 
 // Attention of several new tokens of a sequence (attend.hip).
+struct AttendUnit { int32_t b, block, first, end, n_parts, part, part0, counter; };   // tiles [first, end) of a block's keys
 struct AttendArgs {
     const uint16_t* q;
     const uint16_t* k_pool;
@@ -451,16 +452,20 @@ struct AttendArgs {
     int32_t* arrivals;               // [batch][H_kv][kArrivalStride], zero between launches
     float scale_log2;                // sm_scale log2(e)
     float cap_in, cap_out;           // sm_scale / cap, cap log2(e); 0: no cap
-    int window, n_rows, max_new, rows_most;
+    int window, n_rows, max_new;
     int batch, max_pages, max_sel, n_kv_heads, group;
-    int n_slots, n_splits;           // (of the shape)
+    int n_slots;                     // workgroups of a KV head (few rows), of the card (many)
+    // many rows: the plan
+    int4* blocks;                    // [blocks_most]: sequence, block of it, first tile, tiles
+    AttendUnit* units;               // [blocks_most + extra_most]
+    int32_t* n_units;
+    int32_t* counters;               // [blocks_most][H_kv]
+    int blocks_most, extra_most;
 };
-// How a call is cut: rows of a workgroup, blocks of them a sequence, splits of the keys (n_slots > 0: dealt by length, at most n_splits to one sequence).
-struct AttendShape {
-    int rows, blocks, n_splits, n_slots;
-    int64_t parts;                   // partials of `rows` rows
-};
-AttendShape attend_shape(const chess_ctx* ctx, int64_t max_new, int batch, bool list);
+// How a call is cut.  rows: of a workgroup (32, 64: few; 128: many); blocks, extra: most blocks of 128 rows, most units beyond one a block; parts: most
+// partials of `rows` rows.
+struct AttendShape { int64_t rows, n_slots, blocks, extra, parts; };
+AttendShape attend_shape(const chess_ctx* ctx, int64_t n_rows, int64_t max_new, int64_t batch);
 hipError_t launch_attend(chess_ctx* ctx, AttendArgs a, const AttendShape& s, hipStream_t stream);
 
 // Drafted tokens verified (verify.hip).

@@ -83,12 +83,12 @@ def test_documents_and_rows_that_see_nothing(new, listed):
 @pytest.mark.parametrize("B", [16, 32])
 @pytest.mark.parametrize("rule", RULES, ids=rule_name)
 def test_prompts(rule, B, heads):
-    Batch(6, [0, 100, 7, 0], [129, 70, 1, 333], *heads, B=B, **rule).check(weight_step=2.0 ** -8)
+    Batch(6, [0, 100, 7, 0], [129, 70, 1, 333], *heads, B=B, **rule).check()
 
 
 @pytest.mark.parametrize("new", [4, 130])
 def test_a_longer_context_with_peaks(new):
-    Batch(7, [3000, 5], [new, new], 4, 2, sharp=3.0).check(weight_step=2.0 ** -8)
+    Batch(7, [3000, 5], [new, new], 4, 2, sharp=3.0).check()
 
 
 def poisoned(new, value, listed=None, **rule):
@@ -112,7 +112,7 @@ def test_what_a_row_does_not_see_does_not_touch_it(rule, new, value):
         rule = dict(first=np.concatenate([np.arange(h, h + new) - 15 for h in (60, 210)]))
     b = poisoned(new, value, **rule)
     got = b.run()
-    y, off = b.want(2.0 ** -8)
+    y, off = b.want()
     got = got.double().cpu().numpy()
     fine = np.isfinite(y)
     assert fine[:-1].any() and not fine.all()
@@ -199,7 +199,7 @@ def test_replayed_with_other_lengths_between_eager_work(new):
 @pytest.mark.parametrize("new", [2, 60])
 def test_many_sequences(new):
     rng = np.random.default_rng(0)
-    Batch(13, rng.integers(0, 90, 150), rng.integers(0, new + 1, 150), 4, 1).check(weight_step=2.0 ** -8)
+    Batch(13, rng.integers(0, 90, 150), rng.integers(0, new + 1, 150), 4, 1).check()
 
 
 def test_far_pages_of_a_large_pool():
