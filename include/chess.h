@@ -438,7 +438,7 @@ int chess_quant_dense_decode(chess_ctx* ctx, const void* q, const void* k_pool, 
 /* How queries and keys are normed and turned.  A host struct; the pointers are device pointers. */
 typedef struct {
     const float* inv_freq;   /* fp32 [rotary_dim / 2]: radians a position, of each pair of dims                               */
-    const float* q_norm;     /* fp32 weights of the queries' norm, or NULL: queries are not normed                            */
+    const float* q_norm;     /* fp32 weights of the queries' norm, 16-byte aligned, or NULL: queries are not normed           */
     const float* k_norm;     /* ... of the keys'                                                                             */
     int32_t rotary_dim;      /* dims of a head that turn: the first ones; a multiple of 16 from 16 to 128                     */
     int32_t interleaved;     /* pair i is 0: dims i and i + rotary_dim / 2; 1: dims 2 i and 2 i + 1                          */

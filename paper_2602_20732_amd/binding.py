@@ -96,6 +96,15 @@ class SelectPlan:
                       self.cut_rule, per)
 
 
+def _plain(t, name, dtype):
+    """A contiguous tensor of the type, or None: (elements, device index) of it."""
+    if t is None:
+        return 0, None
+    if t.dtype is not dtype or not t.is_contiguous():
+        raise ChessError(f"{name}: a contiguous {dtype} tensor is wanted, got {t.dtype} {tuple(t.shape)} of strides {t.stride()}")
+    return t.numel(), t.get_device()
+
+
 class Rotary:
     """How queries and keys are normed and turned (``chess_rotary``); holds its tensors.
 
@@ -103,7 +112,7 @@ class Rotary:
     [128], or [heads, 128] both, or None; interleaved: pairs are neighbours."""
 
     def __init__(self, inv_freq, axis=None, interleaved: bool = False, q_norm=None, k_norm=None, eps: float = 1e-6, scale: float = 1.0):
-        pairs = inv_freq.numel()
+        pairs, dev = _plain(inv_freq, "inv_freq", torch.float32)
         axis = [0] * pairs if axis is None else [int(i) for i in axis]
         if len(axis) != pairs or pairs > 64 or min(axis, default=0) < 0 or max(axis, default=0) > 3:
             raise ChessError(f"axis: one of 0 to 3 for each of at most 64 pairs is wanted, got {axis} for {pairs}")
@@ -111,10 +120,16 @@ class Rotary:
             raise ChessError(f"q_norm, k_norm: weights a head, or for all heads, in both, got {tuple(q_norm.shape)} and {tuple(k_norm.shape)}")
         if scale == 0:
             raise ChessError("scale: not 0")
-        self.inv_freq, self.q_norm, self.k_norm = inv_freq, q_norm, k_norm
+        self.inv_freq, self.q_norm, self.k_norm, self.device = inv_freq, q_norm, k_norm, dev
         self.n_axes = max(axis, default=0) + 1
-        self.per_head = any(t is not None and t.dim() == 2 for t in (q_norm, k_norm))
-        self._c = _CRotary(inv_freq.data_ptr(), _ptr(q_norm), _ptr(k_norm), 2 * pairs, int(bool(interleaved)), int(self.per_head), self.n_axes,
+        per_head = any(t is not None and t.dim() == 2 for t in (q_norm, k_norm))
+        self.weights = []                  # (heads that each kind's weights are for, or None: for any)
+        for t, name in ((q_norm, "q_norm"), (k_norm, "k_norm")):
+            n, at = _plain(t, name, torch.float32)
+            if t is not None and (at != dev or (t.shape[-1] if t.dim() else 0) != 128 or t.dim() > 2):
+                raise ChessError(f"{name}: [128] or [heads, 128] on the device of inv_freq is wanted, got {tuple(t.shape)} on {t.device}")
+            self.weights.append(n // 128 if t is not None and per_head else None)
+        self._c = _CRotary(inv_freq.data_ptr(), _ptr(q_norm), _ptr(k_norm), 2 * pairs, int(bool(interleaved)), int(per_head), self.n_axes,
                            (ctypes.c_uint8 * 64)(*axis), eps, scale)
         self._ref = ctypes.byref(self._c)
 
@@ -126,8 +141,16 @@ class Scores:
 
     def __init__(self, cap: float = 0.0, slopes=None, window: int = 0, prefix_lens=None, first_keys=None):
         self.slopes, self.prefix_lens, self.first_keys = slopes, prefix_lens, first_keys
+        self.has = [(*_plain(t, name, dtype), name) for t, name, dtype in
+                    ((slopes, "slopes", torch.float32), (prefix_lens, "prefix_lens", torch.int32), (first_keys, "first_keys", torch.int32))]
+        self.any = any(dev is not None for _, dev, _ in self.has)
         self._c = _CScores(cap, window, _ptr(slopes), _ptr(prefix_lens), _ptr(first_keys))
         self._ref = ctypes.byref(self._c)
+
+    def _need(self, *numels, dev):
+        for (n, at, name), numel in zip(self.has, numels):
+            if at is not None and (at != dev or n < numel):
+                raise ChessError(f"{name}: at least {numel} elements on the context's device are wanted, got {n} on device {at}")
 
 
 def library_path() -> str:
@@ -491,20 +514,20 @@ class Chess:
     # ---- several tokens of a sequence in a step
     def _need_rows(self, t, name, heads, n, dev):
         """bf16 [n, heads, 128] whose token rows are contiguous; the stride from one to the next."""
-        d = self.cfg.head_dim
-        if (t.dtype is not torch.bfloat16 or t.dim() != 3 or t.size(0) != n or t.size(1) != heads or t.size(2) != d or t.stride(2) != 1 or
-                (t.stride(1) != d and heads > 1) or t.get_device() != dev):
-            raise ChessError(f"{name}: a bf16 tensor [{n}, {heads}, {d}] on the context's device with contiguous token rows is wanted, "
-                             f"got {t.dtype} {tuple(t.shape)} of strides {t.stride()} on {t.device}")
-        return t.stride(0) if n > 1 else heads * d    # (one token's stride leads nowhere)
+        stride = t.stride()
+        if t.dtype is not torch.bfloat16 or t.shape != (n, heads, 128) or stride[2] != 1 or (stride[1] != 128 and heads > 1) or t.get_device() != dev:
+            raise ChessError(f"{name}: a bf16 tensor [{n}, {heads}, 128] on the context's device with contiguous token rows is wanted, "
+                             f"got {t.dtype} {tuple(t.shape)} of strides {stride} on {t.device}")
+        return stride[0] if n > 1 else heads * 128    # (one token's stride leads nowhere)
 
     def _need_rotary(self, rotary, positions, n, dev):
         c = self.cfg
-        _need(rotary.inv_freq, "inv_freq", _FLOAT, 1, dev)
-        for t, name, heads in ((rotary.q_norm, "q_norm", c.n_q_heads), (rotary.k_norm, "k_norm", c.n_kv_heads)):
-            if t is not None:
-                _need(t, name, _FLOAT, c.head_dim * (heads if rotary.per_head else 1), dev)
+        if rotary.device != dev or rotary.weights[0] not in (None, c.n_q_heads) or rotary.weights[1] not in (None, c.n_kv_heads):
+            raise ChessError(f"rotary: of the context's device ({dev}) and, with weights a head, {c.n_q_heads} and {c.n_kv_heads} heads is wanted, "
+                             f"got device {rotary.device}, heads {rotary.weights}")
         _need(positions, "positions", _INT, rotary.n_axes * n, dev)
+        if positions.numel() != rotary.n_axes * n:
+            raise ChessError(f"positions: [{rotary.n_axes}, {n}] is wanted, got {tuple(positions.shape)}")
 
     def rotate(self, rotary: Rotary, q, k, positions, q_out=None, k_out=None, counts=None):
         """q: bf16 [rows, n_q_heads, 128] or None, k: bf16 [rows, H_kv, 128] or None (slices of a wider projection will do); positions: int32
@@ -525,8 +548,6 @@ class Chess:
             _need(counts, "counts", _INT, 1, dev)
         if n == 0:
             return
-        if positions.numel() != rotary.n_axes * n:
-            raise ChessError(f"positions: [{rotary.n_axes}, {n}] is wanted, got {tuple(positions.shape)}")
         self._check(self.lib.chess_rotate(self._h, rotary._ref, _ptr(q), q_stride, _ptr(k), k_stride, positions.data_ptr(), n, _ptr(counts),
                                           None if q is None else q_out.data_ptr(), None if k is None else k_out.data_ptr(),
                                           torch._C._cuda_getCurrentRawStream(dev)))
@@ -549,8 +570,6 @@ class Chess:
             raise ChessError(f"k_pool, v_pool: {k_pool.numel()} and {v_pool.numel()} values are not of the same pages")
         if n == 0:
             return
-        if positions.numel() != rotary.n_axes * n:
-            raise ChessError(f"positions: [{rotary.n_axes}, {n}] is wanted, got {tuple(positions.shape)}")
         self._check(self.lib.chess_rotate_store(self._h, rotary._ref, _ptr(q), q_stride, k_new.data_ptr(), k_stride, v_new.data_ptr(), v_stride,
                                                 positions.data_ptr(), n, writes.data_ptr(), counts.data_ptr(), writes.numel() // 4,
                                                 None if q is None else q_out.data_ptr(), k_pool.data_ptr(), v_pool.data_ptr(),
@@ -566,10 +585,11 @@ class Chess:
 
     def _need_attend(self, q, token_start, k_pool, v_pool, block_table, seq_lens, out, workspace, scratch, scores, batch, dev):
         c = self.cfg
-        n = q.size(0)
+        shape = q.shape
+        if len(shape) != 3 or shape[1] != c.n_q_heads or shape[2] != c.head_dim:
+            raise ChessError(f"q: [rows, {c.n_q_heads}, {c.head_dim}] is wanted, got {tuple(shape)}")
+        n = shape[0]
         values = n * c.n_q_heads * c.head_dim
-        if q.dim() != 3:
-            raise ChessError(f"q: [rows, {c.n_q_heads}, {c.head_dim}] is wanted, got {tuple(q.shape)}")
         _need(q, "q", _BF16, values, dev)
         _need(out, "out", _BF16, values, dev)
         _need(token_start, "token_start", _INT, batch + 1, dev)
@@ -580,15 +600,8 @@ class Chess:
         _need(seq_lens, "seq_lens", _INT, batch, dev)
         _need(workspace, "workspace", _BYTE, self.workspace_bytes, dev)
         _need(scratch, "scratch", _BYTE, 1, dev)
-        if scores is not None:
-            if scores.slopes is not None:
-                _need(scores.slopes, "slopes", _FLOAT, c.n_q_heads, dev)
-            if scores.prefix_lens is not None:
-                _need(scores.prefix_lens, "prefix_lens", _INT, batch, dev)
-            if scores.first_keys is not None:
-                _need(scores.first_keys, "first_keys", _INT, n, dev)
-        if q.size(1) != c.n_q_heads or q.size(2) != c.head_dim:
-            raise ChessError(f"q: [rows, {c.n_q_heads}, {c.head_dim}] is wanted, got {tuple(q.shape)}")
+        if scores is not None and scores.any:
+            scores._need(c.n_q_heads, batch, n, dev=dev)
         return n
 
     def dense_attend(self, q, token_start, max_new: int, k_pool, v_pool, block_table, seq_lens, out, workspace, scratch, scores: Scores = None):
@@ -621,18 +634,21 @@ class Chess:
         batch, dev = seq_lens.numel(), self.device
         if uniforms.dim() != 2 or uniforms.size(0) != batch or uniforms.size(1) < 1:
             raise ChessError(f"uniforms: [{batch}, max_drafts + 1] is wanted, got {tuple(uniforms.shape)}")
-        if target.dim() != 2 or target.dtype is not torch.float32 or target.stride(1) != 1 and target.size(1) > 1 or target.get_device() != dev or target.size(0) < 1:
+        shape, stride = target.shape, target.stride()
+        if len(shape) != 2 or target.dtype is not torch.float32 or stride[1] != 1 and shape[1] > 1 or target.get_device() != dev or shape[0] < 1 or shape[1] < 1:
             raise ChessError(f"target: an fp32 tensor [rows, vocab] with contiguous rows on the context's device is wanted, got {target.dtype} "
-                             f"{tuple(target.shape)} of strides {target.stride()} on {target.device}")
-        n, vocab = target.shape
+                             f"{tuple(shape)} of strides {stride} on {target.device}")
+        n, vocab = shape
+        target_stride = stride[0] if n > 1 else vocab
         most = uniforms.size(1) - 1
         draft_seq = draft_row = 0
         if draft is not None:
-            if (draft.dim() != 3 or draft.dtype is not torch.float32 or draft.size(0) != batch or draft.size(1) < most or draft.size(2) != vocab or
-                    draft.stride(2) != 1 and vocab > 1 or draft.get_device() != dev):
+            shape, stride = draft.shape, draft.stride()
+            if (len(shape) != 3 or draft.dtype is not torch.float32 or shape[0] != batch or shape[1] < most or shape[2] != vocab or
+                    stride[2] != 1 and vocab > 1 or draft.get_device() != dev):
                 raise ChessError(f"draft: an fp32 tensor [{batch}, {most}, {vocab}] with contiguous rows on the context's device is wanted, got {draft.dtype} "
-                                 f"{tuple(draft.shape)} of strides {draft.stride()} on {draft.device}")
-            draft_seq, draft_row = (draft.stride(0) if batch > 1 else max(vocab, draft.stride(0))), (draft.stride(1) if draft.size(1) > 1 else vocab)
+                                 f"{tuple(shape)} of strides {stride} on {draft.device}")
+            draft_seq, draft_row = stride[0] if batch > 1 else vocab, stride[1] if shape[1] > 1 else vocab
         _need(tokens, "tokens", _INT, n, dev)
         _need(token_start, "token_start", _INT, batch + 1, dev)
         _need(uniforms, "uniforms", _FLOAT, batch * (most + 1), dev)
@@ -641,7 +657,7 @@ class Chess:
         _need(out_tokens, "out_tokens", _INT, batch * (most + 1), dev)
         _need(lens_after, "lens_after", _INT, batch, dev)
         _need(workspace, "workspace", _BYTE, self.workspace_bytes, dev)
-        self._check(self.lib.chess_verify(self._h, target.data_ptr(), target.stride(0) if n > 1 else vocab, _ptr(draft), draft_seq, draft_row, vocab,
+        self._check(self.lib.chess_verify(self._h, target.data_ptr(), target_stride, _ptr(draft), draft_seq, draft_row, vocab,
                                           tokens.data_ptr(), n, token_start.data_ptr(), uniforms.data_ptr(), most, seq_lens.data_ptr(), batch,
                                           n_accepted.data_ptr(), out_tokens.data_ptr(), lens_after.data_ptr(), workspace.data_ptr(),
                                           torch._C._cuda_getCurrentRawStream(dev)))

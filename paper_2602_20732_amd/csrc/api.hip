@@ -855,7 +855,7 @@ static int rotate_common(chess_ctx* ctx, const chess_rotary* rot, chess::RotateA
     if (a.k && (a.k_stride < kv_row || (a.k_stride & 7))) return CHESS_EINVAL;
     if (rot->rotary_dim < 16 || rot->rotary_dim > kHeadDim || rot->rotary_dim % 16 != 0 || rot->n_axes < 1 || rot->n_axes > 4) return CHESS_EINVAL;
     if (!(rot->eps >= 0.f) || !std::isfinite(rot->eps) || !std::isfinite(rot->scale)) return CHESS_EINVAL;
-    if (misaligned({a.q, a.k, a.v, a.q_out, a.k_out, a.v_pool, a.writes}, 15) || misaligned({rot->inv_freq, rot->q_norm, rot->k_norm, a.positions, a.counts}, 3) ||
+    if (misaligned({a.q, a.k, a.v, a.q_out, a.k_out, a.v_pool, a.writes, rot->q_norm, rot->k_norm}, 15) || misaligned({rot->inv_freq, a.positions, a.counts}, 3) ||
         !on_device(ctx))
         return CHESS_EINVAL;
     a.pairs = rot->rotary_dim / 2;
@@ -870,6 +870,7 @@ static int rotate_common(chess_ctx* ctx, const chess_rotary* rot, chess::RotateA
     a.eps = rot->eps;
     a.scale = rot->scale == 0.f ? 1.f : rot->scale;
     a.position_stride = a.n_rows;
+    a.n_axes = rot->n_axes;
     a.q_heads = ctx->geom.n_q_heads;
     a.kv_heads = ctx->geom.n_kv_heads;
     const chess::RotateShape s = chess::rotate_shape(ctx, a, paged);

@@ -4,8 +4,9 @@
 //
 // Causal order, a window, a prefix that all see and the start of the row's document are all of them an interval: lo and hi are worked out once
 // a row, and a key is compared with two numbers.  A tile that every row sees whole is not compared at all.
-#include "attend_device.h"
+#include <atomic>
 
+#include "attend_device.h"
 #include "deal.h"
 #include "split_rule.h"
 
@@ -386,6 +387,7 @@ __device__ __forceinline__ Keys keys_of_block(const AttendArgs& a, const Span& s
     Keys k{a.window > 0 ? max(p0 - a.window + 1, 0) : 0, min(a.prefix_lens != nullptr ? max(p1, a.prefix_lens[b] - 1) : p1, s.len - 1)};
     if (a.first_keys != nullptr) {
         int first = INT32_MAX;
+#pragma unroll 8
         for (int i = i0; i <= i1; ++i) first = min(first, a.first_keys[s.start + i]);
         k.first = max(k.first, first);
     }
@@ -395,44 +397,44 @@ __device__ __forceinline__ Keys keys_of_block(const AttendArgs& a, const Span& s
 
 // One workgroup.  Blocks in sequence order: their tiles; how long a unit may be (by what the card would take for it, of sixteen lengths); the units, longest
 // first as far as it is known (whole lengths, then the rest), and which partials they leave.
+// Bound: the chain starts -> blocks -> sums -> units, and that its code runs once.
 template <int B>
 __global__ __launch_bounds__(kPlanThreads) void plan_kernel(AttendArgs a)
 {
     constexpr int kWaves = kPlanThreads / 64, kTry = 16;
     extern __shared__ int upto[];                     // [batch]: blocks of the sequences up to this one
-    __shared__ int of_wave[kWaves], counts[kTry], n_tiles_most;
-    __shared__ int64_t n_tiles_all;
+    __shared__ int of_wave[3][kWaves], most_of_wave[kWaves], units_of_wave[kTry][kWaves];
+    __shared__ float tiles_of_wave[kWaves];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    // a running sum over all threads' numbers, chunk by chunk
-    const auto sum_before = [&](int v, int* all) {
-        const int own = lanes_upto(v);
+    // running sums over all threads' numbers, and the whole sums
+    const auto sums_before = [&](int (&v)[3], int (&all)[3]) {
+        int own[3];
+#pragma unroll
+        for (int i = 0; i < 3; ++i) own[i] = lanes_upto(v[i]);
         __syncthreads();
-        if (lane == 63) of_wave[wave] = own;
+        if (lane == 63)
+#pragma unroll
+            for (int i = 0; i < 3; ++i) of_wave[i][wave] = own[i];
         __syncthreads();
-        int base = 0, sum = 0;
-        for (int w = 0; w < kWaves; ++w) {
-            if (w == wave) base = sum;
-            sum += of_wave[w];
+#pragma unroll
+        for (int i = 0; i < 3; ++i) {
+            const int upto_wave = lanes_upto(lane < kWaves ? of_wave[i][lane] : 0);
+            all[i] = lane_of(upto_wave, kWaves - 1);
+            v[i] = own[i] - v[i] + (wave > 0 ? lane_of(upto_wave, max(wave - 1, 0)) : 0);
         }
-        *all = sum;
-        return base + own - v;
     };
     int n_blocks = 0;
     for (int b0 = 0; b0 < a.batch; b0 += kPlanThreads) {
-        const int b = b0 + (int)threadIdx.x;
-        const int v = b < a.batch ? blocks_of(span_by_lane(a, b, B).n_new, a.group) : 0;
-        int all;
-        const int before = sum_before(v, &all);
-        if (b < a.batch) upto[b] = n_blocks + before + v;
-        n_blocks += all;
-    }
-    if (threadIdx.x < kTry) counts[threadIdx.x] = 0;
-    if (threadIdx.x == 0) {
-        n_tiles_most = 1;
-        n_tiles_all = 0;
+        const int b = b0 + (int)threadIdx.x, n = b < a.batch ? blocks_of(span_by_lane(a, b, B).n_new, a.group) : 0;
+        int v[3] = {n, 0, 0}, all[3];
+        sums_before(v, all);
+        if (b < a.batch) upto[b] = n_blocks + v[0] + n;
+        n_blocks += all[0];
     }
     __syncthreads();
     n_blocks = min(n_blocks, a.blocks_most);
+    int most = 1;
+    float tiles = 0.f;                                // (estimates only)
     for (int i = threadIdx.x; i < n_blocks; i += kPlanThreads) {
         int lo = 0, hi = a.batch - 1;                 // the first sequence whose blocks go beyond i
         while (lo < hi) {
@@ -446,65 +448,77 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(AttendArgs a)
         const bool any = k.last >= k.first;
         const int first = any ? k.first / 64 : 0, n = a.page_ids != nullptr ? 1 : any ? k.last / 64 - first + 1 : 1;
         a.blocks[i] = make_int4(lo, block, first, n);
-        atomicMax(&n_tiles_most, n);
-        atomicAdd(reinterpret_cast<unsigned long long*>(&n_tiles_all), (unsigned long long)n);
+        most = max(most, n);
+        tiles += (float)n;
         for (int h = 0; h < a.n_kv_heads; ++h) a.counters[(int64_t)i * a.n_kv_heads + h] = 0;
     }
+    most = lanes_max(most);
+    tiles = lane_of(lanes_upto(tiles), 63);
+    if (lane == 0) {
+        most_of_wave[wave] = most;
+        tiles_of_wave[wave] = tiles;
+    }
     __syncthreads();
+    most = 1;
+    tiles = 0.f;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+        most = max(most, most_of_wave[w]);
+        tiles += tiles_of_wave[w];
+    }
     // units of each length tried
-    const int most = n_tiles_most;
     const auto length = [&](int y) { return max((most + y) / (y + 1), 1); };
+    int units[kTry] = {};
     for (int i = threadIdx.x; i < n_blocks; i += kPlanThreads) {
         const int n = a.blocks[i].w;
-        for (int y = 0; y < kTry; ++y) atomicAdd(&counts[y], (n + length(y) - 1) / length(y));
+#pragma unroll
+        for (int y = 0; y < kTry; ++y) units[y] += (n + length(y) - 1) / length(y);
     }
-    __syncthreads();
-    // what they would take, in tiles: a unit costs some of its own, and a cut one the partials'
-    const float slots = (float)a.n_slots, heads = (float)a.n_kv_heads, all_tiles = (float)n_tiles_all;
-    int best = 0;
-    float least = INFINITY;
+#pragma unroll
     for (int y = 0; y < kTry; ++y) {
-        const int len = length(y), units = counts[y], extra = units - n_blocks;
-        if (y > 0 && (len < 8 || extra > a.extra_most)) break;
-        const float own = 5.f, size = (float)len + own, work = heads * (all_tiles + own * (float)units + (extra > 0 ? 6.f * (float)units : 0.f));
-        const float rounds = work / (slots * size);
-        const float cost = rounds >= 4.f ? work / slots + 0.5f * size : ceilf(rounds) * size + (extra > 0 ? 6.f : 0.f);
-        if (cost < 0.97f * least) {
-            least = cost;
-            best = y;
-        }
+        const int n = lanes_upto(units[y]);
+        if (lane == 63) units_of_wave[y][wave] = n;
     }
-    const int len = length(best);
     __syncthreads();
+    // what each would take, in tiles: a unit costs some of its own, and a cut one the partials'.  Lane y: length y
+    int n_units = 0;
+    if (lane < kTry)
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) n_units += units_of_wave[lane][w];
+    const int len_y = length(lane), extra = n_units - n_blocks;
+    const float own = 5.f, cut = extra > 0 ? 6.f : 0.f, size = (float)len_y + own, slots = (float)a.n_slots;
+    const float work = (float)a.n_kv_heads * (tiles + (own + cut) * (float)n_units), rounds = work / (slots * size);
+    float cost = rounds >= 4.f ? work / slots + 0.5f * size : ceilf(rounds) * size + cut;
+    if (lane > 0 && (lane >= kTry || len_y < 8 || extra > a.extra_most)) cost = INFINITY;
+    float least = cost;
+#pragma unroll
+    for (int by = 32; by > 0; by /= 2) least = fminf(least, __shfl_xor(least, by));
+    const int len = lane_of(len_y, __builtin_ctzll(__ballot(cost <= 1.03f * least)));       // (the longest of those that are as good)
     // whole lengths first, then what is left of the blocks
-    int n_whole_all = 0, units_before = 0, parts_before = 0;
+    int whole_before = 0, rest_before = 0, parts_before = 0;
     for (int i0 = 0; i0 < n_blocks; i0 += kPlanThreads) {
         const int i = i0 + (int)threadIdx.x;
-        int all;
-        const int v = i < n_blocks ? a.blocks[i].w / len : 0;
-        sum_before(v, &all);
-        n_whole_all += all;
+        int v[3] = {i < n_blocks ? a.blocks[i].w / len : 0, 0, 0}, all[3];
+        sums_before(v, all);
+        rest_before += all[0];
     }
-    int rest_before = n_whole_all;
     for (int i0 = 0; i0 < n_blocks; i0 += kPlanThreads) {
         const int i = i0 + (int)threadIdx.x;
         const int4 blk = i < n_blocks ? a.blocks[i] : make_int4(0, 0, 0, 0);
         const int whole = blk.w / len, rest = blk.w - whole * len, n = whole + (rest > 0 ? 1 : 0);
-        int all;
-        int at = units_before + sum_before(whole, &all);
-        units_before += all;
-        const int at_rest = rest_before + sum_before(rest > 0 ? 1 : 0, &all);
-        rest_before += all;
-        const int part0 = parts_before + sum_before(n > 1 ? n : 0, &all);
-        parts_before += all;
+        int v[3] = {whole, rest > 0 ? 1 : 0, n > 1 ? n : 0}, all[3];
+        sums_before(v, all);
+        const int at = whole_before + v[0], at_rest = rest_before + v[1], part0 = parts_before + v[2];
+        whole_before += all[0];
+        rest_before += all[1];
+        parts_before += all[2];
         for (int s = 0; s < n; ++s) {
-            const int to = s < whole ? at + s : at_rest;
             AttendUnit u;
             u.b = blk.x; u.block = blk.y;
             u.first = blk.z + s * len;
-            u.end = a.page_ids != nullptr ? INT32_MAX : blk.z + min((s + 1) * len, blk.w);
+            u.end = blk.z + min((s + 1) * len, blk.w);
             u.n_parts = n; u.part = part0 + s; u.part0 = part0; u.counter = i;
-            a.units[to] = u;
+            a.units[s < whole ? at + s : at_rest] = u;
         }
     }
     if (threadIdx.x == 0) *a.n_units = rest_before;
@@ -793,20 +807,34 @@ __global__ __launch_bounds__(256, 2) void attend_many_kernel(AttendArgs a)
 }
 
 // ---- launch -----------------------------------------------------------------------------------------------------------------------------------
-template <class Kernel>
-static hipError_t launch_lds(Kernel kernel, dim3 grid, int threads, size_t lds, hipStream_t stream, const AttendArgs& a)
+// A kernel with more LDS than one may have unasked: asked for once a device (it costs the host more than a microsecond).
+template <auto kKernel>
+static hipError_t launch_lds(chess_ctx* ctx, dim3 grid, size_t lds, hipStream_t stream, const AttendArgs& a)
 {
-    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
-    if (e != hipSuccess) return e;
-    return launch(kernel, grid, dim3(threads), lds, stream, a);
+    static std::atomic<uint64_t> asked{0};
+    const uint64_t bit = ctx->device < 64 ? (uint64_t)1 << ctx->device : 0;
+    if ((asked.load(std::memory_order_relaxed) & bit) == 0) {
+        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kKernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+        if (e != hipSuccess) return e;
+        asked.fetch_or(bit, std::memory_order_relaxed);
+    }
+    return launch(kKernel, grid, dim3(256), lds, stream, a);
 }
 
 template <int B, int kRows, bool kCap>
-static hipError_t launch_few(const AttendArgs& a, bool list, hipStream_t stream)
+static hipError_t launch_few(chess_ctx* ctx, const AttendArgs& a, bool list, hipStream_t stream)
 {
     const dim3 grid((unsigned)(a.n_slots * a.n_kv_heads));
-    return list ? launch_lds(attend_few_kernel<B, kRows, true, kCap>, grid, 256, few_lds(32 * kRows), stream, a)
-                : launch_lds(attend_few_kernel<B, kRows, false, kCap>, grid, 256, few_lds(32 * kRows), stream, a);
+    return list ? launch_lds<attend_few_kernel<B, kRows, true, kCap>>(ctx, grid, few_lds(32 * kRows), stream, a)
+                : launch_lds<attend_few_kernel<B, kRows, false, kCap>>(ctx, grid, few_lds(32 * kRows), stream, a);
+}
+
+template <int B, bool kList>
+static hipError_t launch_many(chess_ctx* ctx, const AttendArgs& a, const AttendShape& s, bool general, hipStream_t stream)
+{
+    const dim3 grid((unsigned)((s.blocks + s.extra) * a.n_kv_heads));
+    constexpr size_t lds = 2 * kManyStage * 16;
+    return general ? launch_lds<attend_many_kernel<B, kList, true>>(ctx, grid, lds, stream, a) : launch_lds<attend_many_kernel<B, kList, false>>(ctx, grid, lds, stream, a);
 }
 
 // Few rows: a line a KV head.  Many: units; `most` blocks and cut units that there can be, whatever the sequences are.
@@ -836,25 +864,19 @@ hipError_t launch_attend(chess_ctx* ctx, AttendArgs a, const AttendShape& s, hip
     const bool list = a.page_ids != nullptr, cap = a.cap_in != 0.f, b16 = ctx->geom.page_size == 16;
     if (s.rows < kBlockRows) {
         if (b16) {
-            if (s.rows == 32) return cap ? launch_few<16, 1, true>(a, list, stream) : launch_few<16, 1, false>(a, list, stream);
-            return cap ? launch_few<16, 2, true>(a, list, stream) : launch_few<16, 2, false>(a, list, stream);
+            if (s.rows == 32) return cap ? launch_few<16, 1, true>(ctx, a, list, stream) : launch_few<16, 1, false>(ctx, a, list, stream);
+            return cap ? launch_few<16, 2, true>(ctx, a, list, stream) : launch_few<16, 2, false>(ctx, a, list, stream);
         }
-        if (s.rows == 32) return cap ? launch_few<32, 1, true>(a, list, stream) : launch_few<32, 1, false>(a, list, stream);
-        return cap ? launch_few<32, 2, true>(a, list, stream) : launch_few<32, 2, false>(a, list, stream);
+        if (s.rows == 32) return cap ? launch_few<32, 1, true>(ctx, a, list, stream) : launch_few<32, 1, false>(ctx, a, list, stream);
+        return cap ? launch_few<32, 2, true>(ctx, a, list, stream) : launch_few<32, 2, false>(ctx, a, list, stream);
     }
     a.blocks_most = (int)s.blocks;
     a.extra_most = (int)s.extra;
     const hipError_t e = launch(b16 ? plan_kernel<16> : plan_kernel<32>, dim3(1), dim3(kPlanThreads), (size_t)a.batch * sizeof(int), stream, a);
     if (e != hipSuccess) return e;
-    const dim3 grid((unsigned)((s.blocks + s.extra) * a.n_kv_heads));
-    constexpr size_t lds = 2 * kManyStage * 16;
     const bool general = cap || a.slopes != nullptr;
-    if (b16) {
-        if (list) return general ? launch_lds(attend_many_kernel<16, true, true>, grid, 256, lds, stream, a) : launch_lds(attend_many_kernel<16, true, false>, grid, 256, lds, stream, a);
-        return general ? launch_lds(attend_many_kernel<16, false, true>, grid, 256, lds, stream, a) : launch_lds(attend_many_kernel<16, false, false>, grid, 256, lds, stream, a);
-    }
-    if (list) return general ? launch_lds(attend_many_kernel<32, true, true>, grid, 256, lds, stream, a) : launch_lds(attend_many_kernel<32, true, false>, grid, 256, lds, stream, a);
-    return general ? launch_lds(attend_many_kernel<32, false, true>, grid, 256, lds, stream, a) : launch_lds(attend_many_kernel<32, false, false>, grid, 256, lds, stream, a);
+    if (b16) return list ? launch_many<16, true>(ctx, a, s, general, stream) : launch_many<16, false>(ctx, a, s, general, stream);
+    return list ? launch_many<32, true>(ctx, a, s, general, stream) : launch_many<32, false>(ctx, a, s, general, stream);
 }
 
 }  // namespace chess

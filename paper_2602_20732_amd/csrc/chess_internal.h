@@ -420,14 +420,15 @@ struct RotateArgs {
     uint16_t* q_out;
     uint16_t* k_out;                 // rows, or the K pool
     uint16_t* v_pool;
-    int q_heads, kv_heads, pairs, norm_stride, max_writes, n_rows, n_pages;
+    int q_heads, kv_heads, pairs, n_axes, norm_stride, max_writes, n_rows, n_pages;
     float eps, scale;
-    int q_parts, k_parts, parts;     // runs of heads, workgroups a unit (rotate_shape)
+    int q_runs, k_runs, head_parts, parts, units;   // (of rotate_shape)
 };
-// Heads / 4 that a wave turns at a time, and how many units (an entry of the write list, or 16 rows) of how many workgroups there are.
+// Units (an entry of the write list, or 16 rows) of `parts` workgroups, of which head_parts have the runs of heads (of 16 where there are many units, of 4 otherwise).
 struct RotateShape {
-    int quads, q_parts, k_parts, parts;
+    int q_runs, k_runs, head_parts, parts;
     int64_t units;
+    bool many;
 };
 RotateShape rotate_shape(const chess_ctx* ctx, const RotateArgs& a, bool paged);
 hipError_t launch_rotate(chess_ctx* ctx, RotateArgs a, bool paged, bool beside, hipStream_t stream);

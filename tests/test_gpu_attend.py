@@ -231,10 +231,11 @@ def test_refusals():
                       ("token_start", args["token_start"][:1]), ("block_table", args["block_table"][:, :1]), ("workspace", args["workspace"][:64]),
                       ("scratch", args["scratch"][1:]), ("scratch", args["scratch"][:0]), ("max_new", 0), ("scores", s(cap=-1.0)), ("scores", s(cap=float("nan"))),
                       ("scores", s(cap=float("inf"))), ("scores", s(cap=1e-42)), ("scores", s(window=-1)),
-                      ("scores", s(slopes=torch.ones(7, device="cuda"))), ("scores", s(slopes=torch.ones(8))), ("scores", s(first_keys=ints([0] * 3))),
-                      ("scores", s(prefix_lens=torch.zeros(1, device="cuda")))):
+                      ("scores", s(slopes=torch.ones(7, device="cuda"))), ("scores", s(slopes=torch.ones(8))), ("scores", s(first_keys=ints([0] * 3)))):
         with pytest.raises(pk.ChessError):
             dense(**{**args, name: bad})
+    with pytest.raises(pk.ChessError):
+        s(prefix_lens=torch.zeros(1, device="cuda"))
     with pytest.raises(pk.ChessError):
         b.lib.sparse_attend(**args, page_ids=ints([0]), n_selected=ints([1]))
     n = ctypes.c_size_t()
