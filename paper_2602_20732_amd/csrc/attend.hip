@@ -153,39 +153,48 @@ __global__ __launch_bounds__(256, 1) void attend_few_kernel(AttendArgs a)
                 for (int i = 0; i < 16; ++i) o[y][d][i] = 0.f;
         }
 
-        // logical pages of a tile (one that is none of the sequence's: -1), and their physical ones
-        const auto pages_of = [&](int tile, int (&page)[PPT], int (&phys)[PPT]) {
-#pragma unroll
-            for (int s = 0; s < PPT; ++s) {
-                const int i = tile * PPT + s;
-                int p = i;
-                if constexpr (kList) p = load_same(ids, min(i, a.max_sel - 1));
-                page[s] = i < n_list && p >= 0 && p < P ? p : -1;
-                phys[s] = load_same(table, max(page[s], 0));
-            }
+        // Logical pages (one that is none of the sequence's: -1) and physical ones of the wave's next tiles, 64 at a time, one a lane: a window of the table (or
+        // list) is asked for a window ahead, and what a tile needs of it is read from a lane.  (A scalar load a tile would be waited for with the LDS reads,
+        // which count with it.)
+        constexpr int kWindow = 64 / PPT;             // tiles of the wave
+        const int t0 = t;
+        struct Window { int page, phys; };
+        const auto window_at = [&](int number) {
+            const int i = (t0 + 4 * (number * kWindow + lane / PPT)) * PPT + lane % PPT;
+            int p = i;
+            if constexpr (kList) p = ids[min(i, a.max_sel - 1)];
+            const int page = i < n_list && p >= 0 && p < P ? p : -1;
+            return Window{page, table[max(page, 0)]};
         };
         const auto fetch = [&](const int (&phys)[PPT], int stage) {
             const uint32_t to = ring_lds + (uint32_t)stage * 16384;
 #pragma unroll
             for (int s = 0; s < 2; ++s) {
-                const int64_t at = ((int64_t)phys[s * PPT / 2] * H + h) * (B * kHeadDim) + (PPT == 1 ? s * 2048 : 0);
+                const int64_t at = ((int64_t)__builtin_amdgcn_readfirstlane(phys[s * PPT / 2]) * H + h) * (B * kHeadDim) + (PPT == 1 ? s * 2048 : 0);
                 load_4k(to + s * 4096, a.k_pool + at, from.key[0], from.key[1], from.key[2], from.key[3]);
                 load_4k(to + 8192 + s * 4096, a.v_pool + at, from.value, from.value, from.value, from.value);
             }
         };
 
-        int lp[PPT], lp_next[PPT], lp_last[PPT], phys[PPT];
-        if (t < t_end) {
-            pages_of(t, lp, phys);
-            fetch(phys, 0);
-            if (t + 4 < t_end) {
-                pages_of(t + 4, lp_next, phys);
-                fetch(phys, 1);
+        Window window{-1, 0}, window_next{-1, 0};     // the one that tile n + 2 of the wave is in, and the next
+        const auto pages_of = [&](int n, int (&page)[PPT], int (&phys)[PPT]) {
+#pragma unroll
+            for (int s = 0; s < PPT; ++s) {
+                page[s] = __builtin_amdgcn_readlane(window.page, n % kWindow * PPT + s);
+                phys[s] = __builtin_amdgcn_readlane(window.phys, n % kWindow * PPT + s);
             }
-            pages_of(min(t + 8, t_end - 1), lp_last, phys);
+        };
+        int lp[PPT], lp_next[PPT], phys[PPT];
+        if (t < t_end) {
+            window = window_at(0);
+            window_next = window_at(1);
+            pages_of(0, lp, phys);
+            fetch(phys, 0);
+            pages_of(1, lp_next, phys);
+            if (t + 4 < t_end) fetch(phys, 1);
         }
         __syncthreads();                              // the queries
-        for (int stage = 0; t < t_end; t += 4, stage ^= 1) {
+        for (int n = 0, stage = 0; t < t_end; t += 4, ++n, stage ^= 1) {
             const uint4* keys = ring_own + stage * 1024;
             const uint4* values = keys + 512;
             if (t + 4 < t_end) loads_left<16>();
@@ -282,16 +291,17 @@ __global__ __launch_bounds__(256, 1) void attend_few_kernel(AttendArgs a)
                     for (int s = 0; s < 2; ++s) v[d][s] = finite_of(v[d][s]);
             }
             // the tile's LDS is free: the one after the next into it
+            if ((n + 2) % kWindow == 0) {
+                window = window_next;
+                window_next = window_at((n + 2) / kWindow + 1);
+            }
+#pragma unroll
+            for (int s = 0; s < PPT; ++s) lp[s] = lp_next[s];
+            pages_of(n + 2, lp_next, phys);
             if (t + 8 < t_end) {
                 reads_done();
                 fetch(phys, stage);
             }
-#pragma unroll
-            for (int s = 0; s < PPT; ++s) {
-                lp[s] = lp_next[s];
-                lp_next[s] = lp_last[s];
-            }
-            pages_of(min(t + 12, t_end - 1), lp_last, phys);
 #pragma unroll
             for (int d = 0; d < 4; ++d)
 #pragma unroll
@@ -365,14 +375,15 @@ __global__ __launch_bounds__(256, 1) void attend_few_kernel(AttendArgs a)
 
 // ---- many rows (prompts): the rows are split ----------------------------------------------------------------------------------------------
 // A unit is 128 rows (token, head of the group) of a sequence and KV head, 32 a wave, and a run of tiles of 64 keys (32 KB) that its workgroup brings to
-// LDS for all of them, the next while one is worked on.  The same products as above, twice as many keys at a time, but the weights are bf16: an output is
-// rounded to bf16 all the same, and its weights' roundings come to less than that (the sum of the weights is of the unrounded ones).
+// LDS for all of them, the next while one is worked on; the next tile's products of queries and keys are formed while this one's exponentials are.  The same
+// products as above, twice as many keys at a time, but the weights are bf16: an output is rounded to bf16 all the same, and its weights' roundings come
+// to less than that (the sum of the weights is of the unrounded ones).
 // A plan says which units there are (plan_kernel): tiles that no row of a block sees are left out, and long blocks are cut where there are too
 // few to fill the card; partials are merged by the last unit of a block to arrive.
 // Bound: the matrix units and the exponentials beside them, 32 products of 32 cycles and 32 exponentials a lane for a tile and wave.
 
 constexpr int kBlockRows = 128;
-constexpr int kManyStage = 2048;                      // 16-byte pieces of a tile: 1024 of keys, 1024 of values
+constexpr size_t kManyLds = 4 * 16384;                // two tiles' keys, two tiles' values
 constexpr int kPlanThreads = 1024;
 
 __device__ __forceinline__ int blocks_of(int n_new, int G) { return (int)(((int64_t)n_new * G + kBlockRows - 1) / kBlockRows); }
@@ -486,10 +497,11 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(AttendArgs a)
 #pragma unroll
         for (int w = 0; w < kWaves; ++w) n_units += units_of_wave[lane][w];
     const int len_y = length(lane), extra = n_units - n_blocks;
-    const float own = 5.f, cut = extra > 0 ? 6.f : 0.f, size = (float)len_y + own, slots = (float)a.n_slots;
-    const float work = (float)a.n_kv_heads * (tiles + (own + cut) * (float)n_units), rounds = work / (slots * size);
-    float cost = rounds >= 4.f ? work / slots + 0.5f * size : ceilf(rounds) * size + cut;
-    if (lane > 0 && (lane >= kTry || len_y < 8 || extra > a.extra_most)) cost = INFINITY;
+    const float cut = extra > 0 ? 6.f : 0.f, size = (float)len_y + 5.f + cut, slots = (float)a.n_slots, of_heads = (float)(n_units * a.n_kv_heads);
+    // units as long as each other go in rounds, others into the gaps
+    const float in_rounds = ceilf(of_heads / slots) * size, in_gaps = ((float)a.n_kv_heads * tiles + of_heads * (5.f + cut)) / slots + 0.5f * size;
+    float cost = fmaxf(fminf(in_rounds, in_gaps), size);
+    if (lane > 0 && (lane >= kTry || len_y < 8 || extra > a.extra_most || min(n_units, 2 * extra) > a.parts_most)) cost = INFINITY;
     float least = cost;
 #pragma unroll
     for (int by = 32; by > 0; by /= 2) least = fminf(least, __shfl_xor(least, by));
@@ -528,9 +540,9 @@ template <int B, bool kList, bool kGeneral>
 __global__ __launch_bounds__(256, 2) void attend_many_kernel(AttendArgs a)
 {
     constexpr int PPT = 64 / B;
-    extern __shared__ uint4 stages[];                 // [2][kManyStage]
+    extern __shared__ uint4 stages[];                 // [2][1024] keys, [2][1024] values
     __shared__ Odd odd[256];
-    __shared__ int flag;
+    __shared__ int wave_lo[4], wave_hi[4], flag;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     const int col = lane & 31, half = lane >> 5;
     const int H = a.n_kv_heads, G = a.group, h = blockIdx.x % H, unit = blockIdx.x / H;
@@ -548,8 +560,9 @@ __global__ __launch_bounds__(256, 2) void attend_many_kernel(AttendArgs a)
         t_end = (n_list + PPT - 1) / PPT;
     }
     if (P == 0) t_end = 0;
+    const int t_first = t;
 
-    // a wave brings 16 keys and their values
+    // a wave brings 16 keys, and 16 keys' values
     const PageLanes from(lane, B);
     const uint32_t to = lds_at(stages) + (uint32_t)wave * 4096;
     const auto page_at = [&](int i) {
@@ -557,16 +570,33 @@ __global__ __launch_bounds__(256, 2) void attend_many_kernel(AttendArgs a)
         if constexpr (kList) p = load_same(ids, min(i, a.max_sel - 1));
         return i < n_list && p >= 0 && p < P ? p : -1;
     };
-    const auto fetch = [&](int phys, int stage) {
-        const int64_t at = ((int64_t)phys * H + h) * (B * kHeadDim) + (B == 32 ? (wave & 1) * 2048 : 0);
-        load_4k(to + (uint32_t)stage * (kManyStage * 16), a.k_pool + at, from.key[0], from.key[1], from.key[2], from.key[3]);
-        load_4k(to + (uint32_t)stage * (kManyStage * 16) + 16384, a.v_pool + at, from.value, from.value, from.value, from.value);
+    const auto place = [&](int phys) { return ((int64_t)__builtin_amdgcn_readfirstlane(phys) * H + h) * (B * kHeadDim) + (B == 32 ? (wave & 1) * 2048 : 0); };
+    const auto fetch_keys = [&](int phys, int stage) {
+        load_4k(to + (uint32_t)stage * 16384, a.k_pool + place(phys), from.key[0], from.key[1], from.key[2], from.key[3]);
     };
-    const auto phys_of = [&](int tile) { return load_same(table, max(page_at(tile * PPT + (B == 32 ? wave >> 1 : wave)), 0)); };
-    int phys = 0;
+    const auto fetch_values = [&](int phys, int stage) {
+        load_4k(to + 32768 + (uint32_t)stage * 16384, a.v_pool + place(phys), from.value, from.value, from.value, from.value);
+    };
+    // Physical pages by the 64, one a lane: a window of the table (or list) is asked for a window ahead, and what a tile needs of it is read from a lane.
+    // (A scalar load a tile would be waited for with the LDS reads, which count with it.)
+    constexpr int kWindow = 64 / PPT;                 // tiles
+    const auto page_of_tile = [&](int tile) { return tile * PPT + (B == 32 ? wave >> 1 : wave); };
+    const auto window_at = [&](int tile) {
+        const int i = min(tile / kWindow * 64 + lane, kList ? a.max_sel - 1 : a.max_pages - 1);
+        int p = i;
+        if constexpr (kList) p = ids[i];
+        return table[i < n_list && p >= 0 && p < P ? p : 0];
+    };
+    // keys of tile t and t + 1, values of t
+    int phys = 0, window = 0, window_next = 0;        // phys: of tile t + 1; the window that tile t + 2 is in
     if (t < t_end) {
-        fetch(phys_of(t), 0);
-        phys = phys_of(min(t + 1, t_end - 1));
+        const int first = load_same(table, max(page_at(page_of_tile(t)), 0));
+        fetch_keys(first, 0);
+        phys = load_same(table, max(page_at(page_of_tile(min(t + 1, t_end - 1))), 0));
+        fetch_keys(phys, 1);
+        fetch_values(first, 0);
+        window = window_at(t + 2);
+        window_next = window_at(t + 2 + kWindow);
     }
 
     RowView row = view_of(a, span, b, h, row0 + col);
@@ -577,7 +607,12 @@ __global__ __launch_bounds__(256, 2) void attend_many_kernel(AttendArgs a)
 #pragma unroll
         for (int s = 0; s < 8; ++s) q[s] = src[2 * s];
     }
-    const int all_lo = lanes_max(row.there ? row.lo : 0), all_hi = lanes_min(row.there ? row.hi : INT32_MAX);
+    // what all rows of the block see
+    int all_lo = lanes_max(row.there ? row.lo : 0), all_hi = lanes_min(row.there ? row.hi : INT32_MAX);
+    if (lane == 0) {
+        wave_lo[wave] = all_lo;
+        wave_hi[wave] = all_hi;
+    }
 
     float m = kNegBig, l = 0.f;
     f32x16 o[4];
@@ -588,24 +623,32 @@ __global__ __launch_bounds__(256, 2) void attend_many_kernel(AttendArgs a)
 #pragma unroll
         for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
 
-    int stage = 0;
-    const uint4 *keys, *values;
-    // the next tile is there, and nobody reads the last one any more: the one behind it into that one's place
+    loads_left<0>();
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+        all_lo = max(all_lo, wave_lo[w]);
+        all_hi = min(all_hi, wave_hi[w]);
+    }
+    all_lo = __builtin_amdgcn_readfirstlane(all_lo);
+    all_hi = __builtin_amdgcn_readfirstlane(all_hi);
+
+    int stage = 0;                                    // of tile t
+    // Keys of tile t + 1 and values of t are there, and nobody reads the keys of t and the values of t - 1 any more: those of t + 2 and t + 1 into their places.
+    // (The first tile's are there already.)
     const auto begin_tile = [&] {
         loads_left<0>();
-        __syncthreads();
-        if (t + 1 < t_end) {
-            fetch(phys, stage ^ 1);
-            phys = phys_of(min(t + 2, t_end - 1));
+        if ((t + 2) % kWindow == 0 && t > t_first) {
+            window = window_next;
+            window_next = window_at(t + 2 + kWindow);
         }
-        keys = stages + stage * kManyStage;
-        values = keys + 1024;
+        __syncthreads();
+        const int phys_next = __builtin_amdgcn_readlane(window, page_of_tile(t + 2) & 63);
+        if (t + 2 < t_end) fetch_keys(phys_next, stage);
+        if (t + 1 < t_end) fetch_values(phys, stage ^ 1);
+        phys = phys_next;
     };
-    const auto end_tile = [&] {
-        ++t;
-        stage ^= 1;
-    };
-    // whether every row sees all of tile t (the same in every lane)
+    // whether every row of the block sees all of tile t (the same in every wave)
     const auto is_whole = [&] {
         if constexpr (!kList) return ((t * 64 - all_lo) | (all_hi - t * 64 - 63)) >= 0;
         int less = 0;
@@ -620,36 +663,83 @@ __global__ __launch_bounds__(256, 2) void attend_many_kernel(AttendArgs a)
         const int p = page_at(t * PPT + 16 * i / B);
         return p < 0 ? INT32_MIN / 2 : p * B + (16 * i) % B + 8 * half;
     };
-    // scores of 32 keys, from y on; z[8 s + e] is key 32 y + 16 s + 8 half + e of the tile
-    const auto scores = [&](f32x16& z, int y) {
+    // z[y][8 s + e] is key 32 y + 16 s + 8 half + e of a tile
+    const auto products = [&](f32x16 (&z)[2], int of_stage) {
+        const uint4* keys = stages + of_stage * 1024;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) z[i] = 0.f;
+        for (int y = 0; y < 2; ++y)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) z[y][i] = 0.f;
 #pragma unroll
         for (int s = 0; s < 8; ++s)
-            z = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(keys[key_piece(32 * y + key_of_col(col), half, s)]), as_bf16x8(q[s]), z, 0, 0, 0);
+#pragma unroll
+            for (int y = 0; y < 2; ++y)
+                z[y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(keys[key_piece(32 * y + key_of_col(col), half, s)]), as_bf16x8(q[s]), z[y], 0, 0, 0);
+    };
+    // values that are not finite, as above: what they do to the rows that see them is noted, then they are taken out of the tile, by all waves for all
+    const auto clean = [&](const Seen (&seen)[2]) {
+        uint4* values = stages + 2048 + stage * 1024;
+        Magnitudes most = {0, 0};
+#pragma unroll
+        for (int i = 0; i < 16; ++i) most = larger(most, values[i * 64 + lane]);
+        if (__builtin_expect(!not_finite(most), 1)) return;
+        any_odd = true;
+#pragma unroll
+        for (int y = 0; y < 2; ++y) note_not_finite<B>(odd + threadIdx.x, values, 2 * y, col, half, seen[y]);
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < 4; ++i) values[i * 256 + threadIdx.x] = finite_of(values[i * 256 + threadIdx.x]);
+        __syncthreads();
+    };
+    const float scale = kGeneral ? 1.f : a.scale_log2;
+    // Tile t, whose products are in z; those of t + 1 into next while the exponentials of t are worked out.
+    const auto work_on = [&](f32x16 (&z)[2], f32x16 (&next)[2]) {
+        begin_tile();
         if constexpr (kGeneral) {
             if (a.cap_in != 0.f) {
 #pragma unroll
-                for (int i = 0; i < 16; ++i) z[i] = score_of<true>(a, z[i]);
+                for (int y = 0; y < 2; ++y)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) z[y][i] = score_of<true>(a, z[y][i]);
             } else {
 #pragma unroll
-                for (int i = 0; i < 16; ++i) z[i] = score_of<false>(a, z[i]);
+                for (int y = 0; y < 2; ++y)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) z[y][i] = score_of<false>(a, z[y][i]);
             }
-            __builtin_amdgcn_sched_barrier(0);
             if (a.slopes != nullptr)
 #pragma unroll
-                for (int s = 0; s < 2; ++s) {
-                    const float d = (float)(row.p - first_key(2 * y + s));
+                for (int i = 0; i < 4; ++i) {
+                    const float d = (float)(row.p - first_key(i));
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) z[8 * s + e] = fmaf(-row.slope, fabsf(d - (float)e), z[8 * s + e]);
+                    for (int e = 0; e < 8; ++e) z[i >> 1][8 * (i & 1) + e] = fmaf(-row.slope, fabsf(d - (float)e), z[i >> 1][8 * (i & 1) + e]);
                 }
         }
-    };
-    const float scale = kGeneral ? 1.f : a.scale_log2;
-    // the running maximum (of scores times `scale`), and what was summed, to a new one
-    const auto raise = [&](float largest) {
+        if (!is_whole()) {
+            Seen seen[2];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int key0 = first_key(i);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const bool see = key0 + e >= row.lo && key0 + e <= row.hi;
+                    const float x = z[i >> 1][8 * (i & 1) + e];
+                    seen[i >> 1].any |= see ? 1u << (8 * (i & 1) + e) : 0u;
+                    seen[i >> 1].lowest |= see && x == -INFINITY ? 1u << (8 * (i & 1) + e) : 0u;
+                    z[i >> 1][8 * (i & 1) + e] = see ? x : -INFINITY;
+                }
+            }
+            clean(seen);
+        }
+        float largest = z[0][0];
+#pragma unroll
+        for (int y = 0; y < 2; ++y)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) largest = fmaxf(largest, z[y][i]);
+        // The running maximum (of scores times `scale`) and what was summed are moved to a new one where that is 2^8 times as large: until then weights above 1 do
+        // no harm.
         const float m_new = fmaxf(m, product(fmaxf(largest, __shfl_xor(largest, 32)), scale));
-        if (__any(m_new > m)) {
+        if (__any(m_new - m > 8.f)) {
             const float alpha = __builtin_amdgcn_exp2f(m - m_new);
             l *= alpha;
 #pragma unroll
@@ -658,121 +748,58 @@ __global__ __launch_bounds__(256, 2) void attend_many_kernel(AttendArgs a)
                 for (int i = 0; i < 16; ++i) o[d][i] *= alpha;
             m = m_new;
         }
-    };
-    // a score times `scale` this large is rounded before the difference, as the maximum was: what one rounding would keep could weigh more than 1
-    const auto is_large = [&] { return !kGeneral && __any(fabsf(m) > 0x1p24f && m != kNegBig); };
-    while (!works && t < t_end) {
-        begin_tile();
-        end_tile();
-    }
-    while (t < t_end) {
-        for (; t < t_end && is_whole(); end_tile()) {
-            begin_tile();
-            f32x16 z[2];
-            scores(z[0], 0);
-            scores(z[1], 1);
-            float largest = z[0][0];
+        // a score times `scale` this large is rounded before the difference, as the maximum was: what one rounding would keep could weigh more than 1
+        float by = scale, top = m;
+        if (!kGeneral && __builtin_expect(__any(fabsf(m_new) > 0x1p24f && m != kNegBig), 0)) {
 #pragma unroll
             for (int y = 0; y < 2; ++y)
 #pragma unroll
-                for (int i = 0; i < 16; ++i) largest = fmaxf(largest, z[y][i]);
-            raise(largest);
-            float by = scale, top = m;
-            if (__builtin_expect(is_large(), 0)) {
+                for (int i = 0; i < 16; ++i) z[y][i] = product(z[y][i], scale) - m;
+            by = 1.f;
+            top = 0.f;
+        }
+        __builtin_amdgcn_s_setprio(1);
+        products(next, stage ^ 1);                    // (behind the last tile: of whatever is there)
+        float sum = 0.f;
+        bf16x8 w[2][2];
 #pragma unroll
-                for (int y = 0; y < 2; ++y)
+        for (int y = 0; y < 2; ++y)
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) z[y][i] = product(z[y][i], scale) - m;
-                by = 1.f;
-                top = 0.f;
-            }
-            float sum = 0.f;
-            bf16x8 w[2][2];
+            for (int s = 0; s < 2; ++s)
 #pragma unroll
-            for (int y = 0; y < 2; ++y)
+                for (int e = 0; e < 8; ++e) {
+                    const float x = __builtin_amdgcn_exp2f(kGeneral ? z[y][8 * s + e] - top : fmaf(z[y][8 * s + e], by, -top));
+                    sum += x;
+                    w[y][s][e] = (__bf16)x;
+                }
+        l += sum;
+        const uint4* values = stages + 2048 + stage * 1024;
 #pragma unroll
-                for (int s = 0; s < 2; ++s)
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        const float x = __builtin_amdgcn_exp2f(kGeneral ? z[y][8 * s + e] - top : fmaf(z[y][8 * s + e], by, -top));
-                        sum += x;
-                        w[y][s][e] = (__bf16)x;
-                    }
-            l += sum;
+        for (int s = 0; s < 4; ++s)
 #pragma unroll
             for (int d = 0; d < 4; ++d)
-#pragma unroll
-                for (int s = 0; s < 4; ++s)
-                    o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(values[value_piece<B>(32 * d + col, half, s)]), w[s >> 1][s & 1], o[d], 0, 0, 0);
+                o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(values[value_piece<B>(32 * d + col, half, s)]), w[s >> 1][s & 1], o[d], 0, 0, 0);
+        __builtin_amdgcn_s_setprio(0);
+        ++t;
+        stage ^= 1;
+    };
+    if (works) {
+        f32x16 z[2], z_next[2];
+        if (t < t_end) products(z, 0);
+        while (t < t_end) {
+            work_on(z, z_next);
+            if (t >= t_end) break;
+            work_on(z_next, z);
         }
-        // tiles that not every row sees whole: 32 keys at a time
-        for (; t < t_end && !is_whole(); end_tile()) {
+    } else {
+        while (t < t_end) {
             begin_tile();
-#pragma nounroll
-            for (int y = 0; y < 2; ++y) {
-                f32x16 z;
-                scores(z, y);
-                Seen seen;
-                float largest = kNegBig;
-#pragma unroll
-                for (int s = 0; s < 2; ++s) {
-                    const int key0 = first_key(2 * y + s);
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        const bool see = key0 + e >= row.lo && key0 + e <= row.hi;
-                        seen.any |= see ? 1u << (8 * s + e) : 0u;
-                        seen.lowest |= see && z[8 * s + e] == -INFINITY ? 1u << (8 * s + e) : 0u;
-                        z[8 * s + e] = see ? z[8 * s + e] : -INFINITY;
-                        largest = fmaxf(largest, z[8 * s + e]);
-                    }
-                }
-                raise(largest);
-                float by = scale, top = m;
-                if (__builtin_expect(is_large(), 0)) {
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) z[i] = product(z[i], scale) - m;
-                    by = 1.f;
-                    top = 0.f;
-                }
-                float sum = 0.f;
-                bf16x8 w[2];
-#pragma unroll
-                for (int s = 0; s < 2; ++s)
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        const float x = __builtin_amdgcn_exp2f(kGeneral ? z[8 * s + e] - top : fmaf(z[8 * s + e], by, -top));
-                        sum += x;
-                        w[s][e] = (__bf16)x;
-                    }
-                l += sum;
-                __builtin_amdgcn_sched_barrier(0);    // (the values are not asked for earlier: registers are not free)
-                uint4 v[4][2];
-                Magnitudes most = {0, 0};
-#pragma unroll
-                for (int d = 0; d < 4; ++d)
-#pragma unroll
-                    for (int s = 0; s < 2; ++s) {
-                        v[d][s] = values[value_piece<B>(32 * d + col, half, 2 * y + s)];
-                        most = larger(most, v[d][s]);
-                    }
-                // (values that are not finite, as above; where every row sees every key there is nothing to take out)
-                if (__builtin_expect(not_finite(most), 0)) {
-                    any_odd = true;
-                    note_not_finite<B>(odd + threadIdx.x, values, 2 * y, col, half, seen);
-                    asm volatile("" : : : "memory");  // (read again: registers are not free)
-#pragma unroll
-                    for (int d = 0; d < 4; ++d)
-#pragma unroll
-                        for (int s = 0; s < 2; ++s) v[d][s] = finite_of(values[value_piece<B>(32 * d + col, half, 2 * y + s)]);
-                }
-#pragma unroll
-                for (int d = 0; d < 4; ++d)
-#pragma unroll
-                    for (int s = 0; s < 2; ++s) o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(v[d][s]), w[s], o[d], 0, 0, 0);
-            }
+            const Seen none[2];
+            if (!is_whole()) clean(none);
+            ++t;
+            stage ^= 1;
         }
     }
-
     if (any_odd) add_not_finite(o, odd[threadIdx.x]);
     l += __shfl_xor(l, 32);
     if (n_parts == 1) {
@@ -833,8 +860,7 @@ template <int B, bool kList>
 static hipError_t launch_many(chess_ctx* ctx, const AttendArgs& a, const AttendShape& s, bool general, hipStream_t stream)
 {
     const dim3 grid((unsigned)((s.blocks + s.extra) * a.n_kv_heads));
-    constexpr size_t lds = 2 * kManyStage * 16;
-    return general ? launch_lds<attend_many_kernel<B, kList, true>>(ctx, grid, lds, stream, a) : launch_lds<attend_many_kernel<B, kList, false>>(ctx, grid, lds, stream, a);
+    return general ? launch_lds<attend_many_kernel<B, kList, true>>(ctx, grid, kManyLds, stream, a) : launch_lds<attend_many_kernel<B, kList, false>>(ctx, grid, kManyLds, stream, a);
 }
 
 // Few rows: a line a KV head.  Many: units; `most` blocks and cut units that there can be, whatever the sequences are.
@@ -853,8 +879,8 @@ AttendShape attend_shape(const chess_ctx* ctx, int64_t n_rows, int64_t max_new, 
     s.rows = kBlockRows;
     s.n_slots = 2 * (int64_t)ctx->n_cu;               // workgroups that are on the card at once
     s.blocks = n_rows * g.group / kBlockRows + std::min(batch, n_rows);
-    s.extra = 4 * cu;
-    s.parts = 2 * s.extra * g.n_kv_heads;             // (a block of n units has n partials, and n - 1 units more than one)
+    s.extra = 6 * cu;
+    s.parts = 8 * cu * g.n_kv_heads;                  // (a block of n units has n partials, and n - 1 units more than one)
     return s;
 }
 
@@ -872,6 +898,7 @@ hipError_t launch_attend(chess_ctx* ctx, AttendArgs a, const AttendShape& s, hip
     }
     a.blocks_most = (int)s.blocks;
     a.extra_most = (int)s.extra;
+    a.parts_most = (int)(s.parts / a.n_kv_heads);
     const hipError_t e = launch(b16 ? plan_kernel<16> : plan_kernel<32>, dim3(1), dim3(kPlanThreads), (size_t)a.batch * sizeof(int), stream, a);
     if (e != hipSuccess) return e;
     const bool general = cap || a.slopes != nullptr;

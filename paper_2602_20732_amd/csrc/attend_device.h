@@ -155,10 +155,11 @@ __device__ __forceinline__ uint4 finite_of(const uint4& v)
 // for each thread: this is rare, and registers are not free.
 struct Odd { uint64_t up, down; };
 
+// Where the piece of a dim lies that has the eight keys 16 s + 8 half .. of a tile.
 template <int B>
 __device__ __forceinline__ int value_piece(int dim, int half, int s)
 {
-    return B == 16 ? s * 256 + dim * 2 + half : (s >> 1) * 512 + dim * 4 + ((2 * (s & 1) + half) ^ ((dim >> 2) & 3));
+    return B == 16 ? s * 256 + (dim >> 4) * 32 + half * 16 + (dim & 15) : (s >> 1) * 512 + (dim >> 4) * 64 + (2 * (s & 1) + half) * 16 + (dim & 15);
 }
 
 // Which of a lane's keys (bit 8 s + e of a 32 keys') its row sees, and which of those have a score of -infinity: these weigh nothing, and nothing times an
@@ -272,9 +273,10 @@ __device__ __forceinline__ void load_4k(uint32_t lds, const void* base, uint32_t
 template <int kLeft>
 __device__ __forceinline__ void loads_left()
 {
-    static_assert(kLeft == 0 || kLeft == 16);
-    if constexpr (kLeft == 0) asm volatile("s_waitcnt vmcnt(0)" : : : "memory");
-    else asm volatile("s_waitcnt vmcnt(16)" : : : "memory");
+    static_assert(kLeft < 64);
+    asm volatile("" : : : "memory");
+    __builtin_amdgcn_s_waitcnt(0xf70 | (kLeft & 15) | (kLeft >> 4) << 14);       // vmcnt(kLeft), nothing else; the compiler counts its own loads with it
+    asm volatile("" : : : "memory");
 }
 __device__ __forceinline__ void reads_done() { asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory"); }
 
@@ -284,21 +286,24 @@ __device__ __forceinline__ uint32_t lds_at(T* p) { return (uint32_t)(uintptr_t)(
 // The same number in every lane, as a load of its own that does not count with the lanes' loads.
 __device__ __forceinline__ int load_same(const int32_t* p, int64_t i) { return ((const __attribute__((address_space(4))) int32_t*)p)[i]; }
 
-// What a lane reads of 16 keys (4 KB; of keys 16 .. 31 of a page the same) and of 4 KB of a page's values.
-// Keys: row r has its 16-byte piece c at c ^ (r % 16), so that the same piece of sixteen rows is on all banks.  Values of pages of 16: as they are, a lane
-// reads 16 bytes of 32 of a dim, 64 lanes a KB.  Of 32: a dim's four pieces at j ^ (dim / 4 % 4).
+// What a lane reads of 16 keys (4 KB; of keys 16 .. 31 of a page the same) and of 4 KB of a page's values, so that sixteen lanes one behind the other, which read
+// at once, find the pieces of 16 bytes that they want in different ones of the 16 that lie across all banks.
+// Keys: row r has its piece c at c ^ turned(r), and lanes read rows in the order of turned(r).  Values: of sixteen dims, first every one's first piece, then every
+// one's second and so on (two of a dim in pages of 16, four in pages of 32); as they lie in memory, a read of pages of 16 took 8 cycles where it takes 4.
+__device__ __forceinline__ int turned(int r) { return (r & 19) + ((r & 4) << 1) + ((r & 8) >> 1); }     // bits 2 and 3 change places
 struct PageLanes {
     uint32_t key[4], value;
     __device__ __forceinline__ PageLanes(int lane, int page_size)
     {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) key[i] = (uint32_t)((lane >> 4) * 256 + (((lane & 15) ^ (4 * i + (lane >> 4))) & 15) * 16);
-        value = page_size == 16 ? (uint32_t)lane * 16 : (uint32_t)((lane >> 2) * 64 + ((lane & 3) ^ (lane >> 4)) * 16);
+        for (int i = 0; i < 4; ++i) key[i] = (uint32_t)((lane >> 4) * 256 + ((lane & 15) ^ turned(4 * i + (lane >> 4))) * 16);
+        value = (uint32_t)(page_size == 16 ? ((lane >> 5) * 16 + (lane & 15)) * 2 + ((lane >> 4) & 1) : (lane & 15) * 4 + (lane >> 4)) * 16;
     }
 };
 
 // Where 32 keys' operands lie in LDS, in 16-byte pieces from their page's (pages': of 16) beginning.  Row `col` of a product over keys is key
 // 16 (col / 16) + 8 (bit 2) + 4 (bit 3) + (col % 4), and with it the 16 weights of a lane are keys 8 half .. + 7 and 16 + 8 half .. + 7.
-__device__ __forceinline__ int key_of_col(int col) { return (col & 16) + ((col & 4) << 1) + ((col & 8) >> 1) + (col & 3); }
-__device__ __forceinline__ int key_piece(int key, int half, int step) { return key * 16 + ((2 * step + half) ^ (key & 15)); }
+__device__ __forceinline__ int key_of_col(int col) { return turned(col); }
+__device__ __forceinline__ int key_piece(int key, int half, int step) { return key * 16 + ((2 * step + half) ^ turned(key & 15)); }
+
 }  // namespace chess
