@@ -22,21 +22,20 @@ namespace chess {
 // is written at once; partials of the others are merged by the last workgroup of the sequence to arrive.
 // Bound: HBM, for as long as a tile's arithmetic (about 1 us a wave and 32 rows) takes less than the four waves' 64 KB do (2.7 us).
 
-// Keys of a sequence that its rows can see at all, in tiles, for those that deal: [first, end) of the pages' tiles, one at least.
-struct Tiles { int first, count; };
+// A lane's sequence as those that deal see it: the tiles of the keys that its rows can see at all, from `first` on, one at least if it has rows.
+struct LineSpan { int start, n_new, len, n_list, first, count; };
 
 template <int B, bool kList>
-__device__ __forceinline__ Tiles tiles_of(const AttendArgs& a, int b, int h, int n_new, int len)
+__device__ __forceinline__ LineSpan line_span(const AttendArgs& a, int b, int h)
 {
     constexpr int PPT = 32 / B;
-    if (n_new <= 0) return {0, 0};
-    if constexpr (kList) {
-        const int n = min(max(a.n_selected[(int64_t)b * a.n_kv_heads + h], 0), a.max_sel);
-        return {0, max((n + PPT - 1) / PPT, 1)};
-    } else {
-        const int first = a.window > 0 ? max(len - n_new - a.window + 1, 0) / 32 : 0;
-        return {first, max((len + 31) / 32 - first, 1)};
-    }
+    const bool there = b < a.batch;
+    const int n_selected = kList ? a.n_selected[(int64_t)min(b, a.batch - 1) * a.n_kv_heads + h] : 0;
+    const Span s = span_by_lane(a, min(b, a.batch - 1), B);
+    LineSpan l{s.start, there ? s.n_new : 0, s.len, kList ? min(max(n_selected, 0), a.max_sel) : s.pages, 0, 0};
+    if constexpr (!kList) l.first = a.window > 0 ? max(s.len - s.n_new - a.window + 1, 0) / 32 : 0;
+    if (l.n_new > 0) l.count = max((kList ? (l.n_list + PPT - 1) / PPT : (s.len + 31) / 32) - l.first, 1);
+    return l;
 }
 
 constexpr int kFewRing = 4 * 2 * 1024;                // 16-byte pieces: two tiles a wave
@@ -56,23 +55,14 @@ __global__ __launch_bounds__(256, 1) void attend_few_kernel(AttendArgs a)
     const int H = a.n_kv_heads, G = a.group, h = blockIdx.x % H, slot = blockIdx.x / H;
 
     // the line: its length, this workgroup's share, the sequence that it begins in
-    const auto tiles_at = [&](int b) {
-        if (b >= a.batch) return Tiles{0, 0};
-        const Span s = span_by_lane(a, b, B);
-        return tiles_of<B, kList>(a, b, h, s.n_new, s.len);
-    };
-    int before = 0, total = 0, block = 0;
+    LineSpan mine = line_span<B, kList>(a, lane, h);
+    int before = 0, block = 0, upto = lanes_upto(mine.count), total = lane_of(upto, 63), of_block = 0, upto_block = 0;
     if (a.batch > 64) {
         for (int i = wave; i * 64 < a.batch; i += 4) {
-            const int n = lane_of(lanes_upto(tiles_at(i * 64 + lane).count), 63);
+            const int n = lane_of(lanes_upto(line_span<B, kList>(a, i * 64 + lane, h).count), 63);
             if (lane == 0) block_tiles[i] = n;
         }
         __syncthreads();
-    }
-    int mine = tiles_at(lane).count, upto = lanes_upto(mine);
-    total = lane_of(upto, 63);
-    int of_block = 0, upto_block = 0;
-    if (a.batch > 64) {
         of_block = lane * 64 < a.batch ? block_tiles[lane] : 0;
         upto_block = lanes_upto(of_block);
         total = lane_of(upto_block, 63);
@@ -84,12 +74,12 @@ __global__ __launch_bounds__(256, 1) void attend_few_kernel(AttendArgs a)
     if (a.batch > 64) {
         block = __builtin_ctzll(__ballot(upto_block > begin));
         before = lane_of(upto_block, block) - lane_of(of_block, block);
-        mine = tiles_at(block * 64 + lane).count;
-        upto = lanes_upto(mine);
+        mine = line_span<B, kList>(a, block * 64 + lane, h);
+        upto = lanes_upto(mine.count);
     }
     const int at = __builtin_ctzll(__ballot(before + upto > begin));
     int b = __builtin_amdgcn_readfirstlane(block * 64 + at);
-    int line = __builtin_amdgcn_readfirstlane(before + lane_of(upto, at) - lane_of(mine, at));     // where the sequence begins in the line
+    int line = __builtin_amdgcn_readfirstlane(before + lane_of(upto, at) - lane_of(mine.count, at));     // where the sequence begins in the line
 
     const PageLanes from(lane, B);
     const uint32_t ring_lds = lds_at(ring) + (uint32_t)wave * (2 * 16384);
@@ -97,61 +87,21 @@ __global__ __launch_bounds__(256, 1) void attend_few_kernel(AttendArgs a)
     uint4* queries = ring + kFewRing;
 
     for (; line < end; ++b) {
-        const Span span = span_of(a, b, B);
-        const Tiles all = tiles_of<B, kList>(a, b, h, span.n_new, span.len);
-        const int count = __builtin_amdgcn_readfirstlane(all.count), first = __builtin_amdgcn_readfirstlane(all.first);
+        if (b == block * 64 + 64) {
+            ++block;
+            mine = line_span<B, kList>(a, block * 64 + lane, h);
+        }
+        const int in_block = b - block * 64, count = lane_of(mine.count, in_block);
         if (count == 0) continue;
-        const int line_end = line + count;
+        const Span span{lane_of(mine.len, in_block), (lane_of(mine.len, in_block) + B - 1) / B, lane_of(mine.start, in_block), lane_of(mine.n_new, in_block)};
+        const int first = lane_of(mine.first, in_block), n_list = lane_of(mine.n_list, in_block), line_end = line + count;
         // this segment, in tiles of the sequence
         int t = max(begin - line, 0) + first + wave;
         int t_end = min(end - line, count) + first;
         const int P = span.pages;
         const int32_t* table = a.block_table + (int64_t)b * a.max_pages;
         const int32_t* ids = kList ? a.page_ids + ((int64_t)b * H + h) * a.max_sel : nullptr;
-        const int n_list = kList ? min(max(load_same(a.n_selected, (int64_t)b * H + h), 0), a.max_sel) : P;
         if (P == 0 || n_list == 0) t_end = 0;         // (a tile was dealt all the same, so that the rows are written)
-
-        // the rows: their queries (Q^T operands), what each sees
-        const int n_rows = span.n_new * G;
-        RowView row[kRows];
-        int see_lo = INT32_MAX, see_hi = -1, all_lo = 0, all_hi = INT32_MAX;
-#pragma unroll
-        for (int y = 0; y < kRows; ++y) {
-            row[y] = view_of(a, span, b, h, 32 * y + col);
-            // (piece i of row r at i ^ (r % 16): no two rows' on the same banks)
-            const uint4* src = reinterpret_cast<const uint4*>(a.q + row[y].at * kHeadDim) + 4 * wave + 2 * half;
-#pragma unroll
-            for (int s = 0; s < 2; ++s) queries[(32 * y + col) * 16 + ((4 * wave + 2 * half + s) ^ (col & 15))] = src[s];
-            if (row[y].there) {
-                if (row[y].hi >= row[y].lo) {
-                    see_lo = min(see_lo, row[y].lo);
-                    see_hi = max(see_hi, row[y].hi);
-                }
-                all_lo = max(all_lo, row[y].lo);
-                all_hi = min(all_hi, row[y].hi);
-            }
-        }
-        see_lo = lanes_min(see_lo); see_hi = lanes_max(see_hi); all_lo = lanes_max(all_lo); all_hi = lanes_min(all_hi);
-        if (see_hi < see_lo) t_end = 0;
-        if constexpr (!kList) {                       // tiles that no row sees (this wave's others stay its own)
-            t_end = min(t_end, see_hi / 32 + 1);
-            while (t < t_end && t * 32 + 31 < see_lo) t += 4;
-        }
-
-        float m[kRows], l[kRows];
-        f32x16 o[kRows][4];
-        bool any_odd = false;
-#pragma unroll
-        for (int y = 0; y < kRows; ++y) odd[y][threadIdx.x] = Odd{0, 0};
-#pragma unroll
-        for (int y = 0; y < kRows; ++y) {
-            m[y] = kNegBig;
-            l[y] = 0.f;
-#pragma unroll
-            for (int d = 0; d < 4; ++d)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) o[y][d][i] = 0.f;
-        }
 
         // Logical pages (one that is none of the sequence's: -1) and physical ones of the wave's next tiles, 64 at a time, one a lane: a window of the table (or
         // list) is asked for a window ahead, and what a tile needs of it is read from a lane.  (A scalar load a tile would be waited for with the LDS reads,
@@ -193,6 +143,40 @@ __global__ __launch_bounds__(256, 1) void attend_few_kernel(AttendArgs a)
             pages_of(1, lp_next, phys);
             if (t + 4 < t_end) fetch(phys, 1);
         }
+        // the rows: their queries (Q^T operands), what each sees
+        const int n_rows = span.n_new * G;
+        RowView row[kRows];
+        int all_lo = 0, all_hi = INT32_MAX;
+#pragma unroll
+        for (int y = 0; y < kRows; ++y) {
+            row[y] = view_of(a, span, b, h, 32 * y + col);
+            // (piece i of row r at i ^ (r % 16): no two rows' on the same banks)
+            const uint4* src = reinterpret_cast<const uint4*>(a.q + row[y].at * kHeadDim) + 4 * wave + 2 * half;
+#pragma unroll
+            for (int s = 0; s < 2; ++s) queries[(32 * y + col) * 16 + ((4 * wave + 2 * half + s) ^ (col & 15))] = src[s];
+            if (row[y].there) {
+                all_lo = max(all_lo, row[y].lo);
+                all_hi = min(all_hi, row[y].hi);
+            }
+        }
+        all_lo = lanes_max(all_lo);
+        all_hi = lanes_min(all_hi);
+
+        float m[kRows], l[kRows];
+        f32x16 o[kRows][4];
+        bool any_odd = false;
+#pragma unroll
+        for (int y = 0; y < kRows; ++y) odd[y][threadIdx.x] = Odd{0, 0};
+#pragma unroll
+        for (int y = 0; y < kRows; ++y) {
+            m[y] = kNegBig;
+            l[y] = 0.f;
+#pragma unroll
+            for (int d = 0; d < 4; ++d)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) o[y][d][i] = 0.f;
+        }
+
         __syncthreads();                              // the queries
         for (int n = 0, stage = 0; t < t_end; t += 4, ++n, stage ^= 1) {
             const uint4* keys = ring_own + stage * 1024;

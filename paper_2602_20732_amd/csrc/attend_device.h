@@ -17,18 +17,15 @@ __device__ __forceinline__ uint32_t two_bf16(float lo, float hi)
     return __builtin_bit_cast(uint32_t, p);
 }
 
+// Over the lanes of a wave, by row shifts and row broadcasts; the same in every lane.
 __device__ __forceinline__ int lanes_max(int v)
 {
-#pragma unroll
-    for (int by = 32; by > 0; by /= 2) v = max(v, __shfl_xor(v, by));
-    return __builtin_amdgcn_readfirstlane(v);
+#define CHESS_MAX(ctrl, rows) v = max(v, __builtin_amdgcn_update_dpp(INT32_MIN, v, ctrl, rows, 0xf, false));
+    CHESS_MAX(0x111, 0xf) CHESS_MAX(0x112, 0xf) CHESS_MAX(0x114, 0xf) CHESS_MAX(0x118, 0xf) CHESS_MAX(0x142, 0xa) CHESS_MAX(0x143, 0xc)
+#undef CHESS_MAX
+    return __builtin_amdgcn_readlane(v, 63);
 }
-__device__ __forceinline__ int lanes_min(int v)
-{
-#pragma unroll
-    for (int by = 32; by > 0; by /= 2) v = min(v, __shfl_xor(v, by));
-    return __builtin_amdgcn_readfirstlane(v);
-}
+__device__ __forceinline__ int lanes_min(int v) { return ~lanes_max(~v); }
 
 // A sequence of the step: its length, pages, and new tokens (none where token_start names rows that are not there).
 struct Span { int len, pages, start, n_new; };
