@@ -116,13 +116,14 @@ __global__ __launch_bounds__(256, 1) void attend_few_kernel(AttendArgs a)
             const int page = i < n_list && p >= 0 && p < P ? p : -1;
             return Window{page, table[max(page, 0)]};
         };
+        // (Read once, so not kept in the caches: 32 sequences' lists 57.5 -> 51.6 us, every page of 16 sequences 409 -> 376.)
         const auto fetch = [&](const int (&phys)[PPT], int stage) {
             const uint32_t to = ring_lds + (uint32_t)stage * 16384;
 #pragma unroll
             for (int s = 0; s < 2; ++s) {
                 const int64_t at = ((int64_t)__builtin_amdgcn_readfirstlane(phys[s * PPT / 2]) * H + h) * (B * kHeadDim) + (PPT == 1 ? s * 2048 : 0);
-                load_4k(to + s * 4096, a.k_pool + at, from.key[0], from.key[1], from.key[2], from.key[3]);
-                load_4k(to + 8192 + s * 4096, a.v_pool + at, from.value, from.value, from.value, from.value);
+                load_4k<true>(to + s * 4096, a.k_pool + at, from.key[0], from.key[1], from.key[2], from.key[3]);
+                load_4k<true>(to + 8192 + s * 4096, a.v_pool + at, from.value, from.value, from.value, from.value);
             }
         };
 
@@ -556,10 +557,10 @@ __global__ __launch_bounds__(256, 2) void attend_many_kernel(AttendArgs a)
     };
     const auto place = [&](int phys) { return ((int64_t)__builtin_amdgcn_readfirstlane(phys) * H + h) * (B * kHeadDim) + (B == 32 ? (wave & 1) * 2048 : 0); };
     const auto fetch_keys = [&](int phys, int stage) {
-        load_4k(to + (uint32_t)stage * 16384, a.k_pool + place(phys), from.key[0], from.key[1], from.key[2], from.key[3]);
+        load_4k<false>(to + (uint32_t)stage * 16384, a.k_pool + place(phys), from.key[0], from.key[1], from.key[2], from.key[3]);
     };
     const auto fetch_values = [&](int phys, int stage) {
-        load_4k(to + 32768 + (uint32_t)stage * 16384, a.v_pool + place(phys), from.value, from.value, from.value, from.value);
+        load_4k<false>(to + 32768 + (uint32_t)stage * 16384, a.v_pool + place(phys), from.value, from.value, from.value, from.value);
     };
     // Physical pages by the 64, one a lane: a window of the table (or list) is asked for a window ahead, and what a tile needs of it is read from a lane.
     // (A scalar load a tile would be waited for with the LDS reads, which count with it.)

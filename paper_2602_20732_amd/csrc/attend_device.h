@@ -254,19 +254,25 @@ __device__ __forceinline__ void merge_parts(const AttendArgs& a, const Span& spa
 // Loads that write LDS themselves: no registers hold what is on its way, so that tiles can be asked for far ahead.  One instruction moves 1 KB, a lane
 // 16 bytes to the lane's place behind a common base; what a lane reads is its own choice, and that is how rows are swizzled.  The compiler does not
 // know of these loads: whoever reads what they bring waits for them (loads_left) and whoever overwrites what was read waits for the reads (reads_done).
-// A quarter of 4 KB from `base` (the same in every lane) + `at` and 1 KB each further on, to LDS bytes [lds, lds + 4096).
+// A quarter of 4 KB from `base` (the same in every lane) + `at` and 1 KB each further on, to LDS bytes [lds, lds + 4096).  kOnce: what nobody reads again is
+// not kept in the caches.
+#define CHESS_LOAD_4K(hint)                                  \
+    asm volatile("s_mov_b32 m0, %0\n\t"                      \
+                 "s_nop 0\n\t"                               \
+                 "global_load_lds_dwordx4 %2, %1" hint "\n\t" \
+                 "global_load_lds_dwordx4 %3, %1 offset:1024" hint "\n\t" \
+                 "global_load_lds_dwordx4 %4, %1 offset:2048" hint "\n\t" \
+                 "global_load_lds_dwordx4 %5, %1 offset:3072" hint \
+                 :                                           \
+                 : "s"(lds), "s"(base), "v"(at0), "v"(at1), "v"(at2), "v"(at3) \
+                 : "memory")
+template <bool kOnce>
 __device__ __forceinline__ void load_4k(uint32_t lds, const void* base, uint32_t at0, uint32_t at1, uint32_t at2, uint32_t at3)
 {
-    asm volatile("s_mov_b32 m0, %0\n\t"
-                 "s_nop 0\n\t"
-                 "global_load_lds_dwordx4 %2, %1\n\t"
-                 "global_load_lds_dwordx4 %3, %1 offset:1024\n\t"
-                 "global_load_lds_dwordx4 %4, %1 offset:2048\n\t"
-                 "global_load_lds_dwordx4 %5, %1 offset:3072"
-                 :
-                 : "s"(lds), "s"(base), "v"(at0), "v"(at1), "v"(at2), "v"(at3)
-                 : "memory");
+    if constexpr (kOnce) CHESS_LOAD_4K(" nt");
+    else CHESS_LOAD_4K("");
 }
+#undef CHESS_LOAD_4K
 template <int kLeft>
 __device__ __forceinline__ void loads_left()
 {

@@ -461,7 +461,7 @@ struct AttendArgs {
     AttendUnit* units;               // [blocks_most + extra_most]
     int32_t* n_units;
     int32_t* counters;               // [blocks_most][H_kv]
-    int block_rows, blocks_most, extra_most, parts_most;
+    int blocks_most, extra_most, parts_most;
 };
 // How a call is cut.  rows: of a workgroup (32, 64: few; 128: many); blocks, extra: most blocks of 128 rows, most units beyond one a block; parts: most
 // partials of `rows` rows.
