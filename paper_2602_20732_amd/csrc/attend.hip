@@ -397,9 +397,9 @@ __device__ __forceinline__ Keys keys_of_block(const AttendArgs& a, const Span& s
 template <int B>
 __global__ __launch_bounds__(kPlanThreads) void plan_kernel(AttendArgs a)
 {
-    constexpr int kWaves = kPlanThreads / 64, kTry = 16;
+    constexpr int kWaves = kPlanThreads / 64, kTry = 16, kEighths = 8;
     extern __shared__ int upto[];                     // [batch]: blocks of the sequences up to this one
-    __shared__ int of_wave[3][kWaves], most_of_wave[kWaves], units_of_wave[kTry][kWaves];
+    __shared__ int of_wave[3][kWaves], most_of_wave[kWaves], units_of_wave[kTry][kWaves], eighths_of_wave[kEighths * kWaves];
     __shared__ float tiles_of_wave[kWaves];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     // running sums over all threads' numbers, and the whole sums
@@ -491,24 +491,46 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(AttendArgs a)
 #pragma unroll
     for (int by = 32; by > 0; by /= 2) least = fminf(least, __shfl_xor(least, by));
     const int len = lane_of(len_y, __builtin_ctzll(__ballot(cost <= 1.03f * least)));       // (the longest of those that are as good)
-    // whole lengths first, then what is left of the blocks
-    int whole_before = 0, rest_before = 0, parts_before = 0;
+    // Whole lengths first, then what is left of the blocks by eighths of a length, the longest first, so that the last units to begin are short ones.  A wave
+    // counts its blocks' by the lanes that have one; then where each wave's of each eighth begin.
+    const auto eighth = [&](int i, int rest) { return i < n_blocks && rest > 0 ? 7 - min(8 * rest / len, 7) : kEighths; };
+    int whole_before = 0, rest_before = 0, parts_before = 0, of_eighth = 0;               // (lane: eighth)
     for (int i0 = 0; i0 < n_blocks; i0 += kPlanThreads) {
-        const int i = i0 + (int)threadIdx.x;
-        int v[3] = {i < n_blocks ? a.blocks[i].w / len : 0, 0, 0}, all[3];
+        const int i = i0 + (int)threadIdx.x, n = i < n_blocks ? a.blocks[i].w : 0;
+        int v[3] = {n / len, 0, 0}, all[3];
         sums_before(v, all);
         rest_before += all[0];
+        const int own = eighth(i, n % len);
+#pragma unroll
+        for (int c = 0; c < kEighths; ++c) {
+            const int n_own = __popcll(__ballot(own == c));
+            if (lane == c) of_eighth += n_own;
+        }
+    }
+    if (lane < kEighths) eighths_of_wave[lane * kWaves + wave] = of_eighth;
+    __syncthreads();
+    {
+        const int e0 = eighths_of_wave[2 * lane], e1 = eighths_of_wave[2 * lane + 1], e = lanes_upto(e0 + e1);
+        const int mine = min(lane, kEighths - 1) * kWaves + wave;      // where this wave's begin
+        of_eighth = rest_before + __shfl(e - e0 - e1, mine >> 1) + ((mine & 1) != 0 ? __shfl(e0, mine >> 1) : 0);
+        rest_before += lane_of(e, 63);
     }
     for (int i0 = 0; i0 < n_blocks; i0 += kPlanThreads) {
         const int i = i0 + (int)threadIdx.x;
         const int4 blk = i < n_blocks ? a.blocks[i] : make_int4(0, 0, 0, 0);
         const int whole = blk.w / len, rest = blk.w - whole * len, n = whole + (rest > 0 ? 1 : 0);
-        int v[3] = {whole, rest > 0 ? 1 : 0, n > 1 ? n : 0}, all[3];
+        int v[3] = {whole, n > 1 ? n : 0, 0}, all[3];
         sums_before(v, all);
-        const int at = whole_before + v[0], at_rest = rest_before + v[1], part0 = parts_before + v[2];
+        const int at = whole_before + v[0], part0 = parts_before + v[1], own = eighth(i, rest);
         whole_before += all[0];
-        rest_before += all[1];
-        parts_before += all[2];
+        parts_before += all[1];
+        int at_rest = 0;
+#pragma unroll
+        for (int c = 0; c < kEighths; ++c) {
+            const unsigned long long those = __ballot(own == c);
+            if (own == c) at_rest = lane_of(of_eighth, c) + (int)__builtin_amdgcn_mbcnt_hi((unsigned)(those >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)those, 0));
+            if (lane == c) of_eighth += __popcll(those);
+        }
         for (int s = 0; s < n; ++s) {
             AttendUnit u;
             u.b = blk.x; u.block = blk.y;
