@@ -610,7 +610,7 @@ class Chess:
         n = self._need_attend(q, token_start, k_pool, v_pool, block_table, seq_lens, out, workspace, scratch, scores, batch, dev)
         if n == 0:
             return
-        self._check(self.lib.chess_dense_attend(self._h, None if scores is None else scores._ref, q.data_ptr(), n, token_start.data_ptr(), max_new,
+        self._check(self.lib.chess_dense_attend(self._h, None if scores is None else scores._ref, q.data_ptr(), n, token_start.data_ptr(), min(max_new, n),
                                                 k_pool.data_ptr(), v_pool.data_ptr(), block_table.data_ptr(), seq_lens.data_ptr(), batch,
                                                 out.data_ptr(), workspace.data_ptr(), scratch.data_ptr(), scratch.numel(),
                                                 torch._C._cuda_getCurrentRawStream(dev)))
@@ -623,7 +623,7 @@ class Chess:
         _need(n_selected, "n_selected", _INT, batch * self.cfg.n_kv_heads, dev)
         if n == 0:
             return
-        self._check(self.lib.chess_sparse_attend(self._h, None if scores is None else scores._ref, q.data_ptr(), n, token_start.data_ptr(), max_new,
+        self._check(self.lib.chess_sparse_attend(self._h, None if scores is None else scores._ref, q.data_ptr(), n, token_start.data_ptr(), min(max_new, n),
                                                  k_pool.data_ptr(), v_pool.data_ptr(), block_table.data_ptr(), seq_lens.data_ptr(),
                                                  page_ids.data_ptr(), n_selected.data_ptr(), batch, out.data_ptr(), workspace.data_ptr(),
                                                  scratch.data_ptr(), scratch.numel(), torch._C._cuda_getCurrentRawStream(dev)))

@@ -380,7 +380,7 @@ __device__ __forceinline__ Keys keys_of_block(const AttendArgs& a, const Span& s
     const int G = a.group, row_end = min((block + 1) * kBlockRows, s.n_new * G) - 1;
     const int i0 = (int)((unsigned)(block * kBlockRows) / (unsigned)G), i1 = (int)((unsigned)row_end / (unsigned)G);
     const int p0 = s.len - s.n_new + i0, p1 = s.len - s.n_new + i1;
-    Keys k{a.window > 0 ? max(p0 - a.window + 1, 0) : 0, min(a.prefix_lens != nullptr ? max(p1, a.prefix_lens[b] - 1) : p1, s.len - 1)};
+    Keys k{a.window > 0 ? max(p0 - a.window + 1, 0) : 0, min(a.prefix_lens != nullptr ? max(p1, max(a.prefix_lens[b], 1) - 1) : p1, s.len - 1)};
     if (a.first_keys != nullptr) {
         int first = INT32_MAX;
 #pragma unroll 8

@@ -81,7 +81,7 @@ __device__ __forceinline__ RowView view_of(const AttendArgs& a, const Span& s, i
     v.slope = a.slopes != nullptr ? a.slopes[h * G + g] * kLog2e : 0.f;
     v.lo = a.first_keys != nullptr ? max(a.first_keys[s.start + i], 0) : 0;
     if (a.window > 0) v.lo = max(v.lo, v.p - a.window + 1);
-    v.hi = a.prefix_lens != nullptr ? max(v.p, a.prefix_lens[b] - 1) : v.p;
+    v.hi = a.prefix_lens != nullptr ? max(v.p, max(a.prefix_lens[b], 1) - 1) : v.p;
     v.hi = min(v.hi, s.len - 1);
     if (!v.there || v.p < 0) {
         v.lo = INT32_MAX;

@@ -8,6 +8,7 @@ import pytest
 import torch
 
 import paper_2602_20732_amd as pk
+import step_reference as ref
 from attend_common import Batch, bf16, ints
 
 pytestmark = pytest.mark.gpu
@@ -242,3 +243,77 @@ def test_refusals():
     for bad in ((0, 1, 1), (1, 0, 1), (1, 1, 0), (1, 1, 2)):
         assert b.lib.lib.chess_attend_scratch_bytes(b.lib._h, *bad, ctypes.byref(n)) == -1
     torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("new", [3, 40])
+def test_lists_of_many_sequences(new):
+    rng = np.random.default_rng(1)
+    Batch(16, rng.integers(0, 200, 90), rng.integers(0, new + 1, 90), 4, 1, listed=5).check()
+
+
+@pytest.mark.parametrize("new", [7, 160])
+def test_lists_with_prefixes_and_windows(new):
+    Batch(17, [150, 0, 61], [new, new, 2], 8, 2, listed=7, prefix=[100, new, 0], window=90, cap=25.0).check()
+
+
+@pytest.mark.parametrize("new", [5, 90])
+def test_prefixes_that_are_no_number_of_tokens(new):
+    """A negative one is none, however low."""
+    Batch(18, [30, 0, 77], [new] * 3, 8, 2, prefix=[-(2 ** 31), -1, -(2 ** 31) + 1]).check()
+
+
+@pytest.mark.parametrize("new", [5, 90])
+def test_starts_out_of_order(new):
+    """Sequences whose starts fall, or name rows that are not there, have no new tokens; two may share rows' queries (of outputs, either's)."""
+    b = Batch(19, [30, 50, 20], [new] * 3, 8, 2)
+    args = b.cuda()
+    for starts in ([0, new, 0, new], [-1, new, 2 * new, 3 * new + 1], [2 ** 31 - 1, -(2 ** 31), 2 ** 31 - 1, 5], [0, 3 * new + 1, 0, 0]):
+        args["out"].fill_(5.0)
+        out = b.launch({**args, "token_start": ints(starts)})
+        torch.cuda.synchronize()
+        rows = torch.zeros(len(out), dtype=torch.bool, device="cuda")
+        for i in range(3):
+            if 0 <= starts[i] <= starts[i + 1] <= b.rows:
+                rows[starts[i]:starts[i + 1]] = True
+        assert ((out != 5).flatten(1).any(1) == rows).all(), starts
+
+
+@pytest.mark.parametrize("B", [16, 32])
+@pytest.mark.parametrize("H,length,new", [(32, 40000, 3), (2, 40000, 80)])
+def test_long_contexts_of_few_pages(H, length, new, B):
+    """More pages a workgroup than it looks up at a time; the physical ones are few and repeat, the reference is formed in 64 bits on the device."""
+    G, n_phys, width = 2, 60, -(-length // B)
+    gen = torch.Generator("cuda")
+    gen.manual_seed(B)
+    normal = lambda *s: torch.empty(s, dtype=torch.bfloat16, device="cuda").normal_(generator=gen)  # noqa: E731
+    k, v, q = normal(n_phys, H, B, 128), normal(n_phys, H, 128, B), normal(new, H * G, 128)
+    table = torch.randint(0, n_phys, (1, width), dtype=torch.int32, device="cuda", generator=gen)
+    lib = pk.Chess(pk.Config(H * G, H, B, 1, width, width))
+    out = torch.zeros_like(q)
+    lib.dense_attend(q, ints([0, new]), new, k, v, table, ints([length]), out, lib.new_workspace(), lib.new_attend_scratch(new, new, 1))
+    at, t = table[0].long(), torch.arange(length, device="cuda")
+    p = torch.arange(length - new, length, device="cuda").repeat_interleave(G)
+    for h in range(H):
+        keys, values = k[at, h].reshape(-1, 128)[:length].double(), v[at, h].transpose(1, 2).reshape(-1, 128)[:length].double()
+        rows = q[:, h * G:h * G + G].reshape(-1, 128).double()
+        s = rows @ keys.T / 128 ** 0.5
+        e = 2.0 ** -24 * (130 / 128 ** 0.5 * (rows.abs() @ keys.abs().T).amax(1) + 3 * s.abs().amax(1))
+        w = s.masked_fill(t[None] > p[:, None], -float("inf")).softmax(1)
+        want, size = w @ values, w @ values.abs()
+        step = ref.HALF_STEP if new * G > 64 else ref.HALF_STEP ** 2
+        want, size, e, got = (x.double().cpu().numpy() for x in (want, size, e[:, None], out[:, h * G:h * G + G].reshape(-1, 128)))
+        assert (np.abs(got - want) <= ref.attention_error(want, size, e, length, step)).all(), h
+
+
+def test_more_sequences_than_there_may_be():
+    n = 4097
+    lib = pk.Chess(pk.Config(2, 1, 16, n, 1, 1))
+    lens, out = ints([1] * n), torch.full((n, 2, 128), 5.0, dtype=torch.bfloat16, device="cuda")
+    pool = torch.ones((1, 1, 16, 128), dtype=torch.bfloat16, device="cuda")
+    args = dict(q=out.clone(), max_new=1, k_pool=pool, v_pool=pool.view(1, 1, 128, 16), out=out, workspace=lib.new_workspace(), scratch=lib.new_attend_scratch(n, n, n))
+    with pytest.raises(pk.ChessError):
+        lib.dense_attend(**args, token_start=ints(range(n + 1)), block_table=ints([[0]] * n), seq_lens=lens)
+    assert (out == 5).all()
+    lib.dense_attend(**{**args, "max_new": 2 ** 32}, token_start=ints(range(n)), block_table=ints([[0]] * (n - 1)), seq_lens=lens[:-1])
+    torch.cuda.synchronize()
+    assert (out[:-1] == 1).all() and (out[-1] == 5).all()
