@@ -383,8 +383,20 @@ __device__ __forceinline__ Keys keys_of_block(const AttendArgs& a, const Span& s
     Keys k{a.window > 0 ? max(p0 - a.window + 1, 0) : 0, min(a.prefix_lens != nullptr ? max(p1, max(a.prefix_lens[b], 1) - 1) : p1, s.len - 1)};
     if (a.first_keys != nullptr) {
         int first = INT32_MAX;
-#pragma unroll 8
-        for (int i = i0; i <= i1; ++i) first = min(first, a.first_keys[s.start + i]);
+        const int32_t* of_row = a.first_keys + s.start;
+        if (i1 - i0 < 3) {
+            for (int i = i0; i <= i1; ++i) first = min(first, of_row[i]);
+        } else {
+            for (int i = i0; i <= i1; i += 32) {      // (fours of them, asked for together: one by one they are most of the plan's time)
+                struct Four { int32_t first[4]; } four[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) __builtin_memcpy(&four[j], of_row + min(i + 4 * j, i1 - 3), sizeof(Four));
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) first = min(first, four[j].first[e]);
+            }
+        }
         k.first = max(k.first, first);
     }
     if (p1 < 0) k.last = -1;
@@ -431,6 +443,7 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(AttendArgs a)
     n_blocks = min(n_blocks, a.blocks_most);
     int most = 1;
     float tiles = 0.f;                                // (estimates only)
+    int4 own_block = make_int4(0, 0, 0, 0);           // of the first kPlanThreads: not read again
     for (int i = threadIdx.x; i < n_blocks; i += kPlanThreads) {
         int lo = 0, hi = a.batch - 1;                 // the first sequence whose blocks go beyond i
         while (lo < hi) {
@@ -444,6 +457,7 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(AttendArgs a)
         const bool any = k.last >= k.first;
         const int first = any ? k.first / 64 : 0, n = a.page_ids != nullptr ? 1 : any ? k.last / 64 - first + 1 : 1;
         a.blocks[i] = make_int4(lo, block, first, n);
+        if (i < kPlanThreads) own_block = make_int4(lo, block, first, n);
         most = max(most, n);
         tiles += (float)n;
         for (int h = 0; h < a.n_kv_heads; ++h) a.counters[(int64_t)i * a.n_kv_heads + h] = 0;
@@ -462,11 +476,12 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(AttendArgs a)
         most = max(most, most_of_wave[w]);
         tiles += tiles_of_wave[w];
     }
+    const auto block_at = [&](int i) { return i < kPlanThreads ? own_block : a.blocks[i]; };      // (a thread's own)
     // units of each length tried
     const auto length = [&](int y) { return max((most + y) / (y + 1), 1); };
     int units[kTry] = {};
     for (int i = threadIdx.x; i < n_blocks; i += kPlanThreads) {
-        const int n = a.blocks[i].w;
+        const int n = block_at(i).w;
 #pragma unroll
         for (int y = 0; y < kTry; ++y) units[y] += (n + length(y) - 1) / length(y);
     }
@@ -496,7 +511,7 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(AttendArgs a)
     const auto eighth = [&](int i, int rest) { return i < n_blocks && rest > 0 ? 7 - min(8 * rest / len, 7) : kEighths; };
     int whole_before = 0, rest_before = 0, parts_before = 0, of_eighth = 0;               // (lane: eighth)
     for (int i0 = 0; i0 < n_blocks; i0 += kPlanThreads) {
-        const int i = i0 + (int)threadIdx.x, n = i < n_blocks ? a.blocks[i].w : 0;
+        const int i = i0 + (int)threadIdx.x, n = i < n_blocks ? block_at(i).w : 0;
         int v[3] = {n / len, 0, 0}, all[3];
         sums_before(v, all);
         rest_before += all[0];
@@ -517,7 +532,7 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(AttendArgs a)
     }
     for (int i0 = 0; i0 < n_blocks; i0 += kPlanThreads) {
         const int i = i0 + (int)threadIdx.x;
-        const int4 blk = i < n_blocks ? a.blocks[i] : make_int4(0, 0, 0, 0);
+        const int4 blk = i < n_blocks ? block_at(i) : make_int4(0, 0, 0, 0);
         const int whole = blk.w / len, rest = blk.w - whole * len, n = whole + (rest > 0 ? 1 : 0);
         int v[3] = {whole, n > 1 ? n : 0, 0}, all[3];
         sums_before(v, all);
