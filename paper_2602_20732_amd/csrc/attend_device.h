@@ -208,45 +208,72 @@ __device__ __forceinline__ void add_not_finite(f32x16 (&o)[4], const Odd& odd)
         }
 }
 
-// What the last of n_parts workgroups with partials of a block of kRowsOf rows to arrive does: out = sum_s acc_s 2^(m_s - M) / sum_s l_s 2^(m_s - M),
-// always in the same order; at(s): where partial s is.  A thread has four dims of a row; eight partials are asked for at a time.
-template <int kRowsOf, int kThreads, class At>
-__device__ __forceinline__ void merge_parts(const AttendArgs& a, const Span& span, int h, int row0, int n_rows, int n_parts, At part_at)
+// Where a partial's four sums of row r from dim on are, of a block's rows: 32 rows' in the order in which a wave's lanes have them (dims 32 d + 8 i + 4 half, row
+// r % 32), so that the lanes write side by side.
+__device__ __forceinline__ int64_t part_at(int64_t part, int n_rows, int r, int dim)
 {
-    constexpr int kChunk = 8;
-    for (int i = threadIdx.x; i < kRowsOf * 32; i += kThreads) {
-        const int r = i >> 5, dim = 4 * (i & 31);
-        if (row0 + r >= n_rows) break;
-        float M = kNegBig, l = 0.f, x[4] = {};
-        for (int s0 = 0; s0 < n_parts; s0 += kChunk) {
-            uint64_t ml[kChunk], v[kChunk][2];
+    return part * n_rows * kHeadDim + (int64_t)(r >> 5) * (32 * kHeadDim) + (dim >> 3) * 256 + (dim >> 2 & 1) * 128 + (r & 31) * 4;
+}
+
+// What the last of n_parts workgroups with partials of a block of kRowsOf rows to arrive does: out = sum_s acc_s 2^(m_s - M) / sum_s l_s 2^(m_s - M),
+// always in the same order; number(s): which partial s is.  A thread has four dims of each of kPieces rows; kChunk partials of them are asked for at a time.
+template <int kRowsOf, int kThreads, int kPieces, int kChunk, class Number>
+__device__ __forceinline__ void merge_parts(const AttendArgs& a, const Span& span, int h, int row0, int n_rows, int n_parts, Number number)
+{
+    static_assert(kRowsOf * 32 % (kThreads * kPieces) == 0);
+    for (int i = threadIdx.x; i < kRowsOf * 32; i += kThreads * kPieces) {
+        int r[kPieces], dim[kPieces];
+        float M[kPieces], l[kPieces], x[kPieces][4];
+        bool any = false;
 #pragma unroll
-            for (int s = 0; s < kChunk; ++s) {
-                const int64_t part = part_at(min(s0 + s, n_parts - 1)) * kRowsOf + r;
-                ml[s] = observe_u64(reinterpret_cast<const uint64_t*>(a.part_ml) + part);
-                const uint64_t* at = reinterpret_cast<const uint64_t*>(a.part_acc + part * kHeadDim + dim);
-                v[s][0] = observe_u64(at);
-                v[s][1] = observe_u64(at + 1);
-            }
-            float top = M;
-#pragma unroll
-            for (int s = 0; s < kChunk; ++s) top = fmaxf(top, __builtin_bit_cast(float2, ml[s]).x);   // (the last one again changes nothing)
-            const float keep = __builtin_amdgcn_exp2f(M - top);
-            M = top;
-            l *= keep;
-#pragma unroll
-            for (int d = 0; d < 4; ++d) x[d] *= keep;
-#pragma unroll
-            for (int s = 0; s < kChunk; ++s)
-                if (s0 + s < n_parts) {
-                    const float2 one = __builtin_bit_cast(float2, ml[s]), lo = __builtin_bit_cast(float2, v[s][0]), hi = __builtin_bit_cast(float2, v[s][1]);
-                    const float by = __builtin_amdgcn_exp2f(one.x - M);
-                    l += one.y * by;
-                    x[0] += lo.x * by; x[1] += lo.y * by; x[2] += hi.x * by; x[3] += hi.y * by;
-                }
+        for (int y = 0; y < kPieces; ++y) {
+            const int piece = i + y * kThreads;       // a wave's: 32 rows, two fours of dims
+            r[y] = (piece >> 10) * 32 + (piece & 31);
+            dim[y] = 4 * (piece >> 5 & 31);
+            any |= row0 + r[y] < n_rows;
+            M[y] = kNegBig;
+            l[y] = x[y][0] = x[y][1] = x[y][2] = x[y][3] = 0.f;
         }
-        const float inv = l == 0.f ? 0.f : 1.f / l;
-        *reinterpret_cast<uint2*>(a.out + row_at(a, span, h, row0 + r) * kHeadDim + dim) = make_uint2(two_bf16(x[0] * inv, x[1] * inv), two_bf16(x[2] * inv, x[3] * inv));
+        if (!any) continue;
+        for (int s0 = 0; s0 < n_parts; s0 += kChunk) {
+            uint64_t ml[kPieces][kChunk], v[kPieces][kChunk][2];
+#pragma unroll
+            for (int y = 0; y < kPieces; ++y)
+#pragma unroll
+                for (int s = 0; s < kChunk; ++s) {
+                    const int64_t part = number(min(s0 + s, n_parts - 1));
+                    ml[y][s] = observe_u64(reinterpret_cast<const uint64_t*>(a.part_ml) + part * kRowsOf + r[y]);
+                    const uint64_t* at = reinterpret_cast<const uint64_t*>(a.part_acc + part_at(part, kRowsOf, r[y], dim[y]));
+                    v[y][s][0] = observe_u64(at);
+                    v[y][s][1] = observe_u64(at + 1);
+                }
+#pragma unroll
+            for (int y = 0; y < kPieces; ++y) {
+                float top = M[y];
+#pragma unroll
+                for (int s = 0; s < kChunk; ++s) top = fmaxf(top, __builtin_bit_cast(float2, ml[y][s]).x);   // (the last one again changes nothing)
+                const float keep = __builtin_amdgcn_exp2f(M[y] - top);
+                M[y] = top;
+                l[y] *= keep;
+#pragma unroll
+                for (int d = 0; d < 4; ++d) x[y][d] *= keep;
+#pragma unroll
+                for (int s = 0; s < kChunk; ++s)
+                    if (s0 + s < n_parts) {
+                        const float2 one = __builtin_bit_cast(float2, ml[y][s]), lo = __builtin_bit_cast(float2, v[y][s][0]), hi = __builtin_bit_cast(float2, v[y][s][1]);
+                        const float by = __builtin_amdgcn_exp2f(one.x - M[y]);
+                        l[y] += one.y * by;
+                        x[y][0] += lo.x * by; x[y][1] += lo.y * by; x[y][2] += hi.x * by; x[y][3] += hi.y * by;
+                    }
+            }
+        }
+#pragma unroll
+        for (int y = 0; y < kPieces; ++y) {
+            const float inv = l[y] == 0.f ? 0.f : 1.f / l[y];
+            if (row0 + r[y] < n_rows)
+                *reinterpret_cast<uint2*>(a.out + row_at(a, span, h, row0 + r[y]) * kHeadDim + dim[y]) =
+                    make_uint2(two_bf16(x[y][0] * inv, x[y][1] * inv), two_bf16(x[y][2] * inv, x[y][3] * inv));
+        }
     }
 }
 
