@@ -432,7 +432,8 @@ int chess_quant_dense_decode(chess_ctx* ctx, const void* q, const void* k_pool, 
  * chess_trim_pages takes back the pages of the others.  token_start: int32 [batch + 1] as chess_map_tokens writes it; the rows of sequence b are
  * token_start[b] .. token_start[b + 1] - 1, in the order of their positions.  A sequence for which it names rows that are not there has none.
  * All these calls: CHESS_EINVAL on null or misaligned pointers (16 bytes for rows, pools and workspaces), sizes outside the configuration, or when
- * the context's device is not the current one; CHESS_ENOTSUP for more work than one launch holds.
+ * the context's device is not the current one; CHESS_ENOTSUP for more work than one launch holds (attention and trimming: batch above 4096; verification:
+ * above 65535).  No output may overlap an input or another output but where it is said.
  */
 
 /* How queries and keys are normed and turned.  A host struct; the pointers are device pointers. */
@@ -489,6 +490,7 @@ int chess_attend_scratch_bytes(const chess_ctx* ctx, int32_t n_rows, int32_t max
  * sequence with t <= p or t < prefix_lens[b], t >= first_keys[row], t > p - window; a row that sees no key is 0.  Keys that a row does not see do not
  * touch it, whatever they or their values are.  bf16 in and out; scores, softmax and sums in fp32 (weights are rounded to bf16 where the
  * keys are shared by more rows than a few: see attend.hip), distances p - t in fp32.  Scores may have any size that fp32 holds.
+ * Block table entries behind a sequence's pages are not used.  A block table entry of a page that a sequence has must be a page of the pools.
  * workspace: as elsewhere (arrival counters); scratch: chess_attend_scratch_bytes at least, 256-byte aligned.  The same batch gives the same bits on every call.
  */
 int chess_dense_attend(chess_ctx* ctx, const chess_scores* scores, const void* q, int32_t n_rows, const int32_t* token_start, int32_t max_new,

@@ -344,16 +344,16 @@ __global__ __launch_bounds__(256, 1) void attend_few_kernel(AttendArgs a)
                     if (row[y].there)
                         *reinterpret_cast<uint2*>(a.out + row[y].at * kHeadDim + dim) = make_uint2(two_bf16(x[0] * inv, x[1] * inv), two_bf16(x[2] * inv, x[3] * inv));
                 } else {
-                    uint64_t* to = reinterpret_cast<uint64_t*>(a.part_acc + part_at(part_own, 32 * kRows, 32 * y + col, dim));
+                    uint64_t* to = reinterpret_cast<uint64_t*>(a.part_acc + part_at<false>(part_own, 32 * kRows, 32 * y + col, dim));
                     publish_u64(to, __builtin_bit_cast(uint64_t, make_float2(x[0], x[1])));
-                    publish_u64(to + 1, __builtin_bit_cast(uint64_t, make_float2(x[2], x[3])));
+                    publish_u64(to + kOtherPair<false>, __builtin_bit_cast(uint64_t, make_float2(x[2], x[3])));
                 }
             }
             if (!whole && wave == 0 && half == 0) publish_u64(reinterpret_cast<uint64_t*>(a.part_ml) + part, __builtin_bit_cast(uint64_t, make_float2(top, sum)));
             __syncthreads();
         }
         if (!whole && arrive_last(a.arrivals + ((int64_t)b * H + h) * kArrivalStride, n_parts, &flag))
-            merge_parts<32 * kRows, 256, 2, 4>(a, span, h, 0, n_rows, n_parts, [&](int s) { return part0 + 2 * s + (s == 0 ? 1 : 0); });
+            merge_parts<32 * kRows, 256, 2, 4, false>(a, span, h, 0, n_rows, n_parts, [&](int s) { return part0 + 2 * s + (s == 0 ? 1 : 0); });
         line = line_end;
     }
 }
@@ -844,15 +844,15 @@ __global__ __launch_bounds__(256, 2) void attend_many_kernel(AttendArgs a)
         for (int d = 0; d < 4; ++d)
 #pragma unroll
             for (int i = 0; i < 16; i += 4) {
-                uint64_t* at = reinterpret_cast<uint64_t*>(a.part_acc + part_at(part, kBlockRows, 32 * wave + col, 32 * d + 2 * i + 4 * half));
+                uint64_t* at = reinterpret_cast<uint64_t*>(a.part_acc + part_at<true>(part, kBlockRows, 32 * wave + col, 32 * d + 2 * i + 4 * half));
                 publish_u64(at, __builtin_bit_cast(uint64_t, make_float2(o[d][i], o[d][i + 1])));
-                publish_u64(at + 1, __builtin_bit_cast(uint64_t, make_float2(o[d][i + 2], o[d][i + 3])));
+                publish_u64(at + kOtherPair<true>, __builtin_bit_cast(uint64_t, make_float2(o[d][i + 2], o[d][i + 3])));
             }
         if (half == 0) publish_u64(reinterpret_cast<uint64_t*>(a.part_ml) + part * kBlockRows + 32 * wave + col, __builtin_bit_cast(uint64_t, make_float2(m, l)));
     }
     if (!arrive_last(a.counters + (int64_t)of_unit(7) * H + h, n_parts, &flag)) return;
     const int64_t part0 = (int64_t)of_unit(6) * H + h;
-    merge_parts<kBlockRows, 256, 4, 4>(a, span, h, block * kBlockRows, n_rows, n_parts, [&](int s) { return part0 + (int64_t)s * H; });
+    merge_parts<kBlockRows, 256, 4, 4, true>(a, span, h, block * kBlockRows, n_rows, n_parts, [&](int s) { return part0 + (int64_t)s * H; });
 }
 
 // ---- launch -----------------------------------------------------------------------------------------------------------------------------------

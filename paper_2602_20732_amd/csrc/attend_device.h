@@ -208,16 +208,20 @@ __device__ __forceinline__ void add_not_finite(f32x16 (&o)[4], const Odd& odd)
         }
 }
 
-// Where a partial's four sums of row r from dim on are, of a block's rows: 32 rows' in the order in which a wave's lanes have them (dims 32 d + 8 i + 4 half, row
-// r % 32), so that the lanes write side by side.
+// Where the first two of a partial's four sums of row r from dim on are, of a block's rows, and how many pairs of numbers further on the other two: 32 rows' in
+// the order in which a wave's lanes have them (dims 32 d + 8 i + 4 half, row r % 32).  kLines: pairs of all lanes side by side, so that a store writes whole lines
+// (a chunk of 1531 tokens, with 100 MB of partials: 815 -> 807 us); a lane's four together otherwise (16 sequences of drafts over every page 376 -> 368).
+template <bool kLines>
+constexpr int kOtherPair = kLines ? 64 : 1;
+template <bool kLines>
 __device__ __forceinline__ int64_t part_at(int64_t part, int n_rows, int r, int dim)
 {
-    return part * n_rows * kHeadDim + (int64_t)(r >> 5) * (32 * kHeadDim) + (dim >> 3) * 256 + (dim >> 2 & 1) * 128 + (r & 31) * 4;
+    return part * n_rows * kHeadDim + (int64_t)(r >> 5) * (32 * kHeadDim) + (dim >> 3) * 256 + ((dim >> 2 & 1) * 32 + (r & 31)) * (kLines ? 2 : 4);
 }
 
 // What the last of n_parts workgroups with partials of a block of kRowsOf rows to arrive does: out = sum_s acc_s 2^(m_s - M) / sum_s l_s 2^(m_s - M),
 // always in the same order; number(s): which partial s is.  A thread has four dims of each of kPieces rows; kChunk partials of them are asked for at a time.
-template <int kRowsOf, int kThreads, int kPieces, int kChunk, class Number>
+template <int kRowsOf, int kThreads, int kPieces, int kChunk, bool kLines, class Number>
 __device__ __forceinline__ void merge_parts(const AttendArgs& a, const Span& span, int h, int row0, int n_rows, int n_parts, Number number)
 {
     static_assert(kRowsOf * 32 % (kThreads * kPieces) == 0);
@@ -243,9 +247,9 @@ __device__ __forceinline__ void merge_parts(const AttendArgs& a, const Span& spa
                 for (int s = 0; s < kChunk; ++s) {
                     const int64_t part = number(min(s0 + s, n_parts - 1));
                     ml[y][s] = observe_u64(reinterpret_cast<const uint64_t*>(a.part_ml) + part * kRowsOf + r[y]);
-                    const uint64_t* at = reinterpret_cast<const uint64_t*>(a.part_acc + part_at(part, kRowsOf, r[y], dim[y]));
+                    const uint64_t* at = reinterpret_cast<const uint64_t*>(a.part_acc + part_at<kLines>(part, kRowsOf, r[y], dim[y]));
                     v[y][s][0] = observe_u64(at);
-                    v[y][s][1] = observe_u64(at + 1);
+                    v[y][s][1] = observe_u64(at + kOtherPair<kLines>);
                 }
 #pragma unroll
             for (int y = 0; y < kPieces; ++y) {
@@ -287,9 +291,9 @@ __device__ __forceinline__ void merge_parts(const AttendArgs& a, const Span& spa
     asm volatile("s_mov_b32 m0, %0\n\t"                      \
                  "s_nop 0\n\t"                               \
                  "global_load_lds_dwordx4 %2, %1" hint "\n\t" \
-                 "global_load_lds_dwordx4 %3, %1 offset:1024" hint "\n\t" \
-                 "global_load_lds_dwordx4 %4, %1 offset:2048" hint "\n\t" \
-                 "global_load_lds_dwordx4 %5, %1 offset:3072" hint \
+                 "global_load_lds_dwordx4 %3, %1 offset:0x400" hint "\n\t" \
+                 "global_load_lds_dwordx4 %4, %1 offset:0x800" hint "\n\t" \
+                 "global_load_lds_dwordx4 %5, %1 offset:0xc00" hint \
                  :                                           \
                  : "s"(lds), "s"(base), "v"(at0), "v"(at1), "v"(at2), "v"(at3) \
                  : "memory")
