@@ -193,7 +193,7 @@ __global__ __launch_bounds__(kPageThreads) void release_kernel(ReleaseArgs a)
     if (threadIdx.x == 0) *a.n_left = n_free + total;
 }
 
-// The pages behind what a sequence keeps of its tokens, as release_kernel.
+// The pages behind what a sequence keeps of its tokens, as release_kernel.  Bound: its chain of round trips: one sequence 1.8 us, 32 2.7, 128 4.4.
 template <int B>
 __global__ __launch_bounds__(kPageThreads) void trim_kernel(TrimArgs a)
 {

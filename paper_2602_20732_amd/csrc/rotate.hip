@@ -10,7 +10,8 @@
 // lie side by side).  A workgroup has an entry of the write list (the new tokens of one page), a wave takes a token at a time, works out its
 // angles once and turns all its heads with them; where there are few tokens, workgroups share their heads.  Values go into their pages (token-minor) as in
 // quant_store.hip: a lane reads the same dims of 16 tokens, and has whole 32-byte rows to write.
-// Bound: HBM, read and written alike; for single tokens the chain entry -> position -> angle -> store.
+// Bound: HBM, read and written alike; for single tokens the chain entry -> position -> angle -> store.  Measured: 65531 tokens of 28 + 2 x 4 heads into pages of
+// 32 233 us, 24955 of 32 + 2 x 8 into pages of 16 121 us: 5.1 to 5.2 TB/s, what a copy reaches (4.9); 32 sequences of 5 drafts 5.6 us, one token 3.5.
 #include "attend_device.h"
 #include "quant_device.h"
 #include "split_rule.h"

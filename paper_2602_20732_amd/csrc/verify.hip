@@ -6,7 +6,8 @@
 // u q is exact in fp64, sums are fp64 over pieces of 1024 that do not depend on the launch, so the same row gives the same token in every batch.
 // Each workgroup finds the refused draft for itself (a gather a draft, a wave's ballot), then sums its pieces of the one row that counts;
 // the last of a sequence to arrive looks through the pieces' sums, and through the one piece that the token is in.
-// Bound: HBM (8 bytes a word of the vocabulary, of one row a sequence) behind the chain start -> token -> probabilities -> row.
+// Bound: HBM (8 bytes a word of the vocabulary, of one row a sequence) behind the chain start -> token -> probabilities -> row.  Measured, 151936 words: 128
+// sequences of 3 drafts 31.5 us, 4.9 TB/s; 32 sequences 13.5; one of 4 drafts 8.2.
 #include "chess_internal.h"
 #include "split_rule.h"
 
