@@ -459,7 +459,14 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(AttendArgs a)
         const Span s = span_by_lane(a, lo, B);
         const Keys k = keys_of_block(a, s, lo, block);
         const bool any = k.last >= k.first;
-        const int first = any ? k.first / 64 : 0, n = a.page_ids != nullptr ? 1 : any ? k.last / 64 - first + 1 : 1;
+        int first = any ? k.first / 64 : 0, n = any ? k.last / 64 - first + 1 : 1;
+        if (a.page_ids != nullptr) {                  // tiles of the longest list of its heads (those with shorter ones have units without tiles)
+            int longest = 0;
+#pragma unroll 8
+            for (int h = 0; h < a.n_kv_heads; ++h) longest = max(longest, a.n_selected[(int64_t)lo * a.n_kv_heads + h]);
+            first = 0;
+            n = any ? max((min(longest, a.max_sel) + 64 / B - 1) / (64 / B), 1) : 1;
+        }
         a.blocks[i] = make_int4(lo, block, first, n);
         if (i < kPlanThreads) own_block = make_int4(lo, block, first, n);
         most = max(most, n);
@@ -501,7 +508,9 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(AttendArgs a)
 #pragma unroll
         for (int w = 0; w < kWaves; ++w) n_units += units_of_wave[lane][w];
     const int len_y = length(lane), extra = n_units - n_blocks;
-    const float cut = extra > 0 ? 6.f : 0.f, size = (float)len_y + 5.f + cut, slots = (float)a.n_slots, of_heads = (float)(n_units * a.n_kv_heads);
+    const float cut = extra > 0 ? 6.f : 0.f, slots = (float)a.n_slots, of_heads = (float)(n_units * a.n_kv_heads);
+    // (a workgroup alone on its compute unit takes two thirds of the time for a tile: 32 sequences of 20 tokens over 27 tiles 80 us cut in halves, 68 whole)
+    const float size = (2.f * of_heads <= slots ? 0.65f : 1.f) * (float)len_y + 5.f + cut;
     // units as long as each other go in rounds, others into the gaps
     const float in_rounds = ceilf(of_heads / slots) * size, in_gaps = ((float)a.n_kv_heads * tiles + of_heads * (5.f + cut)) / slots + 0.5f * size;
     float cost = fmaxf(fminf(in_rounds, in_gaps), size);
@@ -581,10 +590,7 @@ __global__ __launch_bounds__(256, 2) void attend_many_kernel(AttendArgs a)
     const int32_t* table = a.block_table + (int64_t)b * a.max_pages;
     const int32_t* ids = kList ? a.page_ids + ((int64_t)b * H + h) * a.max_sel : nullptr;
     const int n_list = kList ? min(max(load_same(a.n_selected, (int64_t)b * H + h), 0), a.max_sel) : P;
-    if constexpr (kList) {
-        t = 0;
-        t_end = (n_list + PPT - 1) / PPT;
-    }
+    if constexpr (kList) t_end = min(t_end, (n_list + PPT - 1) / PPT);
     if (P == 0) t_end = 0;
     const int t_first = t;
 

@@ -317,3 +317,14 @@ def test_more_sequences_than_there_may_be():
     lib.dense_attend(**{**args, "max_new": 2 ** 32}, token_start=ints(range(n)), block_table=ints([[0]] * (n - 1)), seq_lens=lens[:-1])
     torch.cuda.synchronize()
     assert (out[:-1] == 1).all() and (out[-1] == 5).all()
+
+
+@pytest.mark.parametrize("B", [16, 32])
+def test_long_lists_of_many_rows(B):
+    """Lists longer than a unit, of other lengths a head, one empty, for one sequence and for several."""
+    for held in ([6400], [6000, 700, 0]):
+        x = Batch(20, held, [45, 20, 3][: len(held)], 8, 2, B=B, listed=4800 // B)
+        x.n[0, 1] = 37
+        if len(held) > 1:
+            x.n[1, 0] = 0
+        x.check()
