@@ -24,6 +24,26 @@ namespace chess {
 // heads: 16 sequences of 5 drafts over every page of 8 to 64K keys (2.19 GB) 366 us, 6.0 TB/s, what a read reaches; 32 sequences of 2 to 8 over lists of 108 pages
 // (229 MB) 46 us; one sequence's list of 21 pages 10.4.
 
+// The first key that any of the tokens [from, to] sees for its document.
+__device__ __forceinline__ int first_of_rows(const AttendArgs& a, int from, int to)
+{
+    int first = INT32_MAX;
+    if (to - from < 3) {
+        for (int i = from; i <= to; ++i) first = min(first, a.first_keys[i]);
+        return first;
+    }
+    for (int i = from; i <= to; i += 32) {            // (fours of them, asked for together: one by one they were most of the plan's time)
+        struct Four { int32_t first[4]; } four[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) __builtin_memcpy(&four[j], a.first_keys + min(i + 4 * j, to - 3), sizeof(Four));
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) first = min(first, four[j].first[e]);
+    }
+    return first;
+}
+
 // A lane's sequence as those that deal see it: the tiles of the keys that its rows can see at all, from `first` on, one at least if it has rows.
 struct LineSpan { int start, n_new, len, n_list, first, count; };
 
@@ -35,7 +55,10 @@ __device__ __forceinline__ LineSpan line_span(const AttendArgs& a, int b, int h)
     const int n_selected = kList ? a.n_selected[(int64_t)min(b, a.batch - 1) * a.n_kv_heads + h] : 0;
     const Span s = span_by_lane(a, min(b, a.batch - 1), B);
     LineSpan l{s.start, there ? s.n_new : 0, s.len, kList ? min(max(n_selected, 0), a.max_sel) : s.pages, 0, 0};
-    if constexpr (!kList) l.first = a.window > 0 ? max(s.len - s.n_new - a.window + 1, 0) / 32 : 0;
+    if constexpr (!kList) {
+        l.first = a.window > 0 ? max(s.len - s.n_new - a.window + 1, 0) / 32 : 0;
+        if (a.first_keys != nullptr && l.n_new > 0) l.first = max(l.first, max(first_of_rows(a, s.start, s.start + l.n_new - 1), 0) / 32);
+    }
     if (l.n_new > 0) l.count = max((kList ? (l.n_list + PPT - 1) / PPT : (s.len + 31) / 32) - l.first, 1);
     return l;
 }
@@ -386,22 +409,7 @@ __device__ __forceinline__ Keys keys_of_block(const AttendArgs& a, const Span& s
     const int p0 = s.len - s.n_new + i0, p1 = s.len - s.n_new + i1;
     Keys k{a.window > 0 ? max(p0 - a.window + 1, 0) : 0, min(a.prefix_lens != nullptr ? max(p1, max(a.prefix_lens[b], 1) - 1) : p1, s.len - 1)};
     if (a.first_keys != nullptr) {
-        int first = INT32_MAX;
-        const int32_t* of_row = a.first_keys + s.start;
-        if (i1 - i0 < 3) {
-            for (int i = i0; i <= i1; ++i) first = min(first, of_row[i]);
-        } else {
-            for (int i = i0; i <= i1; i += 32) {      // (fours of them, asked for together: one by one they are most of the plan's time)
-                struct Four { int32_t first[4]; } four[8];
-#pragma unroll
-                for (int j = 0; j < 8; ++j) __builtin_memcpy(&four[j], of_row + min(i + 4 * j, i1 - 3), sizeof(Four));
-#pragma unroll
-                for (int j = 0; j < 8; ++j)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) first = min(first, four[j].first[e]);
-            }
-        }
-        k.first = max(k.first, first);
+        k.first = max(k.first, first_of_rows(a, s.start + i0, s.start + i1));
     }
     if (p1 < 0) k.last = -1;
     return k;

@@ -328,3 +328,12 @@ def test_long_lists_of_many_rows(B):
         if len(held) > 1:
             x.n[1, 0] = 0
         x.check()
+
+
+@pytest.mark.parametrize("B", [16, 32])
+@pytest.mark.parametrize("new", [1, 2, 5, 13])
+def test_few_rows_deep_in_documents(new, B):
+    """Documents that begin far behind the sequence's start, at a token of the step, behind all of them, and at numbers that are no key."""
+    held = [900, 333, 64, 500]
+    first = np.concatenate([[870 + (i > 2) * 15] * 1 for i in range(new)] + [[333 + i // 2 for i in range(new)], [2 ** 31 - 1] * new, [-(2 ** 31)] * new])
+    Batch(21, held, [new] * 4, 8, 2, B=B, first=first).check()
