@@ -21,7 +21,7 @@ namespace chess {
 // Each wave has two tiles of LDS of its own: one is worked on, the next is on its way (loads that write LDS, no barrier).  A sequence that lies in one share
 // is written at once; partials of the others are merged by the last workgroup of the sequence to arrive.
 // Bound: HBM, for as long as a tile's arithmetic (about 1 us a wave and 32 rows) takes less than the four waves' 64 KB do (2.7 us).  Measured, 32 query and 8 KV
-// heads: 16 sequences of 5 drafts over every page of 8 to 64K keys (2.19 GB) 366 us, 6.0 TB/s, what a read reaches; 32 sequences of 2 to 8 over lists of 108 pages
+// heads: 16 sequences of 5 drafts over every page of 8 to 64K keys (2.19 GB) 364 to 372 us, 5.9 to 6.0 TB/s, what a read reaches; 32 sequences of 2 to 8 over lists of 108 pages
 // (229 MB) 46 us; one sequence's list of 21 pages 10.4.
 
 // The first key that any of the tokens [from, to] sees for its document.
@@ -141,7 +141,7 @@ __global__ __launch_bounds__(256, 1) void attend_few_kernel(AttendArgs a)
             const int page = i < n_list && p >= 0 && p < P ? p : -1;
             return Window{page, table[max(page, 0)]};
         };
-        // (Read once, so not kept in the caches: 32 sequences' lists 57.5 -> 51.6 us, every page of 16 sequences 409 -> 376.)
+        // (Read once, so not kept in the caches: in a graph 32 sequences' lists 57.5 -> 51.6 us, every page of 16 sequences 409 -> 376.)
         const auto fetch = [&](const int (&phys)[PPT], int stage) {
             const uint32_t to = ring_lds + (uint32_t)stage * 16384;
 #pragma unroll
