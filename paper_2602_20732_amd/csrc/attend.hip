@@ -127,7 +127,7 @@ __global__ __launch_bounds__(256, 1) void attend_few_kernel(AttendArgs a)
     const uint4* ring_own = ring + wave * 2048;
     uint4* queries = ring + kFewRing;
 
-    for (; line < end; ++b) {
+    for (; line < end && b < a.batch; ++b) {          // (b: should the lengths be changed meanwhile)
         if (b == block * 64 + 64) {
             ++block;
             mine = line_span<B, kList>(a, block * 64 + lane, h);
