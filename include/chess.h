@@ -485,8 +485,8 @@ typedef struct {
 int chess_attend_scratch_bytes(const chess_ctx* ctx, int32_t n_rows, int32_t max_new, int32_t batch, size_t* bytes);
 
 /*
- * seq_lens: the lengths WITH the new tokens, which are a sequence's last (chess_map_tokens' lens_after); max_new: no sequence has more of them (host
- * value; rows beyond are not attended).  q, out: bf16 [n_rows][n_q_heads][128].  The row of the token at position p attends to the keys t of its
+ * seq_lens: the lengths WITH the new tokens, which are a sequence's last (chess_map_tokens' lens_after); max_new: how many of them are attended at most, a
+ * sequence (host value; of a sequence that has more the first ones are, at the positions that they have, and the others' rows of out are left).  q, out: bf16 [n_rows][n_q_heads][128].  The row of the token at position p attends to the keys t of its
  * sequence with t <= p or t < prefix_lens[b], t >= first_keys[row], t > p - window; a row that sees no key is 0.  Keys that a row does not see do not
  * touch it, whatever they or their values are.  bf16 in and out; scores, softmax and sums in fp32 (weights are rounded to bf16 where the
  * keys are shared by more rows than a few: see attend.hip), distances p - t in fp32.  Scores may have any size that fp32 holds.

@@ -45,7 +45,7 @@ __device__ __forceinline__ int first_of_rows(const AttendArgs& a, int from, int 
 }
 
 // A lane's sequence as those that deal see it: the tiles of the keys that its rows can see at all, from `first` on, one at least if it has rows.
-struct LineSpan { int start, n_new, len, n_list, first, count; };
+struct LineSpan { int start, n_new, p0, len, n_list, first, count; };
 
 template <int B, bool kList>
 __device__ __forceinline__ LineSpan line_span(const AttendArgs& a, int b, int h)
@@ -54,9 +54,9 @@ __device__ __forceinline__ LineSpan line_span(const AttendArgs& a, int b, int h)
     const bool there = b < a.batch;
     const int n_selected = kList ? a.n_selected[(int64_t)min(b, a.batch - 1) * a.n_kv_heads + h] : 0;
     const Span s = span_by_lane(a, min(b, a.batch - 1), B);
-    LineSpan l{s.start, there ? s.n_new : 0, s.len, kList ? min(max(n_selected, 0), a.max_sel) : s.pages, 0, 0};
+    LineSpan l{s.start, there ? s.n_new : 0, s.p0, s.len, kList ? min(max(n_selected, 0), a.max_sel) : s.pages, 0, 0};
     if constexpr (!kList) {
-        l.first = a.window > 0 ? max(s.len - s.n_new - a.window + 1, 0) / 32 : 0;
+        l.first = a.window > 0 ? max(s.p0 - a.window + 1, 0) / 32 : 0;
         if (a.first_keys != nullptr && l.n_new > 0) l.first = max(l.first, max(first_of_rows(a, s.start, s.start + l.n_new - 1), 0) / 32);
     }
     if (l.n_new > 0) l.count = max((kList ? (l.n_list + PPT - 1) / PPT : (s.len + 31) / 32) - l.first, 1);
@@ -134,7 +134,8 @@ __global__ __launch_bounds__(256, 1) void attend_few_kernel(AttendArgs a)
         }
         const int in_block = b - block * 64, count = lane_of(mine.count, in_block);
         if (count == 0) continue;
-        const Span span{lane_of(mine.len, in_block), (lane_of(mine.len, in_block) + B - 1) / B, lane_of(mine.start, in_block), lane_of(mine.n_new, in_block)};
+        const Span span{lane_of(mine.len, in_block), (lane_of(mine.len, in_block) + B - 1) / B, lane_of(mine.start, in_block), lane_of(mine.n_new, in_block),
+                        lane_of(mine.p0, in_block)};
         const int first = lane_of(mine.first, in_block), n_list = lane_of(mine.n_list, in_block), line_end = line + count;
         // this segment, in tiles of the sequence
         int t = max(begin - line, 0) + first + wave;
@@ -422,7 +423,7 @@ __device__ __forceinline__ Keys keys_of_block(const AttendArgs& a, const Span& s
 {
     const int G = a.group, row_end = min((block + 1) * kBlockRows, s.n_new * G) - 1;
     const int i0 = (int)((unsigned)(block * kBlockRows) / (unsigned)G), i1 = (int)((unsigned)row_end / (unsigned)G);
-    const int p0 = s.len - s.n_new + i0, p1 = s.len - s.n_new + i1;
+    const int p0 = s.p0 + i0, p1 = s.p0 + i1;
     Keys k{a.window > 0 ? max(p0 - a.window + 1, 0) : 0, min(a.prefix_lens != nullptr ? max(p1, max(a.prefix_lens[b], 1) - 1) : p1, s.len - 1)};
     if (a.first_keys != nullptr) {
         k.first = max(k.first, first_of_rows(a, s.start + i0, s.start + i1));

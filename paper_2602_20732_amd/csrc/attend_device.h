@@ -27,8 +27,9 @@ __device__ __forceinline__ int lanes_max(int v)
 }
 __device__ __forceinline__ int lanes_min(int v) { return ~lanes_max(~v); }
 
-// A sequence of the step: its length, pages, and new tokens (none where token_start names rows that are not there).
-struct Span { int len, pages, start, n_new; };
+// A sequence of the step: its length, pages, and new tokens (none where token_start names rows that are not there): how many of them are attended, and the
+// position of the first (the last is at len - 1, whether it is attended or not).
+struct Span { int len, pages, start, n_new, p0; };
 
 __device__ __forceinline__ Span span_of(const AttendArgs& a, int b, int page_size)
 {
@@ -38,6 +39,7 @@ __device__ __forceinline__ Span span_of(const AttendArgs& a, int b, int page_siz
     s.len = min(max(__builtin_amdgcn_readfirstlane(a.seq_lens[b]), 0), a.max_pages * page_size);
     s.pages = (s.len + page_size - 1) / page_size;
     if (s.n_new < 0 || s.start < 0 || s.start > a.n_rows - s.n_new) s.n_new = 0;
+    s.p0 = s.len - s.n_new;
     s.n_new = min(s.n_new, a.max_new);
     return s;
 }
@@ -51,6 +53,7 @@ __device__ __forceinline__ Span span_by_lane(const AttendArgs& a, int b, int pag
     s.len = min(max(a.seq_lens[b], 0), a.max_pages * page_size);
     s.pages = (s.len + page_size - 1) / page_size;
     if (s.n_new < 0 || s.start < 0 || s.start > a.n_rows - s.n_new) s.n_new = 0;
+    s.p0 = s.len - s.n_new;
     s.n_new = min(s.n_new, a.max_new);
     return s;
 }
@@ -77,7 +80,7 @@ __device__ __forceinline__ RowView view_of(const AttendArgs& a, const Span& s, i
     r = min(r, last);
     const int i = (int)((unsigned)r / (unsigned)G), g = r - i * G;
     v.at = (int64_t)(s.start + i) * (a.n_kv_heads * G) + h * G + g;
-    v.p = s.len - s.n_new + i;
+    v.p = s.p0 + i;
     v.slope = a.slopes != nullptr ? a.slopes[h * G + g] * kLog2e : 0.f;
     v.lo = a.first_keys != nullptr ? max(a.first_keys[s.start + i], 0) : 0;
     if (a.window > 0) v.lo = max(v.lo, v.p - a.window + 1);

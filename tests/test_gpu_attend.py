@@ -337,3 +337,24 @@ def test_few_rows_deep_in_documents(new, B):
     held = [900, 333, 64, 500]
     first = np.concatenate([[870 + (i > 2) * 15] * 1 for i in range(new)] + [[333 + i // 2 for i in range(new)], [2 ** 31 - 1] * new, [-(2 ** 31)] * new])
     Batch(21, held, [new] * 4, 8, 2, B=B, first=first).check()
+
+
+RULES_OF_PLACES = [dict(), dict(window=20), dict(slopes=4.0, cap=10.0), dict(prefix=[45, 0, 1]), dict(first=True)]
+
+
+@pytest.mark.parametrize("rule", RULES_OF_PLACES, ids=rule_name)
+@pytest.mark.parametrize("listed", [None, 7])
+@pytest.mark.parametrize("new,most", [(3, 2), (16, 5), (60, 9), (60, 17), (300, 150)])
+def test_rows_before_max_new_keep_their_places(new, most, listed, rule):
+    """Fewer of a sequence's new tokens than it has: the first ones, at the positions that they have; the others' rows are left."""
+    held = [40, 333, 0]
+    if "first" in rule:
+        rule = dict(first=np.concatenate([(h + np.arange(new)) // 9 * 9 for h in held]))
+    b = Batch(22, held, [new] * 3, 8, 2, listed=listed, **rule)
+    b.most = most
+    out = b.launch(b.cuda())
+    torch.cuda.synchronize()
+    y, off = b.want()
+    rows = np.arange(b.rows) % new < most
+    got = out[: b.rows].double().cpu().numpy()
+    assert (np.abs(got - y) <= off)[rows].all() and (got[~rows] == 5).all() and (out[b.rows:] == 5).all()
