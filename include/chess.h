@@ -486,10 +486,12 @@ int chess_attend_scratch_bytes(const chess_ctx* ctx, int32_t n_rows, int32_t max
 
 /*
  * seq_lens: the lengths WITH the new tokens, which are a sequence's last (chess_map_tokens' lens_after); max_new: how many of them are attended at most, a
- * sequence (host value; of a sequence that has more the first ones are, at the positions that they have, and the others' rows of out are left).  q, out: bf16 [n_rows][n_q_heads][128].  The row of the token at position p attends to the keys t of its
- * sequence with t <= p or t < prefix_lens[b], t >= first_keys[row], t > p - window; a row that sees no key is 0.  Keys that a row does not see do not
- * touch it, whatever they or their values are.  bf16 in and out; scores, softmax and sums in fp32 (weights are rounded to bf16 where the
- * keys are shared by more rows than a few: see attend.hip), distances p - t in fp32.  Scores may have any size that fp32 holds.
+ * sequence (host value; of a sequence that has more the first ones are, at the positions that they have, and the others' rows of out are left).  q, out: bf16
+ * [n_rows][n_q_heads][128].  The row of the token at position p attends to the keys t of its sequence with t <= p or t < prefix_lens[b], t >= first_keys[row], t > p - window; a row that sees no key is 0.  Keys that a row does not see do not
+ * touch it, whatever they or their values are.  bf16 in and out; scores, softmax and sums in fp32, distances p - t in fp32.  Weights are a bf16 number and a bf16
+ * remainder (2^-17 of a weight) where min(max_new, n_rows) n_q_heads / H_kv is at most 64 and one bf16 number (2^-8) where it is more, or where `batch` sequences
+ * (lists) of the longest length that the configuration allows would have about 2^31 tiles of 32 keys: so a token's result can differ by that between calls with
+ * another max_new.  Scores may have any size that fp32 holds.
  * Block table entries behind a sequence's pages are not used.  A block table entry of a page that a sequence has must be a page of the pools.
  * workspace: as elsewhere (arrival counters); scratch: chess_attend_scratch_bytes at least, 256-byte aligned.  The same batch gives the same bits on every call.
  */

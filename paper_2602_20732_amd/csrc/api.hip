@@ -922,8 +922,9 @@ static AttendLayout attend_layout(const chess_ctx* ctx, const chess::AttendShape
 int chess_attend_scratch_bytes(const chess_ctx* ctx, int32_t n_rows, int32_t max_new, int32_t batch, size_t* bytes)
 {
     if (!ctx || !bytes || n_rows < 1 || n_rows > CHESS_MAX_TOKENS || max_new < 1 || batch < 1 || batch > ctx->cfg.max_batch) return CHESS_EINVAL;
-    // (a call with fewer new tokens of a sequence may be one of few rows)
-    *bytes = std::max(attend_layout(ctx, chess::attend_shape(ctx, n_rows, max_new, batch)).bytes, attend_layout(ctx, chess::attend_shape(ctx, 64, 64 / ctx->geom.group, 1)).bytes);
+    // (a call over lists, or with fewer new tokens of a sequence or fewer sequences, may be one of few rows)
+    *bytes = std::max({attend_layout(ctx, chess::attend_shape(ctx, n_rows, max_new, batch, false)).bytes, attend_layout(ctx, chess::attend_shape(ctx, n_rows, max_new, batch, true)).bytes,
+                       attend_layout(ctx, chess::attend_shape(ctx, 64, 64 / ctx->geom.group, 1, false)).bytes});
     return CHESS_OK;
 }
 
@@ -950,7 +951,7 @@ static int attend_common(chess_ctx* ctx, const chess_scores* scores, const void*
     }
     max_new = std::min(max_new, n_rows);
     const chess::Geom& g = ctx->geom;
-    const chess::AttendShape s = chess::attend_shape(ctx, n_rows, max_new, batch);
+    const chess::AttendShape s = chess::attend_shape(ctx, n_rows, max_new, batch, page_ids != nullptr);
     const AttendLayout lay = attend_layout(ctx, s);
     if (scratch_bytes < lay.bytes) return CHESS_EINVAL;
     if (batch > chess::kDealMost || (int64_t)n_rows * g.group > (1 << 30) || (s.blocks + s.extra) * g.n_kv_heads > (1 << 24) - 1) return CHESS_ENOTSUP;

@@ -921,13 +921,13 @@ static hipError_t launch_many(chess_ctx* ctx, const AttendArgs& a, const AttendS
 }
 
 // Few rows: a line a KV head.  Many: units; `most` blocks and cut units that there can be, whatever the sequences are.
-AttendShape attend_shape(const chess_ctx* ctx, int64_t n_rows, int64_t max_new, int64_t batch)
+AttendShape attend_shape(const chess_ctx* ctx, int64_t n_rows, int64_t max_new, int64_t batch, bool list)
 {
     const Geom& g = ctx->geom;
     AttendShape s{};
     max_new = std::min(max_new, n_rows);
     const int64_t cu = std::max(ctx->n_cu / g.n_kv_heads, 1);
-    if (max_new * g.group <= 64) {
+    if (few_rows(max_new * g.group, batch, cdiv(list ? g.max_sel : g.max_pages, 32 / g.page_size), cu)) {
         s.rows = max_new * g.group <= 32 ? 32 : 64;
         s.n_slots = cu;
         s.parts = 2 * cu * g.n_kv_heads;

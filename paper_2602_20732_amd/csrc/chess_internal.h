@@ -466,7 +466,7 @@ struct AttendArgs {
 // How a call is cut.  rows: of a workgroup (32, 64: few; 128: many); blocks, extra: most blocks of 128 rows, most units beyond one a block; parts: most
 // partials of `rows` rows.
 struct AttendShape { int64_t rows, n_slots, blocks, extra, parts; };
-AttendShape attend_shape(const chess_ctx* ctx, int64_t n_rows, int64_t max_new, int64_t batch);
+AttendShape attend_shape(const chess_ctx* ctx, int64_t n_rows, int64_t max_new, int64_t batch, bool list);
 hipError_t launch_attend(chess_ctx* ctx, AttendArgs a, const AttendShape& s, hipStream_t stream);
 
 // Drafted tokens verified (verify.hip).

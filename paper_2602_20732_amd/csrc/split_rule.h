@@ -22,6 +22,14 @@ struct SplitLimits {
 
 constexpr int kDealMost = 4096;   // most sequences whose every-page attention is dealt by length
 
+// Attention of a step's new tokens (attend.hip): whether a call is one of few rows, up to `rows` a sequence and KV head.  Those put the batch's tiles in a
+// line of `slots` shares that is counted in 32 bits: not where its sequences of up to `tiles` tiles could be longer together (block tables that share pages can
+// name more than there are), with what shares are rounded up by (a tile or, of few tiles, four, and twelve that spare a change of sequence).
+inline bool few_rows(int64_t rows, int64_t batch, int64_t tiles, int64_t slots)
+{
+    return rows <= 64 && batch * std::max<int64_t>(tiles, 1) + 16 * slots <= INT32_MAX;
+}
+
 inline int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
 inline int64_t clampi(int64_t x, int64_t lo, int64_t hi) { return x < lo ? lo : (x > hi ? hi : x); }
 

@@ -358,3 +358,24 @@ def test_rows_before_max_new_keep_their_places(new, most, listed, rule):
     rows = np.arange(b.rows) % new < most
     got = out[: b.rows].double().cpu().numpy()
     assert (np.abs(got - y) <= off)[rows].all() and (got[~rows] == 5).all() and (out[b.rows:] == 5).all()
+
+
+def test_few_rows_whose_tiles_could_be_more_than_32_bits_count():
+    """33 sequences with room for 2^31 tokens each: not a line of tiles.  Over lists, which are short, one all the same."""
+    new, room = np.arange(33) % 4, (1 << 26) - 1
+    b = Batch(25, np.arange(33) * 37, new, 4, 1, B=32)
+    lib = pk.Chess(pk.Config(4, 1, 32, 33, room, b.width))
+    args = b.cuda()
+    table = torch.zeros((33, room), dtype=torch.int32, device="cuda")
+    table[:, : b.width] = args["block_table"]
+    args.update(block_table=table, workspace=torch.zeros(lib.workspace_bytes, dtype=torch.uint8, device="cuda"), scratch=lib.new_attend_scratch(b.rows, b.most, 33))
+    b.lib = lib
+    dense = b.launch(args).clone()
+    torch.cuda.synchronize()
+    assert (dense[b.rows:] == 5).all()
+    b.ids = np.broadcast_to(np.arange(b.width), (33, 1, b.width)).copy()
+    b.n = np.array(b.pages)[:, None]
+    args["out"].fill_(5.0)
+    b.check(b.launch(args)[: b.rows])
+    b.most = 17                                                   # (weights of many rows)
+    b.check(dense[: b.rows])
