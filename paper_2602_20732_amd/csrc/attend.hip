@@ -74,7 +74,7 @@ __global__ __launch_bounds__(256, 1) void attend_few_kernel(AttendArgs a)
     __shared__ float wave_m[4][32 * kRows], wave_l[4][32 * kRows];
     __shared__ int block_tiles[kDealMost / 64];
     __shared__ Odd odd[kRows][256];
-    __shared__ int flag;
+    __shared__ int wave_odd[4], flag;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     const int col = lane & 31, half = lane >> 5;
     const int H = a.n_kv_heads, G = a.group, h = blockIdx.x % H, slot = blockIdx.x / H;
@@ -340,11 +340,8 @@ __global__ __launch_bounds__(256, 1) void attend_few_kernel(AttendArgs a)
                     }
         }
 
-        if (any_odd)
-#pragma unroll
-            for (int y = 0; y < kRows; ++y) add_not_finite(o[y], odd[y][threadIdx.x]);
-
         // the workgroup's waves: O^T[dim 32 d + 8 (i / 4) + 4 half + i % 4][row col]
+        if (lane == 0) wave_odd[wave] = any_odd;
 #pragma unroll
         for (int y = 0; y < kRows; ++y) {
             l[y] += __shfl_xor(l[y], 32);
@@ -356,7 +353,7 @@ __global__ __launch_bounds__(256, 1) void attend_few_kernel(AttendArgs a)
         __syncthreads();                              // (and no wave's tiles are read or written any more)
         float(*comb)[4][16][64] = reinterpret_cast<float(*)[4][16][64]>(ring);
         const int w0 = line / share, n_parts = (line_end - 1) / share - w0 + 1;
-        const bool whole = n_parts == 1;
+        const bool whole = n_parts == 1, some_odd = __builtin_amdgcn_readfirstlane(wave_odd[0] | wave_odd[1] | wave_odd[2] | wave_odd[3]) != 0;
         const int64_t part0 = 2 * ((int64_t)h * a.n_slots + w0);
         const int64_t part_own = 2 * ((int64_t)h * a.n_slots + slot) + (slot == w0 ? 1 : 0);
 #pragma unroll
@@ -381,6 +378,20 @@ __global__ __launch_bounds__(256, 1) void attend_few_kernel(AttendArgs a)
                 float x[4];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) x[i] = (buf[0][4 * wave + i][lane] + buf[1][4 * wave + i][lane]) + (buf[2][4 * wave + i][lane] + buf[3][4 * wave + i][lane]);
+                // (infinities behind the sums: a wave's factor may come to 0 where the weights that it rescales do not)
+                if (__builtin_expect(some_odd, 0)) {
+                    uint64_t up = 0, down = 0;
+#pragma unroll
+                    for (int w = 0; w < 4; ++w) {
+                        up |= odd[y][64 * w + lane].up;
+                        down |= odd[y][64 * w + lane].down;
+                    }
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        if (up >> (16 * d + 4 * wave + i) & 1) x[i] += INFINITY;
+                        if (down >> (16 * d + 4 * wave + i) & 1) x[i] -= INFINITY;
+                    }
+                }
                 const int dim = 32 * d + 8 * wave + 4 * half;
                 if (whole) {
                     if (row[y].there)

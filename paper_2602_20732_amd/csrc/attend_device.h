@@ -276,6 +276,22 @@ __device__ __forceinline__ void merge_parts(const AttendArgs& a, const Span& spa
         }
 #pragma unroll
         for (int y = 0; y < kPieces; ++y) {
+            // A factor may come to 0 where the weights that it rescales do not: an infinite sum stays infinite.  (Looked for behind the sums: a choice a product
+            // in code that runs once, cold, cost 1.5 to 2.7 us a launch.)
+            const float any_nan = (x[y][0] + x[y][1]) + (x[y][2] + x[y][3]);
+            if (__builtin_expect(__any(any_nan != any_nan), 0)) {
+                x[y][0] = x[y][1] = x[y][2] = x[y][3] = 0.f;
+#pragma nounroll
+                for (int s = 0; s < n_parts; ++s) {
+                    const int64_t part = number(s);
+                    const float by = __builtin_amdgcn_exp2f(__builtin_bit_cast(float2, observe_u64(reinterpret_cast<const uint64_t*>(a.part_ml) + part * kRowsOf + r[y])).x - M[y]);
+                    const uint64_t* at = reinterpret_cast<const uint64_t*>(a.part_acc + part_at<kLines>(part, kRowsOf, r[y], dim[y]));
+                    const float2 lo = __builtin_bit_cast(float2, observe_u64(at)), hi = __builtin_bit_cast(float2, observe_u64(at + kOtherPair<kLines>));
+                    const float v[4] = {lo.x, lo.y, hi.x, hi.y};
+#pragma unroll
+                    for (int d = 0; d < 4; ++d) x[y][d] += fabsf(v[d]) == INFINITY ? v[d] : v[d] * by;
+                }
+            }
             const float inv = l[y] == 0.f ? 0.f : 1.f / l[y];
             if (row0 + r[y] < n_rows)
                 *reinterpret_cast<uint2*>(a.out + row_at(a, span, h, row0 + r[y]) * kHeadDim + dim[y]) =

@@ -379,3 +379,26 @@ def test_few_rows_whose_tiles_could_be_more_than_32_bits_count():
     b.check(b.launch(args)[: b.rows])
     b.most = 17                                                   # (weights of many rows)
     b.check(dense[: b.rows])
+
+
+# single keys, a tile, several shares of a line, the last tile
+LOW = [(300, 301), (320, 352), (0, 512), (1024, 2048), (2995, 2996)]
+
+
+@pytest.mark.parametrize("rule", [dict(), dict(slopes=40.0)], ids=rule_name)
+@pytest.mark.parametrize("value", [np.inf, -np.inf, np.nan])
+@pytest.mark.parametrize("low", LOW, ids=str)
+@pytest.mark.parametrize("new", [5, 16])
+def test_infinite_values_of_keys_that_weigh_next_to_nothing(new, low, value, rule):
+    """Weights of e^-250 to e^-700 are not 0: their sum with an infinity is one, in whatever tile, share or unit the keys lie, and it stays in its dims."""
+    b = Batch(23, [3000, 2300], [new, new], 8, 2, **rule)
+    b.q = bf16(b.q.float().numpy() + 2)
+    for s, (k, v) in enumerate(b.seqs):
+        if low[1] <= len(k):
+            k[low[0]:low[1]] = -15
+            v[low[0], 0, 3], v[low[1] - 1, 1, 64:] = value, -value
+            for p in range(b.pages[s]):
+                b.put(s, p)
+    y, _ = b.want()
+    assert not np.isfinite(y).all() and np.isfinite(y).any()
+    b.check()
