@@ -613,7 +613,7 @@ __global__ __launch_bounds__(256, 2) void attend_many_kernel(AttendArgs a)
     constexpr int PPT = 64 / B;
     extern __shared__ uint4 stages[];                 // [2][1024] keys, [2][1024] values
     __shared__ Odd odd[256];
-    __shared__ int wave_lo[4], wave_hi[4], flag;
+    __shared__ int wave_lo[4], wave_hi[4], wave_nan[4], flag;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
     const int col = lane & 31, half = lane >> 5;
     const int H = a.n_kv_heads, G = a.group, h = blockIdx.x % H, unit = blockIdx.x / H;
@@ -716,13 +716,13 @@ __global__ __launch_bounds__(256, 2) void attend_many_kernel(AttendArgs a)
         if (t + 1 < t_end) fetch_values(phys, stage ^ 1);
         phys = phys_next;
     };
-    // whether every row of the block sees all of tile t (the same in every wave)
-    const auto is_whole = [&] {
-        if constexpr (!kList) return ((t * 64 - all_lo) | (all_hi - t * 64 - 63)) >= 0;
+    // whether every row of the block sees all of a tile (the same in every wave)
+    const auto is_whole = [&](int tile) {
+        if constexpr (!kList) return ((tile * 64 - all_lo) | (all_hi - tile * 64 - 63)) >= 0;
         int less = 0;
 #pragma unroll
         for (int s = 0; s < PPT; ++s) {
-            const int p = page_at(t * PPT + s);
+            const int p = page_at(tile * PPT + s);
             less |= p | (p * B - all_lo) | (all_hi - p * B - B + 1);
         }
         return less >= 0;
@@ -783,7 +783,7 @@ __global__ __launch_bounds__(256, 2) void attend_many_kernel(AttendArgs a)
                     for (int e = 0; e < 8; ++e) z[i >> 1][8 * (i & 1) + e] = fmaf(-row.slope, fabsf(d - (float)e), z[i >> 1][8 * (i & 1) + e]);
                 }
         }
-        if (!is_whole()) {
+        if (!is_whole(t)) {
             Seen seen[2];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
@@ -863,10 +863,53 @@ __global__ __launch_bounds__(256, 2) void attend_many_kernel(AttendArgs a)
         while (t < t_end) {
             begin_tile();
             const Seen none[2];
-            if (!is_whole()) clean(none);
+            if (!is_whole(t)) clean(none);
             ++t;
             stage ^= 1;
         }
+    }
+    // Tiles that all rows see whole are not looked through for values that are not finite.  Sums that come to NaN with one (a weight that is only small has become 0)
+    // say so by themselves (as two do that are infinite either way), and then the values of those tiles are looked at: what they do is the same for every row.
+    float of_dims[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+#pragma unroll
+        for (int d = 0; d < 4; ++d) of_dims[d] += o[d][i];
+    const float of_all = (of_dims[0] + of_dims[1]) + (of_dims[2] + of_dims[3]);
+    const int some_nan = __any(of_all != of_all);
+    if (lane == 0) wave_nan[wave] = some_nan;
+    __syncthreads();                                  // (and nobody reads the last tile any more)
+    if (__builtin_expect(__builtin_amdgcn_readfirstlane(wave_nan[0] | wave_nan[1] | wave_nan[2] | wave_nan[3]) != 0, 0)) {
+        // A thread: half of a tile's values of a dim; bit 0: up, bit 1: down.  (A key that is not finite has a score of -infinity, if it has one that is not a row's
+        // NaN: it weighs nothing.)
+        const int dim = threadIdx.x % kHeadDim;
+        uint32_t bits = 0;
+#pragma nounroll
+        for (int tile = t_first; tile < t_end; ++tile)
+            if (is_whole(tile))
+#pragma nounroll
+                for (int i = 0; i < 32; ++i) {
+                    const int token = (threadIdx.x / kHeadDim) * 32 + i;
+                    const int64_t at = ((int64_t)table[page_at(tile * PPT + token / B)] * H + h) * (B * kHeadDim);
+                    const uint32_t x = a.v_pool[at + dim * B + token % B];
+                    if ((x & 0x7f80u) == 0x7f80u) {
+                        uint32_t most = (x & 0x7fu) != 0 ? 0x7f80u : 0u;
+#pragma nounroll
+                        for (int c = 0; a.cap_in == 0.f && c < kHeadDim; ++c) most = max(most, a.k_pool[at + token % B * kHeadDim + c] & 0x7fffu);
+                        bits |= most >= 0x7f80u ? 3u : x >> 15 != 0 ? 2u : 1u;
+                    }
+                }
+        uint32_t* of_dim = reinterpret_cast<uint32_t*>(stages);
+        of_dim[threadIdx.x] = bits;
+        __syncthreads();
+#pragma unroll
+        for (int d = 0; d < 4; ++d)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const int at = 32 * d + 8 * (i >> 2) + 4 * half + (i & 3);
+                const uint32_t both = of_dim[at] | of_dim[kHeadDim + at];
+                if (o[d][i] != o[d][i] && (both == 1 || both == 2)) o[d][i] = both == 1 ? INFINITY : -INFINITY;
+            }
     }
     if (any_odd) add_not_finite(o, odd[threadIdx.x]);
     l += __shfl_xor(l, 32);

@@ -385,10 +385,10 @@ def test_few_rows_whose_tiles_could_be_more_than_32_bits_count():
 LOW = [(300, 301), (320, 352), (0, 512), (1024, 2048), (2995, 2996)]
 
 
-@pytest.mark.parametrize("rule", [dict(), dict(slopes=40.0)], ids=rule_name)
-@pytest.mark.parametrize("value", [np.inf, -np.inf, np.nan])
+@pytest.mark.parametrize("rule", [dict(), dict(slopes=40.0), dict(listed=200, width=210)], ids=rule_name)
+@pytest.mark.parametrize("value", [np.inf, np.nan])
 @pytest.mark.parametrize("low", LOW, ids=str)
-@pytest.mark.parametrize("new", [5, 16])
+@pytest.mark.parametrize("new", [5, 16, 40])
 def test_infinite_values_of_keys_that_weigh_next_to_nothing(new, low, value, rule):
     """Weights of e^-250 to e^-700 are not 0: their sum with an infinity is one, in whatever tile, share or unit the keys lie, and it stays in its dims."""
     b = Batch(23, [3000, 2300], [new, new], 8, 2, **rule)
@@ -402,3 +402,28 @@ def test_infinite_values_of_keys_that_weigh_next_to_nothing(new, low, value, rul
     y, _ = b.want()
     assert not np.isfinite(y).all() and np.isfinite(y).any()
     b.check()
+
+
+@pytest.mark.parametrize("cap", [0.0, 20.0])
+@pytest.mark.parametrize("value", [np.inf, -np.inf])
+@pytest.mark.parametrize("new", [5, 150])
+def test_infinite_keys_whose_values_are_infinite(new, value, cap):
+    """A score of -infinity weighs nothing, and nothing times an infinity is NaN, in that value's dims; with a cap the key weighs something."""
+    b = Batch(26, [1000], [new], 8, 2, cap=cap)
+    b.q = bf16(b.q.float().numpy() + 2)
+    k, v = b.seqs[0]
+    key = np.array(k[300])
+    # (an odd dim of the first KV head's key; all but the negative ones of the queries see -infinity)
+    k[300, 0, 7], v[300, 0, 3], v[300, 1, 9], v[301, 0, 11] = -np.inf, value, value, value
+    b.put(0, 300 // 16)
+    got = b.run().double().cpu().numpy()
+    y, _ = b.want()
+    k[300, 0, 7], v[300, 0, 3] = key[0, 7], 0
+    if not cap:
+        k[300, 0] = -15                                           # (what weighs nothing, for the bounds)
+    _, off = b.want()
+    assert (np.isnan(got) == np.isnan(y)).all() and (got[np.isinf(y)] == y[np.isinf(y)]).all()
+    fine = np.isfinite(y)
+    assert np.isnan(y[:, :4, 3]).all() == (cap == 0) and np.isinf(y).any() and fine.any()
+    # (with a cap the score of the key is the cap, off by no more than the others')
+    assert (np.abs(got - y) <= off)[fine].all()
