@@ -56,7 +56,7 @@ __device__ __forceinline__ LineSpan line_span(const AttendArgs& a, int b, int h)
     const Span s = span_by_lane(a, min(b, a.batch - 1), B);
     LineSpan l{s.start, there ? s.n_new : 0, s.p0, s.len, kList ? min(max(n_selected, 0), a.max_sel) : s.pages, 0, 0};
     if constexpr (!kList) {
-        l.first = a.window > 0 ? max(s.p0 - a.window + 1, 0) / 32 : 0;
+        l.first = first_in_window(a, s.p0) / 32;
         if (a.first_keys != nullptr && l.n_new > 0) l.first = max(l.first, max(first_of_rows(a, s.start, s.start + l.n_new - 1), 0) / 32);
     }
     if (l.n_new > 0) l.count = max((kList ? (l.n_list + PPT - 1) / PPT : (s.len + 31) / 32) - l.first, 1);
@@ -435,7 +435,7 @@ __device__ __forceinline__ Keys keys_of_block(const AttendArgs& a, const Span& s
     const int G = a.group, row_end = min((block + 1) * kBlockRows, s.n_new * G) - 1;
     const int i0 = (int)((unsigned)(block * kBlockRows) / (unsigned)G), i1 = (int)((unsigned)row_end / (unsigned)G);
     const int p0 = s.p0 + i0, p1 = s.p0 + i1;
-    Keys k{a.window > 0 ? max(p0 - a.window + 1, 0) : 0, min(a.prefix_lens != nullptr ? max(p1, max(a.prefix_lens[b], 1) - 1) : p1, s.len - 1)};
+    Keys k{first_in_window(a, p0), min(a.prefix_lens != nullptr ? max(p1, max(a.prefix_lens[b], 1) - 1) : p1, s.len - 1)};
     if (a.first_keys != nullptr) {
         k.first = max(k.first, first_of_rows(a, s.start + i0, s.start + i1));
     }

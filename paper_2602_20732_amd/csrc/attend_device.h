@@ -58,6 +58,9 @@ __device__ __forceinline__ Span span_by_lane(const AttendArgs& a, int b, int pag
     return s;
 }
 
+// The first key of the window that ends at position p.  (p may be negative, the window as large as an int: no difference of the two.)
+__device__ __forceinline__ int first_in_window(const AttendArgs& a, int p) { return a.window > 0 && p >= a.window ? p - a.window + 1 : 0; }
+
 // Query row r of a sequence and KV head: head r % G of its new token r / G.  A row that is not there is the last one again, and sees nothing.
 struct RowView {
     int64_t at;              // row of q and out
@@ -82,8 +85,7 @@ __device__ __forceinline__ RowView view_of(const AttendArgs& a, const Span& s, i
     v.at = (int64_t)(s.start + i) * (a.n_kv_heads * G) + h * G + g;
     v.p = s.p0 + i;
     v.slope = a.slopes != nullptr ? a.slopes[h * G + g] * kLog2e : 0.f;
-    v.lo = a.first_keys != nullptr ? max(a.first_keys[s.start + i], 0) : 0;
-    if (a.window > 0) v.lo = max(v.lo, v.p - a.window + 1);
+    v.lo = max(a.first_keys != nullptr ? a.first_keys[s.start + i] : 0, first_in_window(a, v.p));
     v.hi = a.prefix_lens != nullptr ? max(v.p, max(a.prefix_lens[b], 1) - 1) : v.p;
     v.hi = min(v.hi, s.len - 1);
     if (!v.there || v.p < 0) {

@@ -427,3 +427,18 @@ def test_infinite_keys_whose_values_are_infinite(new, value, cap):
     assert np.isnan(y[:, :4, 3]).all() == (cap == 0) and np.isinf(y).any() and fine.any()
     # (with a cap the score of the key is the cap, off by no more than the others')
     assert (np.abs(got - y) <= off)[fine].all()
+
+
+@pytest.mark.parametrize("new,heads,lengths", [(6, (4, 2), (46, 2, 1)), (60, (4, 2), (100, 2, 1)), (200, (2, 2), (240, 150, 100))], ids=str)
+def test_windows_as_large_as_there_are(new, heads, lengths):
+    """A window that no sequence reaches is none, also where a row's position would be negative."""
+    b = Batch(24, [40], [new], *heads)
+    for length in lengths:
+        out = []
+        for window in (0, 2 ** 31 - 1):
+            b.window = window
+            args = b.cuda()
+            args["seq_lens"] = ints([length])
+            out.append(b.launch(args))
+        torch.cuda.synchronize()
+        assert torch.equal(*out) and (out[0][new - min(new, length):new] != 0).any()
