@@ -317,13 +317,17 @@ __device__ __forceinline__ void merge_parts(const AttendArgs& a, const Span& spa
                  "global_load_lds_dwordx4 %5, %1 offset:0xc00" hint \
                  :                                           \
                  : "s"(lds), "s"(base), "v"(at0), "v"(at1), "v"(at2), "v"(at3) \
-                 : "memory")
+                 : "m0", "memory")
+// (m0 is never the compiler's to allocate, of which it warns, but it may put a value there for instructions of its own and use it again later)
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
 template <bool kOnce>
 __device__ __forceinline__ void load_4k(uint32_t lds, const void* base, uint32_t at0, uint32_t at1, uint32_t at2, uint32_t at3)
 {
     if constexpr (kOnce) CHESS_LOAD_4K(" nt");
     else CHESS_LOAD_4K("");
 }
+#pragma clang diagnostic pop
 #undef CHESS_LOAD_4K
 template <int kLeft>
 __device__ __forceinline__ void loads_left()
