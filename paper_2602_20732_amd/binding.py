@@ -526,7 +526,8 @@ class Chess:
             raise ChessError(f"rotary: of the context's device ({dev}) and, with weights a head, {c.n_q_heads} and {c.n_kv_heads} heads is wanted, "
                              f"got device {rotary.device}, heads {rotary.weights}")
         _need(positions, "positions", _INT, rotary.n_axes * n, dev)
-        if positions.numel() != rotary.n_axes * n:
+        # (one axis in any shape of as many; [rows, axes] would be read as [axes, rows])
+        if positions.numel() != rotary.n_axes * n or rotary.n_axes > 1 and positions.dim() > 1 and positions.shape[-1] != n:
             raise ChessError(f"positions: [{rotary.n_axes}, {n}] is wanted, got {tuple(positions.shape)}")
 
     def rotate(self, rotary: Rotary, q, k, positions, q_out=None, k_out=None, counts=None):

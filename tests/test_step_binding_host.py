@@ -145,3 +145,19 @@ def test_verification_refuses(chess, name, bad):
     with pytest.raises(pk.ChessError):
         chess.verify(**{**verify_args(), name: bad})
     assert not chess.lib.calls
+
+
+def test_positions_by_rows_are_refused(chess):
+    """[rows, axes] has as many numbers as [axes, rows], in another order."""
+    args = {**rotate_args(), "rotary": pk.Rotary(torch.ones(64), axis=[0, 1, 2, 1] * 16)}
+    for bad in (i32(5, 3), i32(1, 5, 3), i32(15, 1)):
+        with pytest.raises(pk.ChessError):
+            chess.rotate_store(**{**args, "positions": bad})
+        with pytest.raises(pk.ChessError):
+            chess.rotate(args["rotary"], args["q"], None, bad, args["q_out"])
+    assert not chess.lib.calls
+    for good in (i32(3, 5), i32(15)):
+        chess.rotate_store(**{**args, "positions": good})
+    for one in (i32(5), i32(1, 5), i32(5, 1)):
+        chess.rotate_store(**{**rotate_args(), "positions": one})
+    assert len(chess.lib.calls) == 5
