@@ -249,3 +249,71 @@ def test_on_a_stream_of_its_own_and_replayed():
         g.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(want, (q_out, kp, vp)))
+
+
+shape_name = lambda s: "-".join(f"{k}{v}" for k, v in s.items()) or "plain"  # noqa: E731
+MANY = [dict(), dict(interleaved=True, turned=48, axes=4, norms="head"), dict(norms="head", axes=2), dict(norms=None, scale=1.25, turned=96), dict(interleaved=True, turned=64)]
+
+
+def many_rows():
+    """Enough for the kernel of prompts, which turns all heads of a token in one workgroup (16 rows are one, 2 a compute unit are many); the last has 9."""
+    return 32 * torch.cuda.get_device_properties(0).multi_processor_count + 9
+
+
+@pytest.mark.parametrize("heads", [(20, 5), (7, 1), (16, 16)], ids=str)
+@pytest.mark.parametrize("shape", MANY, ids=shape_name)
+def test_rotate_many_rows(shape, heads):
+    n = many_rows()
+    c = Case(n, n, *heads, **shape)
+    q, k, _, positions = c.cuda()
+    lib = pk.Chess(pk.Config(*heads, 16, 1, 4, 4))
+    q_out, k_out = (torch.full((n + 1, h, D), 7.0, dtype=torch.bfloat16, device="cuda") for h in heads)
+    lib.rotate(c.rotary, q, k, positions, q_out[:n], k_out[:n])
+    torch.cuda.synchronize()
+    q_exact, k_exact = c.exact(0), c.exact(1)
+    near(q_out[:n], q_exact)
+    near(k_out[:n], k_exact)
+    assert (q_out[n:] == 7).all() and (k_out[n:] == 7).all()
+    # one of the two, fewer rows than there is room for, and in place
+    some, alone = n - 20, torch.full((n, heads[0], D), 7.0, dtype=torch.bfloat16, device="cuda")
+    lib.rotate(c.rotary, q, None, positions, alone, None, counts=ints([some]))
+    assert torch.equal(alone[:some], q_out[:some]) and (alone[some:] == 7).all()
+    own = k.contiguous()
+    lib.rotate(c.rotary, None, own, positions, None, own)
+    assert torch.equal(own, k_out[:n])
+    both = [q.contiguous(), k.contiguous()]
+    lib.rotate(c.rotary, *both, positions, *both)
+    assert torch.equal(both[0], q_out[:n]) and torch.equal(both[1], k_out[:n])
+
+
+@pytest.mark.parametrize("queries", [True, False], ids=["both", "keys"])
+@pytest.mark.parametrize("heads", [(20, 5), (8, 2)], ids=str)
+@pytest.mark.parametrize("B", [16, 32])
+@pytest.mark.parametrize("shape", MANY, ids=shape_name)
+def test_store_with_room_for_many_entries(shape, B, heads, queries):
+    """The room of the write list chooses the kernel; entries behind counts[1] are anything."""
+    rng = np.random.default_rng(B + heads[0])
+    n_pages, H = 130, heads[1]
+    writes, n = entries_of(rng, B, n_pages, SPANS[3])
+    c = Case(n, n, *heads, **shape)
+    q, k, v, positions = c.cuda()
+    lib = pk.Chess(pk.Config(*heads, B, 8, 64, 64))
+    before = bf16(rng.normal(0, 1, (2, n_pages, H, B, D)))
+    k_pool, v_pool = before[0].cuda(), before[1].transpose(2, 3).contiguous().cuda()
+    q_out = torch.zeros((n, heads[0], D), dtype=torch.bfloat16, device="cuda")
+    room = torch.zeros((many_rows() // 16 + 3, 4), dtype=torch.int32, device="cuda")
+    room[:, 1] = n - 1
+    room[:, 3] = 1
+    room[: len(writes)] = ints(writes)
+    lib.rotate_store(c.rotary, q if queries else None, k, v, positions, room, ints([n, len(writes), 0, 0]), q_out if queries else None, k_pool, v_pool)
+    torch.cuda.synchronize()
+    if queries:
+        near(q_out, c.exact(0))
+    y, off = c.exact(1)
+    k_want, k_off, v_want = before[0].double().numpy(), np.zeros((n_pages, H, B, D)), before[1].clone()
+    for page, row, first, count in writes:
+        k_want[page][:, first:first + count] = y[row:row + count].transpose(1, 0, 2)
+        k_off[page][:, first:first + count] = off[row:row + count].transpose(1, 0, 2)
+        v_want[page][:, first:first + count] = c.v[row:row + count].transpose(0, 1)
+    near(k_pool, (k_want, k_off))
+    assert torch.equal(v_pool.cpu().view(torch.int16), v_want.transpose(2, 3).contiguous().view(torch.int16))
