@@ -880,25 +880,30 @@ __global__ __launch_bounds__(256, 2) void attend_many_kernel(AttendArgs a)
     if (lane == 0) wave_nan[wave] = some_nan;
     __syncthreads();                                  // (and nobody reads the last tile any more)
     if (__builtin_expect(__builtin_amdgcn_readfirstlane(wave_nan[0] | wave_nan[1] | wave_nan[2] | wave_nan[3]) != 0, 0)) {
-        // A thread: half of a tile's values of a dim; bit 0: up, bit 1: down.  (A key that is not finite has a score of -infinity, if it has one that is not a row's
-        // NaN: it weighs nothing.)
+        // A thread: half of a tile's values of a dim, eight at a time; bit 0: up, bit 1: down.  (A key that is not finite has a score of -infinity, if it has one that
+        // is not a row's NaN: it weighs nothing.)
         const int dim = threadIdx.x % kHeadDim;
         uint32_t bits = 0;
 #pragma nounroll
-        for (int tile = t_first; tile < t_end; ++tile)
-            if (is_whole(tile))
+        for (int tile = t_first; tile < t_end && bits != 3; ++tile) {
+            if (!is_whole(tile)) continue;
 #pragma nounroll
-                for (int i = 0; i < 32; ++i) {
-                    const int token = (threadIdx.x / kHeadDim) * 32 + i;
-                    const int64_t at = ((int64_t)table[page_at(tile * PPT + token / B)] * H + h) * (B * kHeadDim);
-                    const uint32_t x = a.v_pool[at + dim * B + token % B];
-                    if ((x & 0x7f80u) == 0x7f80u) {
-                        uint32_t most = (x & 0x7fu) != 0 ? 0x7f80u : 0u;
+            for (int i = 0; i < 4 && bits != 3; ++i) {
+                const int token = (threadIdx.x / kHeadDim) * 32 + 8 * i;
+                const int64_t at = ((int64_t)table[page_at(tile * PPT + token / B)] * H + h) * (B * kHeadDim);
+                const ulonglong2 v = *reinterpret_cast<const ulonglong2*>(a.v_pool + at + dim * B + token % B);
 #pragma nounroll
-                        for (int c = 0; a.cap_in == 0.f && c < kHeadDim; ++c) most = max(most, a.k_pool[at + token % B * kHeadDim + c] & 0x7fffu);
-                        bits |= most >= 0x7f80u ? 3u : x >> 15 != 0 ? 2u : 1u;
-                    }
+                for (int e = 0; e < 8; ++e) {
+                    const uint32_t x = (uint32_t)((e < 4 ? v.x : v.y) >> (16 * (e & 3))) & 0xffffu;
+                    if ((x & 0x7f80u) != 0x7f80u) continue;
+                    Magnitudes most = {(unsigned short)(x & 0x7fu ? 0x7f80 : 0), 0};
+                    const uint4* key = reinterpret_cast<const uint4*>(a.k_pool + at + (token % B + e) * kHeadDim);
+#pragma nounroll
+                    for (int c = 0; c < kHeadDim / 8 && a.cap_in == 0.f && most.x < 0x7f80 && most.y < 0x7f80; ++c) most = larger(most, key[c]);
+                    bits |= most.x >= 0x7f80 || most.y >= 0x7f80 ? 3u : x >> 15 != 0 ? 2u : 1u;
                 }
+            }
+        }
         uint32_t* of_dim = reinterpret_cast<uint32_t*>(stages);
         of_dim[threadIdx.x] = bits;
         __syncthreads();

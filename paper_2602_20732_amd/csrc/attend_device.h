@@ -281,8 +281,8 @@ __device__ __forceinline__ void merge_parts(const AttendArgs& a, const Span& spa
             // A factor may come to 0 where the weights that it rescales do not: an infinite sum stays infinite.  (Looked for behind the sums: a choice a product
             // in code that runs once, cold, cost 1.5 to 2.7 us a launch.)
             const float any_nan = (x[y][0] + x[y][1]) + (x[y][2] + x[y][3]);
-            if (__builtin_expect(__any(any_nan != any_nan), 0)) {
-                x[y][0] = x[y][1] = x[y][2] = x[y][3] = 0.f;
+            if (__builtin_expect(any_nan != any_nan, 0)) {
+                float again[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma nounroll
                 for (int s = 0; s < n_parts; ++s) {
                     const int64_t part = number(s);
@@ -291,8 +291,10 @@ __device__ __forceinline__ void merge_parts(const AttendArgs& a, const Span& spa
                     const float2 lo = __builtin_bit_cast(float2, observe_u64(at)), hi = __builtin_bit_cast(float2, observe_u64(at + kOtherPair<kLines>));
                     const float v[4] = {lo.x, lo.y, hi.x, hi.y};
 #pragma unroll
-                    for (int d = 0; d < 4; ++d) x[y][d] += fabsf(v[d]) == INFINITY ? v[d] : v[d] * by;
+                    for (int d = 0; d < 4; ++d) again[d] += fabsf(v[d]) == INFINITY ? v[d] : v[d] * by;
                 }
+#pragma unroll
+                for (int d = 0; d < 4; ++d) x[y][d] = x[y][d] != x[y][d] ? again[d] : x[y][d];
             }
             const float inv = l[y] == 0.f ? 0.f : 1.f / l[y];
             if (row0 + r[y] < n_rows)
