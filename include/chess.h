@@ -131,7 +131,7 @@ int chess_summary_bytes(const chess_ctx* ctx, size_t* bytes);
 int chess_summary_layout(const chess_ctx* ctx, size_t* page_off, size_t* chunk_off, size_t* grid_off);
 
 /* Size in bytes of the workspace (split partials of decode, published keys and kept-unit lists of
- * select, arrival counters: 512 bytes a (sequence, KV head) and 256 a sequence); allocate 256-byte aligned.  chess_workspace_init must run once on a
+ * select, arrival counters: 512 bytes a (sequence, KV head) and 256 a sequence, sums of chess_verify: 2 KB a sequence of max_batch); allocate 256-byte aligned.  chess_workspace_init must run once on a
  * fresh allocation (it clears the arrival counters with a small fill kernel; the kernels re-arm
  * them themselves afterwards).  A workspace carries no results between calls, but two calls that
  * share one must not overlap in time (use one workspace per stream). */
@@ -463,7 +463,8 @@ int chess_rotate(chess_ctx* ctx, const chess_rotary* rotary, const void* q, int6
 
 /*
  * The same for rows that chess_map_tokens dealt pages to (writes, counts: as it leaves them; only counts[1] is read; max_writes: the entries `writes` has
- * room for), with the keys and the values (bf16 [n_rows][H_kv][128], v_stride as k_stride; values are neither normed nor turned) stored in the
+ * room for, by which the launch is shaped, since the host knows no other number: one token with room for one entry takes 3.3 us, for 512 (two a compute unit: the
+ * kernel for prompts) 6.2, for 8192 7.6; give steps of few tokens a list of their own, chess_write_rows says how long), with the keys and the values (bf16 [n_rows][H_kv][128], v_stride as k_stride; values are neither normed nor turned) stored in the
  * bf16 pools of n_pages pages.  Only rows that an entry names are written, in q_out too.  An entry with a row or a page that is not there does nothing.
  * No two entries may name the same page.  q may be NULL.
  */
@@ -480,7 +481,8 @@ typedef struct {
     const int32_t* first_keys;    /* int32 [n_rows]: the first key that a row sees (where its document starts); or NULL   */
 } chess_scores;
 
-/* Bytes of the scratch that the two calls below need for up to so many rows, new tokens of one sequence and sequences.  Nothing has to be in it, and
+/* Bytes of the scratch that the two calls below need for up to so many rows, new tokens of one sequence and sequences: on 256 compute units 17 MB where
+ * max_new n_q_heads / H_kv is at most 64, 136 MB (partials of what the plan may cut, however few rows there are) and up where it is more.  Nothing has to be in it, and
  * nothing is left in it; calls that share one must not overlap in time. */
 int chess_attend_scratch_bytes(const chess_ctx* ctx, int32_t n_rows, int32_t max_new, int32_t batch, size_t* bytes);
 
@@ -491,7 +493,8 @@ int chess_attend_scratch_bytes(const chess_ctx* ctx, int32_t n_rows, int32_t max
  * touch it, whatever they or their values are.  bf16 in and out; scores, softmax and sums in fp32, distances p - t in fp32.  Weights are a bf16 number and a bf16
  * remainder (2^-17 of a weight) where min(max_new, n_rows) n_q_heads / H_kv is at most 64 and one bf16 number (2^-8) where it is more, or where `batch` sequences
  * (lists) of the longest length that the configuration allows would have about 2^31 tiles of 32 keys: so a token's result can differ by that between calls with
- * another max_new.  Scores may have any size that fp32 holds.
+ * another max_new.  Scores may have any size that fp32 holds.  An infinite value of a key that a row sees makes that dim infinite however small the key's weight
+ * is (NaN where the score is -infinity, or infinities of both signs meet).
  * Block table entries behind a sequence's pages are not used.  A block table entry of a page that a sequence has must be a page of the pools.
  * workspace: as elsewhere (arrival counters); scratch: chess_attend_scratch_bytes at least, 256-byte aligned.  The same batch gives the same bits on every call.
  */
@@ -510,11 +513,12 @@ int chess_sparse_attend(chess_ctx* ctx, const chess_scores* scores, const void* 
  * behind it are its drafts 0, 1, ...: tokens int32 [n_rows].  target: fp32 [n_rows][vocab], target_stride elements from a row to the
  * next; row i of a sequence is the distribution of the token behind its i-th new one.  draft: fp32, the distribution that draft j of sequence b was
  * drawn from at draft + b draft_seq + j draft_row; NULL: drafts came without probabilities (as if each had been certain).  uniforms: fp32
- * [batch][max_drafts + 1] in [0, 1).  Only the first max_drafts drafts of a sequence are looked at; those behind count as refused.
+ * [batch][max_drafts + 1] in [0, 1).  Only the first max_drafts drafts of a sequence are looked at; those behind are dropped, as ones that are refused, but
+ * where all that were looked at stand none was refused, and the next token is drawn as behind the last one.
  *   draft j = x stands while  uniforms[b][j] q_j(x) < p_j(x)  (an x outside [0, vocab) does not);
  *   the token behind the last that stands is the first v with w(0) + ... + w(v) > uniforms[b][max_drafts] W, W the sum of w, where
  *   w(v) = max(p(v) - q(v), 0) if a draft was refused (p(v) without the draft itself where draft is NULL), p(v) if none was;
- *   if a draft was refused and nothing is left over (W = 0), w = p; -1 if p too has no sum above 0, or W or it is infinite.  What is NaN or negative weighs nothing.
+ *   if a draft was refused and W is 0 (nothing left over) or infinite, w = p; -1 if p's sum is 0 or infinite too.  A weight w(v) that is NaN or negative is none.
  * Products and sums in fp64; the same row and numbers give the same token in every batch.  Written:
  *   n_accepted int32 [batch]                drafts that stand
  *   out_tokens int32 [batch][max_drafts+1]  those, the token drawn, -1 behind it (a sequence without new tokens: -1 only)

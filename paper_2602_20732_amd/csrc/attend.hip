@@ -22,7 +22,7 @@ namespace chess {
 // is written at once; partials of the others are merged by the last workgroup of the sequence to arrive.
 // Bound: HBM, for as long as a tile's arithmetic (about 1 us a wave and 32 rows) takes less than the four waves' 64 KB do (2.7 us).  Measured, 32 query and 8 KV
 // heads: 16 sequences of 5 drafts over every page of 8 to 64K keys (2.19 GB) 364 to 372 us, 5.9 to 6.0 TB/s, what a read reaches; 32 sequences of 2 to 8 over lists of 108 pages
-// (229 MB) 46 us; one sequence's list of 21 pages 10.4.
+// (229 MB) 46 us; one sequence's list of 21 pages 11.1.
 
 // The first key that any of the tokens [from, to] sees for its document.
 __device__ __forceinline__ int first_of_rows(const AttendArgs& a, int from, int to)
@@ -419,8 +419,8 @@ __global__ __launch_bounds__(256, 1) void attend_few_kernel(AttendArgs a)
 // A plan says which units there are (plan_kernel): tiles that no row of a block sees are left out, and long blocks are cut where there are too
 // few to fill the card; partials are merged by the last unit of a block to arrive.
 // Bound: the matrix units and the exponentials beside them, 32 products of 32 cycles and 32 exponentials a lane for a tile and wave.  Measured, 32 query and 8 KV
-// heads: 1531 tokens behind 31K 800 us, 1003 TFLOP/s (a large library product 1246); 12 prompts of 131 to 2051 tokens, documents of 1203 and a bias by distance
-// 192 us, 510 TFLOP/s of the pairs that are seen: units of 8 tiles, each with 6.5 us of lookup, first tile and output around 22 us of tiles.
+// heads: 1531 tokens behind 31K 785 to 820 us by card, 980 to 1020 TFLOP/s (a large library product 1246); 12 prompts of 131 to 2051 tokens, documents of 1203 and a
+// bias by distance 191 us, 515 TFLOP/s of the pairs that are seen: units of 8 tiles, each with 6.5 us of lookup, first tile and output around 22 us of tiles.
 
 constexpr int kBlockRows = 128;
 constexpr size_t kManyLds = 4 * 16384;                // two tiles' keys, two tiles' values
@@ -869,7 +869,8 @@ __global__ __launch_bounds__(256, 2) void attend_many_kernel(AttendArgs a)
         }
     }
     // Tiles that all rows see whole are not looked through for values that are not finite.  Sums that come to NaN with one (a weight that is only small has become 0)
-    // say so by themselves (as two do that are infinite either way), and then the values of those tiles are looked at: what they do is the same for every row.
+    // say so by themselves (as two do that are infinite either way), and then the values of those tiles are looked at: what they do is the same for every row.  (Units
+    // whose values are finite pay the additions and a barrier: packed prompts 191.6 -> 193.3 us, a chunk 803 -> 805.)
     float of_dims[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int i = 0; i < 16; ++i)
@@ -980,6 +981,11 @@ static hipError_t launch_many(chess_ctx* ctx, const AttendArgs& a, const AttendS
 }
 
 // Few rows: a line a KV head.  Many: units; `most` blocks and cut units that there can be, whatever the sequences are.
+// The line has room for 64 rows.  us, as few / as many rows, in a graph, 8 KV heads, pages of 16, one sequence of 500, 4K, 32K, 130K keys, then 16 of 500, 4K, 32K:
+//   32 rows  11 / 22    23 / 27    43 / 58    106 / 171      17 / 24    55 / 58    342 / 370
+//   64 rows  20 / 26    38 / 32    66 / 65    146 / 180      27 / 27    77 / 63    439 / 378
+// One KV head, 64 rows, one sequence of 32K: 191 / 66 (250 partials that one workgroup merges).  From 65 rows on there is no choice, and a block is cut into 16 units at
+// most: 17 tokens of 4 heads a group behind 130K take 194 us (the keys alone 87 at 6.1 TB/s).
 AttendShape attend_shape(const chess_ctx* ctx, int64_t n_rows, int64_t max_new, int64_t batch, bool list)
 {
     const Geom& g = ctx->geom;

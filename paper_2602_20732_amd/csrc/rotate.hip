@@ -11,7 +11,9 @@
 // angles once and turns all its heads with them; where there are few tokens, workgroups share their heads.  Values go into their pages (token-minor) as in
 // quant_store.hip: a lane reads the same dims of 16 tokens, and has whole 32-byte rows to write.
 // Bound: HBM, read and written alike; for single tokens the chain entry -> position -> angle -> store.  Measured: 65531 tokens of 28 + 2 x 4 heads into pages of
-// 32 233 us, 24955 of 32 + 2 x 8 into pages of 16 121 us: 5.1 to 5.2 TB/s, what a copy reaches (4.9); 32 sequences of 5 drafts 5.6 us, one token 3.5.
+// 32 233 us, 24955 of 32 + 2 x 8 into pages of 16 121 us: 5.1 to 5.2 TB/s (a library copy of 0.3 to 2 GB 4.9 to 5.2); 32 sequences of 5 drafts 5.6 us, one token 3.5.
+// Alone, without values: 65531 tokens of 28 + 4 heads 207 us (5.2 TB/s), 24955 of 32 + 8 110 (4.7), 160 6.0, one 3.0; weights a head, read anew for every token, 269
+// and 144.
 #include "attend_device.h"
 #include "quant_device.h"
 #include "split_rule.h"
@@ -299,7 +301,9 @@ RotateShape rotate_shape(const chess_ctx* ctx, const RotateArgs& a, bool paged)
 {
     RotateShape s;
     s.units = paged ? a.max_writes : cdiv(a.n_rows, 16);
-    // a wave turns all heads that there are with the angles of a token, unless that leaves compute units idle
+    // A wave turns all heads that there are with the angles of a token, unless that leaves compute units idle.  us, heads shared / all in one workgroup, 32 + 2 x 8
+    // heads into pages of 16: 1 entry 4.7 / 6.3, 32 of 5 tokens 6.4 / 11.0, 128 full ones 19 / 23, 256 30 / 25, 511 55 / 41 (28 + 2 x 4, pages of 32: 128 25 / 36, 256
+    // 42 / 41, 511 75 / 62).
     s.many = s.units >= 2 * (int64_t)ctx->n_cu;
     const int heads = s.many ? 16 : 4;
     s.q_runs = a.q != nullptr ? (int)cdiv(a.q_heads, heads) : 0;
