@@ -278,6 +278,7 @@ __device__ __forceinline__ void merge_parts(const AttendArgs& a, const Span& spa
         }
 #pragma unroll
         for (int y = 0; y < kPieces; ++y) {
+            if (row0 + r[y] >= n_rows) continue;
             // A factor may come to 0 where the weights that it rescales do not: an infinite sum stays infinite.  (Looked for behind the sums: a choice a product
             // in code that runs once, cold, cost 1.5 to 2.7 us a launch.)
             const float any_nan = (x[y][0] + x[y][1]) + (x[y][2] + x[y][3]);
@@ -297,9 +298,8 @@ __device__ __forceinline__ void merge_parts(const AttendArgs& a, const Span& spa
                 for (int d = 0; d < 4; ++d) x[y][d] = x[y][d] != x[y][d] ? again[d] : x[y][d];
             }
             const float inv = l[y] == 0.f ? 0.f : 1.f / l[y];
-            if (row0 + r[y] < n_rows)
-                *reinterpret_cast<uint2*>(a.out + row_at(a, span, h, row0 + r[y]) * kHeadDim + dim[y]) =
-                    make_uint2(two_bf16(x[y][0] * inv, x[y][1] * inv), two_bf16(x[y][2] * inv, x[y][3] * inv));
+            *reinterpret_cast<uint2*>(a.out + row_at(a, span, h, row0 + r[y]) * kHeadDim + dim[y]) =
+                make_uint2(two_bf16(x[y][0] * inv, x[y][1] * inv), two_bf16(x[y][2] * inv, x[y][3] * inv));
         }
     }
 }
