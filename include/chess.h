@@ -131,8 +131,8 @@ int chess_summary_bytes(const chess_ctx* ctx, size_t* bytes);
 int chess_summary_layout(const chess_ctx* ctx, size_t* page_off, size_t* chunk_off, size_t* grid_off);
 
 /* Size in bytes of the workspace (split partials of decode, published keys and kept-unit lists of
- * select, arrival counters: 512 bytes a (sequence, KV head) and 256 a sequence, sums of chess_verify: 2 KB a sequence of max_batch); allocate 256-byte aligned.  chess_workspace_init must run once on a
- * fresh allocation (it clears the arrival counters with a small fill kernel; the kernels re-arm
+ * select, arrival counters: 512 bytes a (sequence, KV head) and 256 a sequence, sums of chess_verify: 2 KB a sequence of max_batch);
+ * allocate 256-byte aligned.  chess_workspace_init must run once on a fresh allocation (it clears the arrival counters with a small fill kernel; the kernels re-arm
  * them themselves afterwards).  A workspace carries no results between calls, but two calls that
  * share one must not overlap in time (use one workspace per stream). */
 int chess_workspace_bytes(const chess_ctx* ctx, size_t* bytes);
@@ -464,9 +464,9 @@ int chess_rotate(chess_ctx* ctx, const chess_rotary* rotary, const void* q, int6
 /*
  * The same for rows that chess_map_tokens dealt pages to (writes, counts: as it leaves them; only counts[1] is read; max_writes: the entries `writes` has
  * room for, by which the launch is shaped, since the host knows no other number: one token with room for one entry takes 3.3 us, for 512 (two a compute unit: the
- * kernel for prompts) 6.2, for 8192 7.6; give steps of few tokens a list of their own, chess_write_rows says how long), with the keys and the values (bf16 [n_rows][H_kv][128], v_stride as k_stride; values are neither normed nor turned) stored in the
- * bf16 pools of n_pages pages.  Only rows that an entry names are written, in q_out too.  An entry with a row or a page that is not there does nothing.
- * No two entries may name the same page.  q may be NULL.
+ * kernel for prompts) 6.2, for 8192 7.6; give steps of few tokens a list of their own, chess_write_rows says how long), with the keys and the values (bf16
+ * [n_rows][H_kv][128], v_stride as k_stride; values are neither normed nor turned) stored in the bf16 pools of n_pages pages.  Only rows that an entry
+ * names are written, in q_out too.  An entry with a row or a page that is not there does nothing. No two entries may name the same page.  q may be NULL.
  */
 int chess_rotate_store(chess_ctx* ctx, const chess_rotary* rotary, const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v,
                        int64_t v_stride, const int32_t* positions, int32_t n_rows, const int32_t* writes, const int32_t* counts, int32_t max_writes,
@@ -482,18 +482,19 @@ typedef struct {
 } chess_scores;
 
 /* Bytes of the scratch that the two calls below need for up to so many rows, new tokens of one sequence and sequences: on 256 compute units 17 MB where
- * max_new n_q_heads / H_kv is at most 64, 136 MB (partials of what the plan may cut, however few rows there are) and up where it is more.  Nothing has to be in it, and
- * nothing is left in it; calls that share one must not overlap in time. */
+ * max_new n_q_heads / H_kv is at most 64, 136 MB (partials of what the plan may cut, however few rows there are) and up where it is more.  Nothing has to
+ * be in it, and nothing is left in it; calls that share one must not overlap in time. */
 int chess_attend_scratch_bytes(const chess_ctx* ctx, int32_t n_rows, int32_t max_new, int32_t batch, size_t* bytes);
 
 /*
  * seq_lens: the lengths WITH the new tokens, which are a sequence's last (chess_map_tokens' lens_after); max_new: how many of them are attended at most, a
- * sequence (host value; of a sequence that has more the first ones are, at the positions that they have, and the others' rows of out are left).  q, out: bf16
- * [n_rows][n_q_heads][128].  The row of the token at position p attends to the keys t of its sequence with t <= p or t < prefix_lens[b], t >= first_keys[row], t > p - window; a row that sees no key is 0.  Keys that a row does not see do not
- * touch it, whatever they or their values are.  bf16 in and out; scores, softmax and sums in fp32, distances p - t in fp32.  Weights are a bf16 number and a bf16
- * remainder (2^-17 of a weight) where min(max_new, n_rows) n_q_heads / H_kv is at most 64 and one bf16 number (2^-8) where it is more, or where `batch` sequences
- * (lists) of the longest length that the configuration allows would have about 2^31 tiles of 32 keys: so a token's result can differ by that between calls with
- * another max_new.  Scores may have any size that fp32 holds.  An infinite value of a key that a row sees makes that dim infinite however small the key's weight
+ * sequence (host value; of a sequence that has more the first ones are, at the positions that they have, and the others' rows of out are left).
+ * q, out: bf16 [n_rows][n_q_heads][128].  The row of the token at position p attends to the keys t of its sequence with t <= p or t < prefix_lens[b],
+ * t >= first_keys[row], t > p - window; a row that sees no key is 0.  Keys that a row does not see do not touch it, whatever they or their values
+ * are.  bf16 in and out; scores, softmax and sums in fp32, distances p - t in fp32.  Weights are a bf16 number and a bf16 remainder (2^-17 of a weight)
+ * where min(max_new, n_rows) n_q_heads / H_kv is at most 64 and one bf16 number (2^-8) where it is more, or where `batch` sequences (lists) of the longest
+ * length that the configuration allows would have about 2^31 tiles of 32 keys: so a token's result can differ by that between calls with another
+ * max_new.  Scores may have any size that fp32 holds.  An infinite value of a key that a row sees makes that dim infinite however small the key's weight
  * is (NaN where the score is -infinity, or infinities of both signs meet).
  * Block table entries behind a sequence's pages are not used.  A block table entry of a page that a sequence has must be a page of the pools.
  * workspace: as elsewhere (arrival counters); scratch: chess_attend_scratch_bytes at least, 256-byte aligned.  The same batch gives the same bits on every call.

@@ -21,7 +21,7 @@ namespace chess {
 // Each wave has two tiles of LDS of its own: one is worked on, the next is on its way (loads that write LDS, no barrier).  A sequence that lies in one share
 // is written at once; partials of the others are merged by the last workgroup of the sequence to arrive.
 // Bound: HBM, for as long as a tile's arithmetic (about 1 us a wave and 32 rows) takes less than the four waves' 64 KB do (2.7 us).  Measured, 32 query and 8 KV
-// heads: 16 sequences of 5 drafts over every page of 8 to 64K keys (2.19 GB) 364 to 372 us, 5.9 to 6.0 TB/s, what a read reaches; 32 sequences of 2 to 8 over lists of 108 pages
+// heads: 16 sequences of 5 drafts over every page of 8 to 64K keys (2.19 GB) 360 to 373 us, 5.9 to 6.1 TB/s, what a read reaches; 32 sequences of 2 to 8 over lists of 108 pages
 // (229 MB) 46 us; one sequence's list of 21 pages 11.1.
 
 // The first key that any of the tokens [from, to] sees for its document.

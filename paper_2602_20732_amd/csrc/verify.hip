@@ -2,7 +2,8 @@
 //
 // Draft j (token x_j, drawn from q_j) stands while u_j q_j(x_j) < p_j(x_j).  The token behind the last that stands is drawn from
 //   w(v) = max(p(v) - q(v), 0)   where a draft was refused (p(v) without x_j where the draft came without probabilities),  p(v) otherwise,
-// as the first v with w(0) + ... + w(v) > u W, W the sum of all (drafts beyond those that may be looked at are dropped, not refused: the draw is from p(v)).  What a program decides by must not depend on how sums were cut:
+// as the first v with w(0) + ... + w(v) > u W, W the sum of all (drafts beyond those that may be looked at are dropped, not refused: the draw is from p(v)).
+// What a program decides by must not depend on how sums were cut:
 // u q is exact in fp64, sums are fp64 over pieces of 1024 that do not depend on the launch, so the same row gives the same token in every batch.
 // Each workgroup finds the refused draft for itself (a gather a draft, a wave's ballot), then sums its pieces of the one row that counts;
 // the last of a sequence to arrive looks through the pieces' sums, and through the one piece that the token is in.
